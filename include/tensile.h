@@ -352,6 +352,126 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
                         int32_t capacity, int32_t n_initial, int32_t *iv_tensor, int32_t *iv_out, int32_t *iv_in,
                         uint8_t *iv_kind, int32_t *n_intervals, int64_t *peak_trace, int64_t *final_peak);
 
+/* ------------------------------------------------- activations in 8 bits */
+
+/* A plan makes a saved activation cheaper by moving it over the host link or by
+ * recomputing it; the calls below are the third way: it stays, or travels, in
+ * 8.25 bits instead of 16 or 32 (a quarter or half of size_bytes, of the
+ * residence and of the transfer time x_i), and the backward pass reads it in
+ * that form.  A checkpoint holds a matrix of rows (tokens) x cols (features):
+ *   q[row*ld_q + col]              signed byte in [-127,127]
+ *   scale[row*ld_scale + col/32]   code c: the 32 columns' scale is 2^(c-127)
+ *   value = q * 2^(c-127);  c = 255: every value of the group is NaN;  c = 0: every value is 0
+ * Packing takes for each group the smallest power of two with
+ * rint(a / scale) <= 127, a the group's largest magnitude, with c in [1, 248]
+ * (in [1, 136] where the activations are of type TENSILE_F16): magnitudes below
+ * 2^-127 come back as zero, and no finite value comes back infinite.  A group that
+ * holds an infinity or a NaN gets c = 255 and q = 0, so that an overflow is
+ * still seen in the gradients.  Quotients are rounded to nearest, ties to even:
+ * no value is further than half a scale from what it stands for (that is at most 1/127.5 of
+ * the group's largest), except those that the largest code cuts off at 127 scales.
+ * A value has 7 significant bits, so it is a bfloat16 number exactly: the
+ * weight gradient multiplies it on the matrix cores without another rounding.
+ *
+ * All calls compute in 32 bits and round each output once.  A row's columns are
+ * contiguous; rows may lie further apart than cols (ld), at any alignment that
+ * suits the element.  Pointers are DEVICE pointers.  rows == 0 is allowed everywhere (gradients of
+ * parameters are then zero); cols >= 1.  An output may be the very matrix that is
+ * named for it below and must not overlap any other input or output.  The
+ * calls are asynchronous on hip_stream and never wait for the device.  Results do not
+ * depend on timing: the same call on the same inputs gives the same bits.
+ *
+ * tensile_layer_norm_backward and tensile_linear_grad use scratch memory that
+ * the tensile_ops handle keeps per stream, under the rules given at the top for a
+ * sequence's handle: any number of host threads may share one handle, a call that needs
+ * more than any earlier call on its stream allocates it, and a stream that is
+ * to be captured makes one call of the largest shape first. */
+
+#define TENSILE_F32 0
+#define TENSILE_BF16 1
+#define TENSILE_F16 2
+
+typedef struct tensile_ops tensile_ops; /* opaque; owns the scratch memory of the calls below */
+
+/* Creates a handle for the current HIP device; the calls that take it are made
+ * with that device current (TENSILE_E_INVAL otherwise).  *out is NULL on failure. */
+int tensile_ops_create(tensile_ops **out);
+
+/* Releases the handle and its scratch (synchronises the device). NULL is allowed. */
+void tensile_ops_free(tensile_ops *ops);
+
+/* A matrix in DEVICE memory, element (r, c) at data + (r*ld + c) elements. */
+typedef struct {
+    void *data;
+    int64_t rows, cols, ld;      /* ld >= cols                                                       */
+    int32_t type;                /* TENSILE_F32, TENSILE_BF16 or TENSILE_F16                         */
+} tensile_matrix;
+
+/* A checkpoint in DEVICE memory (see above). */
+typedef struct {
+    int8_t *q;
+    uint8_t *scale;
+    int64_t rows, cols;
+    int64_t ld_q, ld_scale;      /* ld_q >= cols, ld_scale >= ceil(cols/32)                          */
+} tensile_ckpt;
+
+/* c = x in 8 bits. */
+int tensile_ckpt_pack(tensile_ops *ops, const tensile_matrix *x, const tensile_ckpt *c, void *hip_stream);
+
+/* y = the values that c holds, rounded to y's type (exact in TENSILE_F32 and TENSILE_BF16). */
+int tensile_ckpt_unpack(tensile_ops *ops, const tensile_ckpt *c, const tensile_matrix *y, void *hip_stream);
+
+/* Layer norm of every row, after an optional residual sum:
+ *   s = x (+ residual);  mean and variance (1/cols) of s over the row;  rstd = 1/sqrt(variance + eps)
+ *   xhat = (s - mean)*rstd;  y = xhat*gamma + beta
+ *   residual    matrix like x, or NULL
+ *   gamma, beta [cols] of param_type, which is TENSILE_F32 or x's type
+ *   eps         >= 0
+ *   y           like x; may be x or residual itself
+ *   total       s, like x, or NULL; may be x or residual itself (but not y)
+ *   xhat        checkpoint of xhat, or NULL
+ *   rstd        [rows] float, or NULL */
+int tensile_layer_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *residual, const void *gamma,
+                       const void *beta, int32_t param_type, double eps, const tensile_matrix *y,
+                       const tensile_matrix *total, const tensile_ckpt *xhat, float *rstd, void *hip_stream);
+
+/* Its backward pass, from the checkpoint of xhat and rstd:
+ *   h = dy*gamma;  dx = rstd*(h - mean(h) - xhat*mean(h*xhat)) (+ dresidual)
+ *   dgamma = sum over the rows of dy*xhat;  dbeta = sum over the rows of dy
+ * dx is the gradient of x, of residual and of what else entered s.
+ *   dresidual   like dy, what reaches s past the norm (the gradient of total), or NULL
+ *   dx          like dy; may be dy or dresidual itself
+ *   dgamma, dbeta [cols] of param_type, both or neither NULL */
+int tensile_layer_norm_backward(tensile_ops *ops, const tensile_matrix *dy, const tensile_ckpt *xhat, const float *rstd,
+                                const void *gamma, int32_t param_type, const tensile_matrix *dresidual,
+                                const tensile_matrix *dx, void *dgamma, void *dbeta, void *hip_stream);
+
+/* y = x*Phi(x), Phi the normal distribution function; with tanh_form non-zero
+ * y = x*(1 + tanh(sqrt(2/pi)*(x + 0.044715*x^3)))/2.
+ *   y   like x; may be x itself
+ *   c   checkpoint of x, or NULL */
+int tensile_gelu(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *y, const tensile_ckpt *c,
+                 int32_t tanh_form, void *hip_stream);
+
+/* dx = dy * (derivative of the above at the x that c holds).
+ *   dx    like dy; may be dy itself
+ *   y_c   checkpoint of gelu(x), for the weight gradient of the layer that read it (which so need not be kept
+ *         from the forward pass), or NULL; may be c itself */
+int tensile_gelu_backward(tensile_ops *ops, const tensile_matrix *dy, const tensile_ckpt *c, const tensile_matrix *dx,
+                          const tensile_ckpt *y_c, int32_t tanh_form, void *hip_stream);
+
+/* Gradients of a linear layer's parameters (y = x W^T + bias, W: N x K) from
+ * dy: M x N and the checkpoint of its input:
+ *   dw[n,k] = sum_m dy[m,n]*X[m,k];  dbias[n] = sum_m dy[m,n]
+ * X is what c holds or, with gamma and beta given, a layer norm's output whose
+ * xhat c holds: X = xhat*gamma + beta.  (dw = gamma[k]*sum_m dy[m,n]*xhat[m,k] + beta[k]*dbias[n]:
+ * one checkpoint serves the norm and the layer behind it.)
+ *   gamma, beta [K] of param_type, both or neither NULL
+ *   dw          N x K, TENSILE_F32 or dy's type
+ *   dbias       [N] of dw's type, or NULL */
+int tensile_linear_grad(tensile_ops *ops, const tensile_matrix *dy, const tensile_ckpt *c, const void *gamma,
+                        const void *beta, int32_t param_type, const tensile_matrix *dw, void *dbias, void *hip_stream);
+
 /* --------------------------------------------------- testing and tuning aids */
 
 /* Forces a launch choice that the library otherwise makes from the shape of the

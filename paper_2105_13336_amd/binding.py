@@ -23,7 +23,9 @@ EXPORTS = ["tensile_last_error", "tensile_version", "tensile_tas_load", "tensile
            "tensile_tas_update_latencies",
            "tensile_tas_base_timeline", "tensile_eval_plans", "tensile_eval_plans_per_job", "tensile_eval_link", "tensile_apply_intervals", "tensile_score_candidates", "tensile_score_recompute",
            "tensile_validate_plans",
-           "tensile_greedy_plan", "tensile_eval_plans_static", "tensile_eval_score_plans", "tensile_tuning_set", "tensile_tuning_reset"]
+           "tensile_greedy_plan", "tensile_eval_plans_static", "tensile_eval_score_plans", "tensile_tuning_set", "tensile_tuning_reset",
+           "tensile_ops_create", "tensile_ops_free", "tensile_ckpt_pack", "tensile_ckpt_unpack", "tensile_layer_norm",
+           "tensile_layer_norm_backward", "tensile_gelu", "tensile_gelu_backward", "tensile_linear_grad"]
 
 
 class TensileError(RuntimeError):
@@ -50,6 +52,16 @@ class _GreedyOpts(ctypes.Structure):
                 ("msr_num", ctypes.c_void_p), ("msr_den", ctypes.c_int64), ("recompute", ctypes.c_int32)]
 
 
+class _Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("type", ctypes.c_int32)]
+
+
+class _Ckpt(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld_q", ctypes.c_int64), ("ld_scale", ctypes.c_int64)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2105_13336_amd/build.py` "
@@ -60,6 +72,16 @@ def _load():
     lib.tensile_tas_free.argtypes = [ctypes.c_void_p]
     lib.tensile_tuning_reset.restype = None
     lib.tensile_tuning_set.argtypes = [ctypes.c_char_p, ctypes.c_int]
+    lib.tensile_ops_free.restype = None
+    lib.tensile_ops_free.argtypes = [ctypes.c_void_p]
+    m, c, p, i32 = ctypes.POINTER(_Matrix), ctypes.POINTER(_Ckpt), ctypes.c_void_p, ctypes.c_int32
+    lib.tensile_ckpt_pack.argtypes = [p, m, c, p]
+    lib.tensile_ckpt_unpack.argtypes = [p, c, m, p]
+    lib.tensile_layer_norm.argtypes = [p, m, m, p, p, i32, ctypes.c_double, m, m, c, p, p]
+    lib.tensile_layer_norm_backward.argtypes = [p, m, c, p, p, i32, m, m, p, p, p]
+    lib.tensile_gelu.argtypes = [p, m, m, c, i32, p]
+    lib.tensile_gelu_backward.argtypes = [p, m, c, m, c, i32, p]
+    lib.tensile_linear_grad.argtypes = [p, m, c, p, p, i32, m, p, p]
     return lib
 
 
@@ -314,3 +336,161 @@ def tensile_greedy_plan(h: TasHandle, budget_bytes: int = 0, max_iters: int = 0,
     m = n.value
     return dict(iv_tensor=t[:m].copy(), iv_out=o[:m].copy(), iv_in=r[:m].copy(), iv_kind=k[:m].copy(),
                 peak_trace=trace[:m - n0 + 1].copy(), final_peak=fp.value, n_initial=n0)
+
+
+# ---------------------------------------------------------------- activations in 8 bits
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # TENSILE_F32, TENSILE_BF16, TENSILE_F16
+GROUP = 32                                                         # columns that share a scale
+
+
+class OpsHandle:
+    """Owner of a ``tensile_ops*`` (scratch memory of the operators, per stream); freed on ``close()`` / garbage collection."""
+
+    def __init__(self, ptr: int):
+        self._ptr = ptr
+
+    @property
+    def ptr(self) -> int:
+        if not self._ptr:
+            raise TensileError(TENSILE_E_INVAL, "operators' handle already freed")
+        return self._ptr
+
+    def close(self) -> None:
+        if self._ptr:
+            _lib.tensile_ops_free(self._ptr)
+            self._ptr = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Checkpoint:
+    """A matrix of activations in 8 bits: ``q`` [rows, cols] int8 and ``scale`` [rows, ceil(cols / 32)] uint8, both on the GPU,
+    the columns of a row contiguous (rows may lie further apart)."""
+
+    __slots__ = ("q", "scale", "_st")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor):
+        if q.dtype != torch.int8 or scale.dtype != torch.uint8 or q.dim() != 2 or scale.dim() != 2 or not q.is_cuda or not scale.is_cuda:
+            raise TensileError(TENSILE_E_INVAL, "checkpoint: need CUDA tensors q [rows, cols] int8 and scale [rows, ceil(cols/32)] uint8")
+        (rows, cols), (srows, groups) = q.shape, scale.shape
+        if srows != rows or groups != (cols + GROUP - 1) // GROUP or (cols > 1 and q.stride(1) != 1) or (groups > 1 and scale.stride(1) != 1):
+            raise TensileError(TENSILE_E_INVAL, f"checkpoint: q {tuple(q.shape)} and scale {tuple(scale.shape)} do not belong together, "
+                                                "or a row's columns are not contiguous")
+        self.q, self.scale = q, scale
+        self._st = _Ckpt(q.data_ptr(), scale.data_ptr(), rows, cols, q.stride(0) if rows > 1 else cols, scale.stride(0) if rows > 1 else groups)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda") -> "Checkpoint":
+        """Room for rows x cols values; rows start at multiples of 16 bytes."""
+        return cls(torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=device)[:, :cols],
+                   torch.empty(rows, (cols + GROUP - 1) // GROUP, dtype=torch.uint8, device=device))
+
+    @property
+    def shape(self):
+        return tuple(self.q.shape)
+
+    @property
+    def nbytes(self) -> int:
+        return self._st.rows * (self._st.ld_q + self._st.ld_scale)
+
+
+def _mat(t: Optional[torch.Tensor], name: str):
+    """[..., cols] with contiguous columns and evenly spaced rows, as a matrix."""
+    if t is None:
+        return None
+    code = _TYPES.get(t.dtype)
+    if code is None or not t.is_cuda or t.dim() < 1:
+        raise TensileError(TENSILE_E_INVAL, f"{name}: need a CUDA tensor of float32, bfloat16 or float16 with at least one dimension")
+    if t.dim() != 2:
+        if not t.is_contiguous():
+            raise TensileError(TENSILE_E_INVAL, f"{name}: a tensor of {t.dim()} dimensions has to be contiguous")
+        cols = t.shape[-1]
+        return _Matrix(t.data_ptr(), t.numel() // cols if cols else 0, cols, cols, code)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise TensileError(TENSILE_E_INVAL, f"{name}: the columns of a row have to be contiguous")
+    return _Matrix(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols, code)
+
+
+def _vec(t: Optional[torch.Tensor], dtype, n: int, name: str):
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise TensileError(TENSILE_E_INVAL, f"{name}: need a contiguous CUDA tensor of {dtype} with {n} elements")
+    return t.data_ptr()
+
+
+def _ck(c: Optional[Checkpoint]):
+    return None if c is None else c._st
+
+
+def _stream_ptr(stream) -> int:
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def tensile_ops_create() -> OpsHandle:
+    """A handle for the current device."""
+    out = ctypes.c_void_p()
+    _check(_lib.tensile_ops_create(ctypes.byref(out)))
+    return OpsHandle(out.value)
+
+
+def tensile_ops_free(ops: OpsHandle) -> None:
+    ops.close()
+
+
+def tensile_ckpt_pack(ops: OpsHandle, x: torch.Tensor, c: Checkpoint, stream=None) -> None:
+    """c = x in 8 bits"""
+    _check(_lib.tensile_ckpt_pack(ops.ptr, _mat(x, "x"), _ck(c), _stream_ptr(stream)))
+
+
+def tensile_ckpt_unpack(ops: OpsHandle, c: Checkpoint, y: torch.Tensor, stream=None) -> None:
+    """y = the values of c"""
+    _check(_lib.tensile_ckpt_unpack(ops.ptr, _ck(c), _mat(y, "y"), _stream_ptr(stream)))
+
+
+def tensile_layer_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, y: torch.Tensor, eps: float = 1e-5,
+                       residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, xhat: Optional[Checkpoint] = None,
+                       rstd: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y = layer norm of x (+ residual); total: the sum; xhat, rstd: what the backward pass reads"""
+    m = _mat(x, "x")
+    _check(_lib.tensile_layer_norm(ops.ptr, m, _mat(residual, "residual"), _vec(gamma, gamma.dtype, m.cols, "gamma"),
+                                   _vec(beta, gamma.dtype, m.cols, "beta"), _TYPES.get(gamma.dtype, -1), eps, _mat(y, "y"), _mat(total, "total"),
+                                   _ck(xhat), _vec(rstd, torch.float32, m.rows, "rstd"), _stream_ptr(stream)))
+
+
+def tensile_layer_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoint, rstd: torch.Tensor, gamma: torch.Tensor, dx: torch.Tensor,
+                                dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                                dresidual: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx = gradient through the norm (+ dresidual); dgamma, dbeta: the parameters' gradients"""
+    m = _mat(dy, "dy")
+    _check(_lib.tensile_layer_norm_backward(ops.ptr, m, _ck(xhat), _vec(rstd, torch.float32, m.rows, "rstd"),
+                                            _vec(gamma, gamma.dtype, m.cols, "gamma"), _TYPES.get(gamma.dtype, -1), _mat(dresidual, "dresidual"),
+                                            _mat(dx, "dx"), _vec(dgamma, gamma.dtype, m.cols, "dgamma"),
+                                            _vec(dbeta, gamma.dtype, m.cols, "dbeta"), _stream_ptr(stream)))
+
+
+def tensile_gelu(ops: OpsHandle, x: torch.Tensor, y: torch.Tensor, ckpt: Optional[Checkpoint] = None, tanh: bool = False, stream=None) -> None:
+    """y = gelu(x); ckpt: x in 8 bits"""
+    _check(_lib.tensile_gelu(ops.ptr, _mat(x, "x"), _mat(y, "y"), _ck(ckpt), 1 if tanh else 0, _stream_ptr(stream)))
+
+
+def tensile_gelu_backward(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dx: torch.Tensor, y_ckpt: Optional[Checkpoint] = None,
+                          tanh: bool = False, stream=None) -> None:
+    """dx = dy * gelu'(x) at the x that ckpt holds; y_ckpt: gelu(x) in 8 bits, for the next layer's weight gradient"""
+    _check(_lib.tensile_gelu_backward(ops.ptr, _mat(dy, "dy"), _ck(ckpt), _mat(dx, "dx"), _ck(y_ckpt), 1 if tanh else 0, _stream_ptr(stream)))
+
+
+def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: torch.Tensor, dbias: Optional[torch.Tensor] = None,
+                        gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dw [N, K] = dy^T X, dbias [N] = column sums of dy; X is what ckpt holds, or that * gamma + beta"""
+    m = _mat(dy, "dy")
+    K = ckpt._st.cols
+    param = None if gamma is None else gamma.dtype
+    _check(_lib.tensile_linear_grad(ops.ptr, m, _ck(ckpt), _vec(gamma, param, K, "gamma"), _vec(beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
+                                    _mat(dw, "dw"), _vec(dbias, dw.dtype, m.cols, "dbias"), _stream_ptr(stream)))

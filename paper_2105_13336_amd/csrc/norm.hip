@@ -1,0 +1,545 @@
+// Layer norm, forward and backward, with the normalised row kept in 8 bits.
+//
+// Bound by HBM: forward reads 2 and writes 3.03 bytes an element (bf16, with a checkpoint), backward reads 3.03 and writes 2.
+// A row is held in the registers of its team (16 lanes, a wavefront, or a workgroup) from the one load to the stores: the
+// mean, then the centred squares (no cancellation), then the outputs.  A team goes from row to row with the parameters in
+// registers and the next row's loads under way.  Backward keeps the two parameter gradients of its columns
+// in registers over all its rows; workgroups leave partial sums, which a second kernel adds up in a fixed order.
+#include "ops_device.h"
+
+namespace tensile {
+
+namespace {
+
+template <typename T>
+__device__ __forceinline__ T *at(const Matrix &m, int64_t row, int64_t col) {
+    return static_cast<T *>(m.p) + row * m.ld + col;
+}
+
+// Sum over the lanes of a team, the same value in each of them.  kWaves > 1: `slot` is one of the team's LDS rows,
+// which no wave still reads (see the callers).
+template <int kLanes, int kWaves>
+__device__ __forceinline__ float team_sum(float x, float *slot) {
+    if constexpr (kLanes == 16) {
+        return sum16(x);
+    } else if constexpr (kWaves == 1) {
+        return sum64(x);
+    } else {
+        const float s = sum64(x);
+        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = s;
+        __syncthreads();
+        float t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) t += slot[w];
+        return t;
+    }
+}
+
+// The columns a thread holds: chunk n covers columns (n * kTeam + lane in team) * 8 onwards.
+template <int kLanes, int kWaves, int kChunks>
+struct Team {
+    static constexpr int kThreads = kLanes * kWaves;                    // of a team
+    static constexpr int kBlock = kWaves == 1 ? 256 : kThreads;
+    static constexpr int kTeams = kBlock / kThreads;                    // of a workgroup
+};
+
+// Forward with rows of at most kThreads * 8 * kChunks columns.
+template <typename T, typename P, int kLanes, int kWaves, int kChunks>
+__global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_kernel(NormArgs a) {
+    using G = Team<kLanes, kWaves, kChunks>;
+    __shared__ float sums[2][kWaves];
+    const int lane = threadIdx.x % G::kThreads;
+    const int64_t teams = static_cast<int64_t>(gridDim.x) * G::kTeams;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * G::kTeams + threadIdx.x / G::kThreads;
+    int col[kChunks], left[kChunks];
+    float gamma[kChunks][8], beta[kChunks][8];
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n) {
+        col[n] = (n * G::kThreads + lane) * kChunk;
+        left[n] = a.cols - col[n];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gamma[n][j] = beta[n][j] = 0.0f;
+        if (left[n] > 0) {
+            load8(static_cast<const P *>(a.gamma) + col[n], left[n], gamma[n]);
+            load8(static_cast<const P *>(a.beta) + col[n], left[n], beta[n]);
+        }
+    }
+    const float n_cols = static_cast<float>(a.cols);
+    Raw8<T> x[kChunks], r[kChunks];
+    auto request = [&](int64_t at_row) {
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            x[n] = r[n] = Raw8<T>{};
+            if (left[n] > 0) {
+                x[n] = load_raw(at<const T>(a.x, at_row, col[n]), left[n]);
+                if (a.r.p) r[n] = load_raw(at<const T>(a.r, at_row, col[n]), left[n]);
+            }
+        }
+    };
+    if (row < a.rows) request(row);
+    for (; row < a.rows; row += teams) {
+        float v[kChunks][8];
+        float s = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            widen(x[n], v[n]);
+            if (a.r.p) {
+                float w[8];
+                widen(r[n], w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[n][j] += w[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[n][j];
+        }
+        if (row + teams < a.rows) request(row + teams);
+        if (a.t.p) {
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n)
+                if (left[n] > 0) store8(at<T>(a.t, row, col[n]), v[n], left[n]);
+        }
+        // (divided, not multiplied by 1/cols: the mean of a constant row whose sum is exact is that constant.
+        // The two rows of `sums` are written in turn, with a barrier between a row's reading and its next writing)
+        const float mean = team_sum<kLanes, kWaves>(s, sums[0]) / n_cols;
+        s = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[n][j] = j < left[n] ? v[n][j] - mean : 0.0f;
+                s += v[n][j] * v[n][j];
+            }
+        }
+        const float var = team_sum<kLanes, kWaves>(s, sums[1]) / n_cols;
+        const float rstd = 1.0f / __builtin_sqrtf(var + a.eps);
+        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[n][j] *= rstd;
+                y[j] = __builtin_fmaf(v[n][j], gamma[n][j], beta[n][j]);
+            }
+            if (left[n] > 0) store8(at<T>(a.y, row, col[n]), y, left[n]);
+            if (a.c.q) {
+                if (left[n] < kChunk) {                                  // (0 * inf: a missing column would be NaN)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j >= left[n]) v[n][j] = 0.0f;
+                }
+                uint32_t code;
+                const u32x2 w = pack8(v[n], static_cast<uint32_t>(a.cap), code);
+                if (left[n] > 0) {
+                    store_q(a.c.q + row * a.c.ld_q + col[n], w, left[n]);
+                    if (col[n] % kGroup == 0) a.c.scale[row * a.c.ld_scale + col[n] / kGroup] = static_cast<uint8_t>(code);
+                }
+            }
+        }
+    }
+}
+
+// Forward with rows too long for the registers: a workgroup of 1024 threads passes over each row three times.
+template <typename T, typename P>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
+    __shared__ float sums[2][16];
+    const float n_cols = static_cast<float>(a.cols);
+    const int last = (a.cols + kGroup - 1) / kGroup * kGroup;            // a group's four lanes stay together
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        auto read = [&](int c, float (&v)[8]) {
+            const int left = a.cols - c;
+            if (left <= 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+                return;
+            }
+            load8(at<const T>(a.x, row, c), left, v);
+            if (a.r.p) {
+                float w[8];
+                load8(at<const T>(a.r, row, c), left, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += w[j];
+            }
+        };
+        float s = 0.0f, v[8];
+        for (int c = threadIdx.x * kChunk; c < last; c += 1024 * kChunk) {
+            read(c, v);
+            float p = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p += v[j];
+            s += p;
+        }
+        const float mean = team_sum<64, 16>(s, sums[0]) / n_cols;
+        s = 0.0f;
+        for (int c = threadIdx.x * kChunk; c < last; c += 1024 * kChunk) {
+            read(c, v);
+            float p = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = c + j < a.cols ? v[j] - mean : 0.0f;
+                p += d * d;
+            }
+            s += p;
+        }
+        const float var = team_sum<64, 16>(s, sums[1]) / n_cols;
+        const float rstd = 1.0f / __builtin_sqrtf(var + a.eps);
+        if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+        for (int c = threadIdx.x * kChunk; c < last; c += 1024 * kChunk) {
+            const int left = a.cols - c;
+            read(c, v);
+            if (a.t.p && left > 0) store8(at<T>(a.t, row, c), v, left);
+            float g[8], b[8], y[8];
+            if (left > 0) {
+                load8(static_cast<const P *>(a.gamma) + c, left, g);
+                load8(static_cast<const P *>(a.beta) + c, left, b);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = j < left ? (v[j] - mean) * rstd : 0.0f;
+                y[j] = left > 0 ? __builtin_fmaf(v[j], g[j], b[j]) : 0.0f;
+            }
+            if (left > 0) store8(at<T>(a.y, row, c), y, left);
+            if (a.c.q) {
+                uint32_t code;
+                const u32x2 w = pack8(v, static_cast<uint32_t>(a.cap), code);
+                if (left > 0) store_q(a.c.q + row * a.c.ld_q + c, w, left);
+                if (c % kGroup == 0) a.c.scale[row * a.c.ld_scale + c / kGroup] = static_cast<uint8_t>(code);
+            }
+        }
+    }
+}
+
+// Backward with rows of at most kThreads * 8 * kChunks columns; a.part: [workgroup][2][cols] or null.
+template <typename T, typename P, int kLanes, int kWaves, int kChunks>
+__global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_backward_kernel(NormArgs a) {
+    using G = Team<kLanes, kWaves, kChunks>;
+    constexpr int kSpan = G::kThreads * kChunk * kChunks;               // columns of a team
+    __shared__ float sums[2][2][kWaves];                                 // [row's parity][sum]
+    __shared__ float merge[G::kTeams > 1 ? G::kTeams * kSpan : 1];
+    const int lane = threadIdx.x % G::kThreads, team = threadIdx.x / G::kThreads;
+    const int64_t teams = static_cast<int64_t>(gridDim.x) * G::kTeams;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * G::kTeams + team;
+    int col[kChunks], left[kChunks];
+    float gamma[kChunks][8], dgamma[kChunks][8], dbeta[kChunks][8];
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n) {
+        col[n] = (n * G::kThreads + lane) * kChunk;
+        left[n] = a.cols - col[n];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gamma[n][j] = dgamma[n][j] = dbeta[n][j] = 0.0f;
+        if (left[n] > 0) load8(static_cast<const P *>(a.gamma) + col[n], left[n], gamma[n]);
+    }
+    const float inv = 1.0f / static_cast<float>(a.cols);
+    // A row as it lies in memory: 28 bytes a chunk (bf16) where its numbers would take 64.  It is widened twice, before and
+    // after the sums; `hide` keeps the compiler from holding on to the first result (1024 threads have 128 registers each).
+    struct Row {
+        Raw8<T> x[kChunks], r[kChunks];
+        u32x2 q[kChunks];
+        uint32_t code[kChunks];
+        float rstd;
+    };
+    auto request = [&](Row &w, int64_t at_row) {
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            w.x[n] = w.r[n] = Raw8<T>{};
+            w.q[n] = u32x2{0, 0};
+            w.code[n] = 0;
+            if (left[n] > 0) {
+                w.x[n] = load_raw(at<const T>(a.x, at_row, col[n]), left[n]);
+                w.q[n] = load_q(a.c.q + at_row * a.c.ld_q + col[n], left[n]);
+                w.code[n] = a.c.scale[at_row * a.c.ld_scale + col[n] / kGroup];
+                if (a.r.p) w.r[n] = load_raw(at<const T>(a.r, at_row, col[n]), left[n]);
+            }
+        }
+        w.rstd = a.rstd[at_row];
+    };
+    // (h = dy*gamma; a NaN group's missing columns belong to no sum)
+    auto numbers = [&](const Row &w, int n, float (&dy)[8], float (&h)[8], float (&xh)[8]) {
+        widen(w.x[n], dy);
+        unpack8(w.q[n], scale_of(w.code[n]), xh);
+        if (left[n] < kChunk) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j >= left[n]) xh[j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = dy[j] * gamma[n][j];
+    };
+    auto hide = [](Row &w) {
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            asm volatile("" : "+v"(w.x[n].v), "+v"(w.q[n]), "+v"(w.code[n]));
+            if constexpr (sizeof(T) == 4) asm volatile("" : "+v"(w.x[n].w));
+        }
+    };
+    Row now{};
+    if (row < a.rows) request(now, row);
+    int parity = 0;
+    for (; row < a.rows; row += teams) {
+        Row next{};
+        if (row + teams < a.rows) request(next, row + teams);
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            float dy[8], h[8], xh[8];
+            numbers(now, n, dy, h, xh);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                dgamma[n][j] = __builtin_fmaf(dy[j], xh[j], dgamma[n][j]);
+                dbeta[n][j] += dy[j];
+                s1 += h[j];
+                s2 = __builtin_fmaf(h[j], xh[j], s2);
+            }
+        }
+        // (one barrier a row: a row's two sums are read before the next row's barrier, and written again behind that)
+        float c1, c2;
+        if constexpr (kWaves == 1) {
+            c1 = team_sum<kLanes, 1>(s1, nullptr) * inv;
+            c2 = team_sum<kLanes, 1>(s2, nullptr) * inv;
+        } else {
+            s1 = sum64(s1);
+            s2 = sum64(s2);
+            if ((threadIdx.x & 63) == 0) {
+                sums[parity][0][threadIdx.x >> 6] = s1;
+                sums[parity][1][threadIdx.x >> 6] = s2;
+            }
+            __syncthreads();
+            c1 = c2 = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                c1 += sums[parity][0][w];
+                c2 += sums[parity][1][w];
+            }
+            c1 *= inv;
+            c2 *= inv;
+            parity ^= 1;
+        }
+        hide(now);
+#pragma unroll
+        for (int n = 0; n < kChunks; ++n) {
+            float dy[8], h[8], xh[8], d[8];
+            numbers(now, n, dy, h, xh);
+            if (a.r.p) widen(now.r[n], d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float e = now.rstd * (h[j] - c1 - xh[j] * c2);
+                d[j] = a.r.p ? d[j] + e : e;
+            }
+            if (left[n] > 0) store8(at<T>(a.y, row, col[n]), d, left[n]);
+        }
+        now = next;
+    }
+    if (!a.part) return;
+    float *part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        float(*own)[8] = half ? dbeta : dgamma;
+        if constexpr (G::kTeams == 1) {
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n)
+                if (left[n] > 0) store8(part + half * static_cast<int64_t>(a.cols) + col[n], own[n], left[n]);
+        } else {
+            if (half) __syncthreads();
+#pragma unroll
+            for (int n = 0; n < kChunks; ++n)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) merge[team * kSpan + col[n] + j] = own[n][j];
+            __syncthreads();
+            for (int c = threadIdx.x; c < kSpan && c < a.cols; c += G::kBlock) {
+                float s = 0.0f;
+#pragma unroll
+                for (int t = 0; t < G::kTeams; ++t) s += merge[t * kSpan + c];
+                part[half * static_cast<int64_t>(a.cols) + c] = s;
+            }
+        }
+    }
+}
+
+// Backward with rows too long for the registers, part one: dx.
+template <typename T, typename P>
+__global__ __launch_bounds__(1024) void norm_backward_long_kernel(NormArgs a) {
+    __shared__ float sums[2][16];
+    const float inv = 1.0f / static_cast<float>(a.cols);
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        auto read = [&](int c, float (&h)[8], float (&xh)[8]) {
+            const int left = a.cols - c;
+            float g[8];
+            load8(at<const T>(a.x, row, c), left, h);
+            load8(static_cast<const P *>(a.gamma) + c, left, g);
+            unpack8(load_q(a.c.q + row * a.c.ld_q + c, left), scale_of(a.c.scale[row * a.c.ld_scale + c / kGroup]), xh);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                h[j] *= g[j];
+                if (j >= left) xh[j] = 0.0f;
+            }
+        };
+        float s1 = 0.0f, s2 = 0.0f, h[8], xh[8];
+        for (int c = threadIdx.x * kChunk; c < a.cols; c += 1024 * kChunk) {
+            read(c, h, xh);
+            float p1 = 0.0f, p2 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                p1 += h[j];
+                p2 = __builtin_fmaf(h[j], xh[j], p2);
+            }
+            s1 += p1;
+            s2 += p2;
+        }
+        const float c1 = team_sum<64, 16>(s1, sums[0]) * inv;
+        const float c2 = team_sum<64, 16>(s2, sums[1]) * inv;
+        const float rstd = a.rstd[row];
+        for (int c = threadIdx.x * kChunk; c < a.cols; c += 1024 * kChunk) {
+            const int left = a.cols - c;
+            read(c, h, xh);
+            float d[8];
+            if (a.r.p) load8(at<const T>(a.r, row, c), left, d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float e = rstd * (h[j] - c1 - xh[j] * c2);
+                d[j] = a.r.p ? d[j] + e : e;
+            }
+            store8(at<T>(a.y, row, c), d, left);
+        }
+    }
+}
+
+// ... part two, before dx may overwrite dy: partial sums of the parameter gradients, 2048 columns and every gridDim.y-th row
+// to a workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a) {
+    const int c = (blockIdx.x * 256 + threadIdx.x) * kChunk, left = a.cols - c;
+    if (left <= 0) return;
+    float dgamma[8] = {}, dbeta[8] = {};
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        float dy[8], xh[8];
+        load8(at<const T>(a.x, row, c), left, dy);
+        unpack8(load_q(a.c.q + row * a.c.ld_q + c, left), scale_of(a.c.scale[row * a.c.ld_scale + c / kGroup]), xh);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            dgamma[j] = __builtin_fmaf(dy[j], xh[j], dgamma[j]);
+            dbeta[j] += dy[j];
+        }
+    }
+    float *part = a.part + static_cast<int64_t>(blockIdx.y) * 2 * a.cols;
+    store8(part + c, dgamma, left);
+    store8(part + a.cols + c, dbeta, left);
+}
+
+// dgamma, dbeta = the partial sums' columns added up: 32 columns and 32 strands to a workgroup, each strand every 32nd
+// partial sum, then the strands in order.
+template <typename P>
+__global__ __launch_bounds__(1024) void norm_gradients_kernel(const float *part, int32_t n_part, int32_t cols, P *dgamma, P *dbeta) {
+    __shared__ float strand[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x, width = 2 * static_cast<int64_t>(cols);
+    float s = 0.0f;
+    if (c < width) {
+#pragma unroll 8
+        for (int k = y; k < n_part; k += 32) s += part[k * width + c];
+    }
+    strand[y][x] = s;
+    __syncthreads();
+    if (y == 0 && c < width) {
+        s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) s += strand[k][x];
+        P out;
+        from_f32(s, out);
+        if (c < cols) dgamma[c] = out;
+        else dbeta[c - cols] = out;
+    }
+}
+
+template <typename F>
+void by_types(int type, int param_type, F f) {
+    if (type == TENSILE_F32) f(float{}, float{});
+    else if (type == TENSILE_BF16 && param_type == TENSILE_F32) f(bf16_t{}, float{});
+    else if (type == TENSILE_BF16) f(bf16_t{}, bf16_t{});
+    else if (param_type == TENSILE_F32) f(f16_t{}, float{});
+    else f(f16_t{}, f16_t{});
+}
+
+uint32_t grid_of(int64_t rows, int64_t teams, int64_t most) {
+    const int64_t n = (rows + teams - 1) / teams;
+    return static_cast<uint32_t>(n < most ? n : most);
+}
+
+}  // namespace
+
+int launch_norm(const ::tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type) {
+    const int64_t cus = ops->num_cus;
+    by_types(type, param_type, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+#define TS_NORM(lanes, waves, chunks, per_cu)                                                                              \
+    do {                                                                                                                   \
+        using G = Team<lanes, waves, chunks>;                                                                              \
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_kernel<T, P, lanes, waves, chunks>), dim3(grid_of(a.rows, G::kTeams, cus * per_cu)), \
+                           dim3(G::kBlock), 0, s, a);                                                                      \
+    } while (0)
+        if (a.cols <= 128) TS_NORM(16, 1, 1, 8);
+        else if (a.cols <= 512) TS_NORM(64, 1, 1, 8);
+        else if (a.cols <= 1024) TS_NORM(64, 1, 2, 4);
+        else if (a.cols <= 2048) TS_NORM(64, 4, 1, 8);
+        else if (a.cols <= 4096) TS_NORM(64, 4, 2, 4);
+        else if (a.cols <= 8192) TS_NORM(64, 8, 2, 2);
+        else if (a.cols <= 16384) TS_NORM(64, 16, 2, 1);
+        else hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_long_kernel<T, P>), dim3(grid_of(a.rows, 1, cus * 2)), dim3(1024), 0, s, a);
+#undef TS_NORM
+    });
+    TS_HIP(hipGetLastError());
+    return TENSILE_OK;
+}
+
+int launch_norm_backward(const ::tensile_ops *ops, hipStream_t s, const NormArgs &args, int type, int param_type, void *dgamma, void *dbeta) {
+    const int64_t cus = ops->num_cus;
+    NormArgs a = args;
+    // workgroups: what is resident, but partial sums (8 bytes a column each) stay small against the rows
+    struct Shape { int lanes, waves, chunks, teams, per_cu; };
+    const Shape sh = a.cols <= 128    ? Shape{16, 1, 1, 16, 4}
+                     : a.cols <= 512  ? Shape{64, 1, 1, 4, 4}
+                     : a.cols <= 1024 ? Shape{64, 1, 2, 4, 4}
+                     : a.cols <= 2048 ? Shape{64, 4, 1, 1, 4}
+                     : a.cols <= 4096 ? Shape{64, 4, 2, 1, 3}
+                     : a.cols <= 8192 ? Shape{64, 16, 1, 1, 1}
+                                       : Shape{0, 0, 0, 1, 1};
+    const bool is_long = sh.lanes == 0;
+    const int64_t n_columns = (static_cast<int64_t>(a.cols) + 2047) / 2048;      // (long rows)
+    uint32_t n_part = grid_of(a.rows, sh.teams, is_long ? (8 * cus + n_columns - 1) / n_columns : cus * sh.per_cu);
+    std::unique_lock<std::mutex> lock;
+    if (dgamma) {
+        OpsScratch &scratch = ops_scratch(ops, s);
+        lock = std::unique_lock<std::mutex>(scratch.mu);
+        const int rc = scratch.provide(static_cast<size_t>(n_part) * 2 * static_cast<size_t>(a.cols), "layer_norm_backward: partial sums");
+        if (rc != TENSILE_OK) return rc;
+        a.part = scratch.buf.p;
+    }
+    by_types(type, param_type, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        if (a.rows > 0) {
+#define TS_NORM(lanes, waves, chunks)                                                                                      \
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_backward_kernel<T, P, lanes, waves, chunks>), dim3(n_part),                    \
+                       dim3(Team<lanes, waves, chunks>::kBlock), 0, s, a)
+            if (a.cols <= 128) TS_NORM(16, 1, 1);
+            else if (a.cols <= 512) TS_NORM(64, 1, 1);
+            else if (a.cols <= 1024) TS_NORM(64, 1, 2);
+            else if (a.cols <= 2048) TS_NORM(64, 4, 1);
+            else if (a.cols <= 4096) TS_NORM(64, 4, 2);
+            else if (a.cols <= 8192) TS_NORM(64, 16, 1);
+            else {
+                if (dgamma)
+                    hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_columns_kernel<T>), dim3(static_cast<uint32_t>(n_columns), n_part), dim3(256), 0, s, a);
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_backward_long_kernel<T, P>), dim3(grid_of(a.rows, 1, cus * 2)), dim3(1024), 0, s, a);
+            }
+#undef TS_NORM
+        }
+        if (dgamma)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_gradients_kernel<P>), dim3(static_cast<uint32_t>((2 * static_cast<int64_t>(a.cols) + 31) / 32)),
+                               dim3(1024), 0, s, a.part, static_cast<int32_t>(n_part), a.cols, static_cast<P *>(dgamma), static_cast<P *>(dbeta));
+    });
+    TS_HIP(hipGetLastError());
+    return TENSILE_OK;
+}
+
+}  // namespace tensile

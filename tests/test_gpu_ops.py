@@ -471,6 +471,29 @@ def test_linear_grad_of_larger_tiles(ops):
         check_grad(ops, "bf16", "f32", M, N, K, affine="f32")
 
 
+def test_linear_grad_of_larger_tiles_at_odd_places(ops):
+    """Rows that start at any element, that end inside a load, and rows of the product that are split."""
+    for M, N, K in ((131, 2049, 2307), (2100, 2050, 2305), (33, 2056, 2320), (31, 2049, 2304), (544, 2048, 2304), (577, 2044, 2290)):
+        say(f"linear grad large, odd places {M}x{N}x{K}")
+        check_grad(ops, "bf16", "f32", M, N, K, affine="f32", skew=1)
+        check_grad(ops, "bf16", "bf16", M, N, K, affine="bf16")
+
+
+def test_linear_grad_of_larger_tiles_keeps_non_finite_values_apart(ops):
+    M, N, K = 70, 2050, 2300
+    rng = np.random.default_rng(16)
+    dy, v = rng.standard_normal((M, N)), rng.standard_normal((M, K))
+    dy[69, 3], dy[0, 2049] = np.inf, np.nan
+    v[69, 2290] = np.nan                               # its group: columns 2272 .. 2299
+    c, _ = filled(v)
+    dw, db = torch.empty(N, K, device="cuda"), torch.empty(N, device="cuda")
+    P.tensile_linear_grad(ops, up(dy, "bf16"), c, dw, dbias=db)
+    want = np.zeros((N, K), dtype=bool)
+    want[3], want[2049], want[:, 2272:] = True, True, True
+    assert np.array_equal(~np.isfinite(dw.cpu().numpy()), want)
+    assert np.array_equal(np.isinf(db.cpu().numpy()), np.arange(N) == 3) and np.array_equal(np.isnan(db.cpu().numpy()), np.arange(N) == 2049)
+
+
 def test_linear_grad_keeps_every_bit_of_the_gradient(ops):
     """One row: each element is one product of the gradient's 24 (or 11) bits with the checkpoint's 7."""
     rng = np.random.default_rng(4)

@@ -347,8 +347,8 @@ GROUP = 32                                                         # columns tha
 class OpsHandle:
     """Owner of a ``tensile_ops*`` (scratch memory of the operators, per stream); freed on ``close()`` / garbage collection."""
 
-    def __init__(self, ptr: int):
-        self._ptr = ptr
+    def __init__(self, ptr: int, device: int):
+        self._ptr, self.device = ptr, device
 
     @property
     def ptr(self) -> int:
@@ -429,15 +429,20 @@ def _ck(c: Optional[Checkpoint]):
     return None if c is None else c._st
 
 
-def _stream_ptr(stream) -> int:
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the current stream without a Stream object (2.8 us)
+
+
+def _stream_ptr(stream, ops: OpsHandle) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(ops.device) if _raw_stream else torch.cuda.current_stream(ops.device).cuda_stream
 
 
 def tensile_ops_create() -> OpsHandle:
     """A handle for the current device."""
     out = ctypes.c_void_p()
     _check(_lib.tensile_ops_create(ctypes.byref(out)))
-    return OpsHandle(out.value)
+    return OpsHandle(out.value, torch.cuda.current_device())
 
 
 def tensile_ops_free(ops: OpsHandle) -> None:
@@ -446,12 +451,12 @@ def tensile_ops_free(ops: OpsHandle) -> None:
 
 def tensile_ckpt_pack(ops: OpsHandle, x: torch.Tensor, c: Checkpoint, stream=None) -> None:
     """c = x in 8 bits"""
-    _check(_lib.tensile_ckpt_pack(ops.ptr, _mat(x, "x"), _ck(c), _stream_ptr(stream)))
+    _check(_lib.tensile_ckpt_pack(ops.ptr, _mat(x, "x"), _ck(c), _stream_ptr(stream, ops)))
 
 
 def tensile_ckpt_unpack(ops: OpsHandle, c: Checkpoint, y: torch.Tensor, stream=None) -> None:
     """y = the values of c"""
-    _check(_lib.tensile_ckpt_unpack(ops.ptr, _ck(c), _mat(y, "y"), _stream_ptr(stream)))
+    _check(_lib.tensile_ckpt_unpack(ops.ptr, _ck(c), _mat(y, "y"), _stream_ptr(stream, ops)))
 
 
 def tensile_layer_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, y: torch.Tensor, eps: float = 1e-5,
@@ -461,7 +466,7 @@ def tensile_layer_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, bet
     m = _mat(x, "x")
     _check(_lib.tensile_layer_norm(ops.ptr, m, _mat(residual, "residual"), _vec(gamma, gamma.dtype, m.cols, "gamma"),
                                    _vec(beta, gamma.dtype, m.cols, "beta"), _TYPES.get(gamma.dtype, -1), eps, _mat(y, "y"), _mat(total, "total"),
-                                   _ck(xhat), _vec(rstd, torch.float32, m.rows, "rstd"), _stream_ptr(stream)))
+                                   _ck(xhat), _vec(rstd, torch.float32, m.rows, "rstd"), _stream_ptr(stream, ops)))
 
 
 def tensile_layer_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoint, rstd: torch.Tensor, gamma: torch.Tensor, dx: torch.Tensor,
@@ -472,18 +477,18 @@ def tensile_layer_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoi
     _check(_lib.tensile_layer_norm_backward(ops.ptr, m, _ck(xhat), _vec(rstd, torch.float32, m.rows, "rstd"),
                                             _vec(gamma, gamma.dtype, m.cols, "gamma"), _TYPES.get(gamma.dtype, -1), _mat(dresidual, "dresidual"),
                                             _mat(dx, "dx"), _vec(dgamma, gamma.dtype, m.cols, "dgamma"),
-                                            _vec(dbeta, gamma.dtype, m.cols, "dbeta"), _stream_ptr(stream)))
+                                            _vec(dbeta, gamma.dtype, m.cols, "dbeta"), _stream_ptr(stream, ops)))
 
 
 def tensile_gelu(ops: OpsHandle, x: torch.Tensor, y: torch.Tensor, ckpt: Optional[Checkpoint] = None, tanh: bool = False, stream=None) -> None:
     """y = gelu(x); ckpt: x in 8 bits"""
-    _check(_lib.tensile_gelu(ops.ptr, _mat(x, "x"), _mat(y, "y"), _ck(ckpt), 1 if tanh else 0, _stream_ptr(stream)))
+    _check(_lib.tensile_gelu(ops.ptr, _mat(x, "x"), _mat(y, "y"), _ck(ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
 
 
 def tensile_gelu_backward(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dx: torch.Tensor, y_ckpt: Optional[Checkpoint] = None,
                           tanh: bool = False, stream=None) -> None:
     """dx = dy * gelu'(x) at the x that ckpt holds; y_ckpt: gelu(x) in 8 bits, for the next layer's weight gradient"""
-    _check(_lib.tensile_gelu_backward(ops.ptr, _mat(dy, "dy"), _ck(ckpt), _mat(dx, "dx"), _ck(y_ckpt), 1 if tanh else 0, _stream_ptr(stream)))
+    _check(_lib.tensile_gelu_backward(ops.ptr, _mat(dy, "dy"), _ck(ckpt), _mat(dx, "dx"), _ck(y_ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
 
 
 def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: torch.Tensor, dbias: Optional[torch.Tensor] = None,
@@ -493,4 +498,4 @@ def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: 
     K = ckpt._st.cols
     param = None if gamma is None else gamma.dtype
     _check(_lib.tensile_linear_grad(ops.ptr, m, _ck(ckpt), _vec(gamma, param, K, "gamma"), _vec(beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
-                                    _mat(dw, "dw"), _vec(dbias, dw.dtype, m.cols, "dbias"), _stream_ptr(stream)))
+                                    _mat(dw, "dw"), _vec(dbias, dw.dtype, m.cols, "dbias"), _stream_ptr(stream, ops)))

@@ -6,240 +6,292 @@
 // magnitude is two moves between lanes away and no element is read twice.
 #include "ops_device.h"
 
+#include <type_traits>
+
 namespace tensile {
 
 namespace {
 
 constexpr int kEachThreads = 256;
+constexpr int kAtOnce = 2;            // slots of a thread whose loads are under way together
 
-// Slots are numbered row by row.  A grid that has to go on advances by `drow` rows and `dslot` slots: one division a thread.
+// Where a thread works.  kDense: the matrices' rows follow each other without a gap and are whole groups, so all of it is one row:
+// slot k is columns 8k .. 8k+7, all there.  Else slots are numbered row by row, 4 * ceil(cols / 32) to a row.
 struct Walk {
-    int64_t rows, cols;
+    int64_t cols;
     int64_t total;                    // slots
     int64_t per_row;
-    int64_t drow, dslot;
+};
+template <bool kDense>
+struct Slot {
+    int64_t row, col;
+    int left;                         // columns of the slot's eight that exist; below 1: none (the last group's end)
+    __device__ __forceinline__ bool whole() const { return kDense || left >= kChunk; }
+    __device__ __forceinline__ bool any() const { return kDense || left > 0; }
+    template <typename T>
+    __device__ __forceinline__ T *in(const Matrix &m) const {
+        return static_cast<T *>(m.p) + (kDense ? col : row * m.ld + col);
+    }
+    __device__ __forceinline__ int8_t *q(const Ckpt &c) const { return c.q + (kDense ? col : row * c.ld_q + col); }
+    __device__ __forceinline__ uint8_t *scale(const Ckpt &c) const { return c.scale + (kDense ? col / kGroup : row * c.ld_scale + col / kGroup); }
+    __device__ __forceinline__ int count() const { return kDense ? kChunk : left; }
 };
 
-template <typename F>
-__device__ __forceinline__ void walk(const Walk &w, F f) {
-    int64_t slot = static_cast<int64_t>(blockIdx.x) * kEachThreads + threadIdx.x;
-    if (slot >= w.total) return;
-    int64_t row, k;
-    if (w.rows == 1) {
-        row = 0;
-        k = slot;
-    } else if (w.total <= UINT32_MAX) {
-        const uint32_t r = static_cast<uint32_t>(slot) / static_cast<uint32_t>(w.per_row);
-        row = r;
-        k = static_cast<uint32_t>(slot) - r * static_cast<uint32_t>(w.per_row);
-    } else {
-        row = slot / w.per_row;
-        k = slot - row * w.per_row;
-    }
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * kEachThreads;
-    for (;;) {
-        const int64_t col = k * kChunk, left = w.cols - col;
-        f(row, col, left < kChunk ? static_cast<int>(left) : kChunk);
-        slot += stride;
-        if (slot >= w.total) return;   // (a group's four lanes leave together)
-        row += w.drow;
-        k += w.dslot;
-        if (k >= w.per_row) {
-            k -= w.per_row;
-            ++row;
+// A workgroup takes kAtOnce * 256 consecutive slots: first all loads, then the rest.
+template <bool kDense, typename Load, typename Finish>
+__device__ __forceinline__ void walk(const Walk &w, Load load, Finish finish) {
+    constexpr int64_t kBlock = kAtOnce * kEachThreads;
+    auto place = [&](int64_t slot) __attribute__((always_inline)) -> Slot<kDense> {
+        if constexpr (kDense) {
+            return {0, slot * kChunk, kChunk};
+        } else {
+            int64_t row, k;
+            if (w.total <= UINT32_MAX) {
+                const uint32_t r = static_cast<uint32_t>(slot) / static_cast<uint32_t>(w.per_row);
+                row = r;
+                k = static_cast<uint32_t>(slot) - r * static_cast<uint32_t>(w.per_row);
+            } else {
+                row = slot / w.per_row;
+                k = slot - row * w.per_row;
+            }
+            const int64_t left = w.cols - k * kChunk;
+            return {row, k * kChunk, left < kChunk ? static_cast<int>(left) : kChunk};
+        }
+    };
+    for (int64_t base = blockIdx.x * kBlock; base < w.total; base += gridDim.x * kBlock) {
+        if (base + kBlock <= w.total) {
+            Slot<kDense> at[kAtOnce];
+            decltype(load(at[0])) raw[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                at[u] = place(base + u * kEachThreads + threadIdx.x);
+                raw[u] = load(at[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) finish(at[u], raw[u]);
+        } else {
+            for (int64_t slot = base + threadIdx.x; slot < w.total; slot += kEachThreads) {   // (a group's four lanes leave together)
+                const Slot<kDense> at = place(slot);
+                finish(at, load(at));
+            }
         }
     }
 }
 
-template <typename T>
-__device__ __forceinline__ T *at(const Matrix &m, int64_t row, int64_t col) {
-    return static_cast<T *>(m.p) + row * m.ld + col;
+template <typename T, bool kDense>
+__device__ __forceinline__ Raw8<T> read_raw(const Matrix &m, const Slot<kDense> &s) {
+    if (s.any()) return load_raw(s.template in<const T>(m), s.count());
+    return Raw8<T>{};
 }
-// (left <= 0: the slot lies behind the row's end, in its last group)
-template <typename T>
-__device__ __forceinline__ void read8(const Matrix &m, int64_t row, int64_t col, int left, float (&f)[8]) {
-    if (left > 0) {
-        load8(at<T>(m, row, col), left, f);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = 0.0f;
-    }
+template <typename T, bool kDense>
+__device__ __forceinline__ void write8(const Matrix &m, const Slot<kDense> &s, const float (&f)[8]) {
+    if (s.any()) store8(s.template in<T>(m), f, s.count());
 }
-template <typename T>
-__device__ __forceinline__ void write8(const Matrix &m, int64_t row, int64_t col, int left, const float (&f)[8]) {
-    if (left > 0) store8(at<T>(m, row, col), f, left);
+struct Held {
+    u32x2 q;
+    uint32_t code;
+};
+template <bool kDense>
+__device__ __forceinline__ Held read_ckpt(const Ckpt &c, const Slot<kDense> &s) {
+    Held h{u32x2{0, 0}, *s.scale(c)};
+    if (s.any()) h.q = load_q(s.q(c), s.count());
+    return h;
 }
-__device__ __forceinline__ void read_ckpt(const Ckpt &c, int64_t row, int64_t col, int left, float (&f)[8]) {
-    u32x2 w = {0, 0};
-    if (left > 0) w = load_q(c.q + row * c.ld_q + col, left);
-    unpack8(w, scale_of(c.scale[row * c.ld_scale + col / kGroup]), f);
-}
-__device__ __forceinline__ void write_ckpt(const Ckpt &c, int64_t row, int64_t col, int left, float (&f)[8], uint32_t cap) {
+template <bool kDense>
+__device__ __forceinline__ void write_ckpt(const Ckpt &c, const Slot<kDense> &s, float (&f)[8], uint32_t cap) {
     uint32_t code;
     const u32x2 w = pack8(f, cap, code);
-    if (left > 0) store_q(c.q + row * c.ld_q + col, w, left);
-    if (col % kGroup == 0) c.scale[row * c.ld_scale + col / kGroup] = static_cast<uint8_t>(code);
+    if (s.any()) store_q(s.q(c), w, s.count());
+    if ((threadIdx.x & 3) == 0) *s.scale(c) = static_cast<uint8_t>(code);
 }
 // Columns that do not exist take no part in a group's largest magnitude.
-__device__ __forceinline__ void blank(float (&f)[8], int left) {
-    if (left < kChunk) {
+template <bool kDense>
+__device__ __forceinline__ void blank(float (&f)[8], const Slot<kDense> &s) {
+    if (!s.whole()) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j >= left) f[j] = 0.0f;
+            if (j >= s.left) f[j] = 0.0f;
     }
 }
 
-// Phi(x) and phi(x) from one exponential and one reciprocal: the normal distribution's tail by Abramowitz and Stegun
-// 7.1.26 (error below 7.5e-8), 1 - Phi(|x|) = t*(a1 + ... + a5 t^4)*exp(-x^2/2)/2, t = 1/(1 + p|x|/sqrt 2).
-__device__ __forceinline__ void normal_cdf(float x, float &cdf, float &pdf) {
-    const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * x * x);     // exp(-x^2/2)
+// The normal distribution's tail by Abramowitz and Stegun 7.1.26 (error below 7.5e-8) from one exponential and one reciprocal:
+// 1 - Phi(|x|) = t*(a1 + ... + a5 t^4)*exp(-x^2/2)/2, t = 1/(1 + p|x|/sqrt 2).  e: exp(-x^2/2).
+__device__ __forceinline__ float normal_tail(float x, float &e) {
+    e = __builtin_amdgcn_exp2f(-0.72134752044448170f * x * x);
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.23164189f, __builtin_fabsf(x), 1.0f));
     float s = __builtin_fmaf(0.5307027145f, t, -0.7265760135f);
     s = __builtin_fmaf(s, t, 0.7107068705f);
     s = __builtin_fmaf(s, t, -0.142248368f);
     s = __builtin_fmaf(s, t, 0.127414796f);
-    const float tail = s * t * e;
-    cdf = x < 0.0f ? tail : 1.0f - tail;
-    pdf = 0.39894228040143268f * e;
+    return s * t * e;
 }
+// The tanh form: (1 + tanh u)/2 = 1/(1 + exp(-2u)).
+__device__ __forceinline__ float tanh_cdf(float x, float x2) {
+    const float u2 = x * __builtin_fmaf(0.071354816272f, x2, 1.5957691216f);            // 2u
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u2));
+}
+// (from |x| = 100 on the distribution function is 0 or 1: no overflow on the way)
+__device__ __forceinline__ float capped_square(float x) { return __builtin_amdgcn_fmed3f(x * x, 0.0f, 1e4f); }
 
-// What y = x*p and dy/dx = p + x*dp are made of.  The tanh form: (1 + tanh u)/2 = 1/(1 + exp(-2u)).
 template <bool kTanh>
-__device__ __forceinline__ void gelu_parts(float x, float &p, float &dp) {
+__device__ __forceinline__ float gelu(float x) {
     if constexpr (kTanh) {
-        const float x2 = __builtin_fminf(x * x, 1e4f);      // (from |x| = 100 on p is 0 or 1; no overflow on the way)
-        const float u2 = x * __builtin_fmaf(0.071354816272f, x2, 1.5957691216f);            // 2u
-        const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * u2);
-        p = __builtin_amdgcn_rcpf(1.0f + e);
-        dp = p * (1.0f - p) * __builtin_fmaf(0.214064448816f, x2, 1.5957691216f);           // p(1-p) * d(2u)/dx
+        return x * tanh_cdf(x, capped_square(x));
+    } else {                                        // x*Phi(x) = max(x, 0) - |x|*(1 - Phi(|x|))
+        float e;
+        const float tail = normal_tail(x, e);
+        const float most = __builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0.0f, 100.0f);
+        float above;
+        asm("v_max_f32 %0, 0, %1" : "=v"(above) : "v"(x));   // (fmax costs two more, to quiet a NaN; `tail` brings it in)
+        return __builtin_fmaf(-most, tail, above);
+    }
+}
+// y and dy/dx
+template <bool kTanh>
+__device__ __forceinline__ float gelu_slope(float x, float &y) {
+    if constexpr (kTanh) {
+        const float x2 = capped_square(x), p = tanh_cdf(x, x2);
+        const float dp = p * (1.0f - p) * __builtin_fmaf(0.214064448816f, x2, 1.5957691216f);   // p(1-p) * d(2u)/dx
+        y = x * p;
+        return __builtin_fmaf(x, dp, p);
     } else {
-        normal_cdf(x, p, dp);
+        float e;
+        const float tail = normal_tail(x, e), p = x < 0.0f ? tail : 1.0f - tail;
+        y = x * p;
+        return __builtin_fmaf(x, 0.39894228040143268f * e, p);
     }
 }
 
-template <typename T>
+template <typename T, bool kDense>
 __global__ __launch_bounds__(kEachThreads) void pack_kernel(Walk w, Matrix x, Ckpt c, uint32_t cap) {
-    walk(w, [&](int64_t row, int64_t col, int left) {
-        float f[8];
-        read8<T>(x, row, col, left, f);
-        write_ckpt(c, row, col, left, f, cap);
-    });
+    using S = Slot<kDense>;
+    walk<kDense>(
+        w, [&](const S &s) { return read_raw<T>(x, s); },
+        [&](const S &s, const Raw8<T> &raw) {
+            float f[8];
+            widen(raw, f);
+            write_ckpt(c, s, f, cap);
+        });
 }
 
-template <typename T>
+template <typename T, bool kDense>
 __global__ __launch_bounds__(kEachThreads) void unpack_kernel(Walk w, Ckpt c, Matrix y) {
-    walk(w, [&](int64_t row, int64_t col, int left) {
-        float f[8];
-        read_ckpt(c, row, col, left, f);
-        write8<T>(y, row, col, left, f);
-    });
+    using S = Slot<kDense>;
+    walk<kDense>(
+        w, [&](const S &s) { return read_ckpt(c, s); },
+        [&](const S &s, const Held &h) {
+            float f[8];
+            unpack8(h.q, scale_of(h.code), f);
+            write8<T>(y, s, f);
+        });
 }
 
-template <typename T, bool kTanh>
+template <typename T, bool kDense, bool kTanh>
 __global__ __launch_bounds__(kEachThreads) void gelu_kernel(Walk w, Matrix x, Matrix y, Ckpt c, uint32_t cap) {
-    walk(w, [&](int64_t row, int64_t col, int left) {
-        float f[8], g[8];
-        read8<T>(x, row, col, left, f);
+    using S = Slot<kDense>;
+    walk<kDense>(
+        w, [&](const S &s) { return read_raw<T>(x, s); },
+        [&](const S &s, const Raw8<T> &raw) {
+            float f[8], g[8];
+            widen(raw, f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float p, dp;
-            gelu_parts<kTanh>(f[j], p, dp);
-            g[j] = f[j] * p;
-        }
-        write8<T>(y, row, col, left, g);
-        if (c.q) write_ckpt(c, row, col, left, f, cap);
-    });
+            for (int j = 0; j < 8; ++j) g[j] = gelu<kTanh>(f[j]);
+            write8<T>(y, s, g);
+            if (c.q) write_ckpt(c, s, f, cap);
+        });
 }
 
-template <typename T, bool kTanh>
+template <typename T, bool kDense, bool kTanh>
 __global__ __launch_bounds__(kEachThreads) void gelu_backward_kernel(Walk w, Matrix dy, Ckpt c, Matrix dx, Ckpt y, uint32_t cap) {
-    walk(w, [&](int64_t row, int64_t col, int left) {
-        float f[8], g[8];
-        read8<T>(dy, row, col, left, g);
-        read_ckpt(c, row, col, left, f);
+    using S = Slot<kDense>;
+    struct Both {
+        Raw8<T> dy;
+        Held x;
+    };
+    walk<kDense>(
+        w, [&](const S &s) { return Both{read_raw<T>(dy, s), read_ckpt(c, s)}; },
+        [&](const S &s, const Both &raw) {
+            float f[8], g[8], v[8];
+            widen(raw.dy, g);
+            unpack8(raw.x.q, scale_of(raw.x.code), f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float p, dp;
-            gelu_parts<kTanh>(f[j], p, dp);
-            g[j] *= __builtin_fmaf(f[j], dp, p);
-            f[j] *= p;
-        }
-        write8<T>(dx, row, col, left, g);
-        if (y.q) {
-            blank(f, left);            // (a NaN group's missing columns)
-            write_ckpt(y, row, col, left, f, cap);
-        }
-    });
+            for (int j = 0; j < 8; ++j) g[j] *= gelu_slope<kTanh>(f[j], v[j]);
+            write8<T>(dx, s, g);
+            if (y.q) {
+                blank(v, s);           // (a NaN group's missing columns)
+                write_ckpt(y, s, v, cap);
+            }
+        });
 }
 
-// Rows that follow each other without a gap are one row: no slot is left empty and none has to be found by division.
-Walk make_walk(const ::tensile_ops *ops, const EachArgs &a, uint32_t *blocks) {
+Walk make_walk(const EachArgs &a, bool *dense, uint32_t *blocks) {
+    auto tight = [&](const Matrix &m) { return !m.p || m.ld == a.cols || a.rows == 1; };
+    auto tight_c = [&](const Ckpt &c) { return !c.q || (c.ld_q == a.cols && c.ld_scale == a.cols / kGroup) || a.rows == 1; };
+    *dense = a.cols % kGroup == 0 && tight(a.a) && tight(a.b) && tight_c(a.c) && tight_c(a.d);
     Walk w{};
-    w.rows = a.rows;
     w.cols = a.cols;
-    const bool whole = a.cols % kGroup == 0;
-    auto dense = [&](const Matrix &m) { return !m.p || m.ld == a.cols; };
-    auto dense_c = [&](const Ckpt &c) { return !c.q || (c.ld_q == a.cols && c.ld_scale == a.cols / kGroup); };
-    if (whole && dense(a.a) && dense(a.b) && dense_c(a.c) && dense_c(a.d)) {
-        w.rows = 1;
-        w.cols = a.rows * a.cols;
-    }
-    w.per_row = (w.cols + kGroup - 1) / kGroup * (kGroup / kChunk);
-    w.total = w.rows * w.per_row;
-    const int64_t want = (w.total + kEachThreads - 1) / kEachThreads;
-    const int64_t most = int64_t{ops->num_cus} * 8;
-    const int64_t n = want < most ? want : most;
-    const int64_t stride = n * kEachThreads;
-    w.drow = stride / w.per_row;
-    w.dslot = stride % w.per_row;
-    *blocks = static_cast<uint32_t>(n);
+    w.per_row = (a.cols + kGroup - 1) / kGroup * (kGroup / kChunk);
+    w.total = a.rows * w.per_row;
+    const int64_t want = (w.total + kAtOnce * kEachThreads - 1) / (kAtOnce * kEachThreads);
+    *blocks = static_cast<uint32_t>(want < (1 << 23) ? want : 1 << 23);
     return w;
 }
 
+// f(element, dense)
 template <typename F>
-int by_type(int type, F f) {
-    if (type == TENSILE_F32) f(float{});
-    else if (type == TENSILE_BF16) f(bf16_t{});
-    else f(f16_t{});
+int by_type(int type, bool dense, F f) {
+    auto with = [&](auto t) {
+        if (dense) f(t, std::true_type{});
+        else f(t, std::false_type{});
+    };
+    if (type == TENSILE_F32) with(float{});
+    else if (type == TENSILE_BF16) with(bf16_t{});
+    else with(f16_t{});
     TS_HIP(hipGetLastError());
     return TENSILE_OK;
 }
 
 }  // namespace
 
-int launch_pack(const ::tensile_ops *ops, hipStream_t s, const EachArgs &a, int type) {
+int launch_pack(const ::tensile_ops *, hipStream_t s, const EachArgs &a, int type) {
     uint32_t blocks;
-    const Walk w = make_walk(ops, a, &blocks);
-    return by_type(type, [&](auto t) {
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(pack_kernel<decltype(t)>), dim3(blocks), dim3(kEachThreads), 0, s, w, a.a, a.c,
+    bool dense;
+    const Walk w = make_walk(a, &dense, &blocks);
+    return by_type(type, dense, [&](auto t, auto d) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(pack_kernel<decltype(t), decltype(d)::value>), dim3(blocks), dim3(kEachThreads), 0, s, w, a.a, a.c,
                            static_cast<uint32_t>(a.cap));
     });
 }
 
-int launch_unpack(const ::tensile_ops *ops, hipStream_t s, const EachArgs &a, int type) {
+int launch_unpack(const ::tensile_ops *, hipStream_t s, const EachArgs &a, int type) {
     uint32_t blocks;
-    const Walk w = make_walk(ops, a, &blocks);
-    return by_type(type, [&](auto t) {
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(unpack_kernel<decltype(t)>), dim3(blocks), dim3(kEachThreads), 0, s, w, a.c, a.b);
+    bool dense;
+    const Walk w = make_walk(a, &dense, &blocks);
+    return by_type(type, dense, [&](auto t, auto d) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(unpack_kernel<decltype(t), decltype(d)::value>), dim3(blocks), dim3(kEachThreads), 0, s, w, a.c, a.b);
     });
 }
 
-int launch_gelu(const ::tensile_ops *ops, hipStream_t s, const EachArgs &a, int type, bool tanh_form) {
+int launch_gelu(const ::tensile_ops *, hipStream_t s, const EachArgs &a, int type, bool tanh_form) {
     uint32_t blocks;
-    const Walk w = make_walk(ops, a, &blocks);
-    return by_type(type, [&](auto t) {
+    bool dense;
+    const Walk w = make_walk(a, &dense, &blocks);
+    return by_type(type, dense, [&](auto t, auto d) {
         using T = decltype(t);
-        auto kernel = tanh_form ? gelu_kernel<T, true> : gelu_kernel<T, false>;
+        constexpr bool kD = decltype(d)::value;
+        auto kernel = tanh_form ? gelu_kernel<T, kD, true> : gelu_kernel<T, kD, false>;
         hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kEachThreads), 0, s, w, a.a, a.b, a.c, static_cast<uint32_t>(a.cap));
     });
 }
 
-int launch_gelu_backward(const ::tensile_ops *ops, hipStream_t s, const EachArgs &a, int type, bool tanh_form) {
+int launch_gelu_backward(const ::tensile_ops *, hipStream_t s, const EachArgs &a, int type, bool tanh_form) {
     uint32_t blocks;
-    const Walk w = make_walk(ops, a, &blocks);
-    return by_type(type, [&](auto t) {
+    bool dense;
+    const Walk w = make_walk(a, &dense, &blocks);
+    return by_type(type, dense, [&](auto t, auto d) {
         using T = decltype(t);
-        auto kernel = tanh_form ? gelu_backward_kernel<T, true> : gelu_backward_kernel<T, false>;
+        constexpr bool kD = decltype(d)::value;
+        auto kernel = tanh_form ? gelu_backward_kernel<T, kD, true> : gelu_backward_kernel<T, kD, false>;
         hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kEachThreads), 0, s, w, a.a, a.c, a.b, a.d, static_cast<uint32_t>(a.cap));
     });
 }

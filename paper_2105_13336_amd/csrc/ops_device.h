@@ -157,8 +157,10 @@ __device__ __forceinline__ void store_q(int8_t *p, u32x2 w, int left) {
 __device__ __forceinline__ float scale_of(uint32_t code) { return as_f32(code == kNanCode ? 0x7fc00000u : code << 23); }
 
 __device__ __forceinline__ void unpack8(u32x2 w, float scale, float (&f)[8]) {
+    uint32_t v[2] = {w[0], w[1]};
+    asm("" : "+v"(v[0]), "+v"(v[1]));  // (or the bytes are taken apart where they are loaded, by two more instructions each)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(static_cast<int8_t>(w[j / 4] >> (8 * (j % 4)))) * scale;
+    for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(static_cast<int8_t>(v[j / 4] >> (8 * (j % 4)))) * scale;
 }
 
 template <int kCtrl>
@@ -167,15 +169,21 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
     return x > y ? x : y;
 }
 
-// The four lanes 4k .. 4k+3 hold a group's 32 values (zero where there are none) and all of them call this.
-// Magnitudes are compared as integers: the order is that of the numbers, and infinities and NaN are above all others.
-__device__ __forceinline__ u32x2 pack8(float (&f)[8], uint32_t cap, uint32_t &code) {
+// The largest magnitude of a lane's eight, as the bits of a 32-bit number.  Magnitudes are compared as integers: the order is that
+// of the numbers, and infinities and NaN are above all others.
+__device__ __forceinline__ uint32_t largest(const float (&f)[8]) {
     uint32_t a = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint32_t m = as_u32(f[j]) & 0x7fffffffu;
         a = a > m ? a : m;
     }
+    return a;
+}
+
+// The four lanes 4k .. 4k+3 hold a group's 32 values (zero where there are none) and all of them call this.
+__device__ __forceinline__ u32x2 pack8(const float (&f)[8], uint32_t cap, uint32_t &code) {
+    uint32_t a = largest(f);
     a = quad_max<0xB1>(a);             // quad_perm [1,0,3,2]
     a = quad_max<0x4E>(a);             // quad_perm [2,3,0,1]
     // a = m * 2^E, 1 <= m < 2: the scale is 2^(E-6), or 2^(E-5) where m >= 127.5/64 (the quotient would round to 128)
@@ -183,21 +191,21 @@ __device__ __forceinline__ u32x2 pack8(float (&f)[8], uint32_t cap, uint32_t &co
     uint32_t c = up > 7 ? up - 6 : 1;
     const bool cut = c > cap;
     if (cut) c = cap;
+    // f / scale is exact, so the one rounding is that of the sum with 1.5 * 2^23, whose low byte is the integer
+    constexpr float kMiddle = 12582912.0f;
     const float inv = as_f32((254u - c) << 23);
+    float b[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[j] = __builtin_fmaf(f[j], inv, kMiddle);
     if (cut) {                         // 127 scales are the most that is held
-        const float most = 127.0f * as_f32(c << 23);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = __builtin_amdgcn_fmed3f(f[j], -most, most);
+        for (int j = 0; j < 8; ++j) b[j] = __builtin_amdgcn_fmed3f(b[j], kMiddle - 127.0f, kMiddle + 127.0f);
     }
-    // f * inv is exact, so the one rounding is that of the sum with 1.5 * 2^23, whose low byte is the integer
-    uint32_t b[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) b[j] = as_u32(__builtin_fmaf(f[j], inv, 12582912.0f));
     u32x2 w;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const uint32_t lo = __builtin_amdgcn_perm(b[4 * k + 1], b[4 * k], 0x0c0c0400);
-        const uint32_t hi = __builtin_amdgcn_perm(b[4 * k + 3], b[4 * k + 2], 0x04000c0c);
+        const uint32_t lo = __builtin_amdgcn_perm(as_u32(b[4 * k + 1]), as_u32(b[4 * k]), 0x0c0c0400);
+        const uint32_t hi = __builtin_amdgcn_perm(as_u32(b[4 * k + 3]), as_u32(b[4 * k + 2]), 0x04000c0c);
         w[k] = lo | hi;
     }
     if (a >= 0x7f800000u) {

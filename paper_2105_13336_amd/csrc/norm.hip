@@ -7,13 +7,37 @@
 // in registers over all its rows; workgroups leave partial sums, which a second kernel adds up in a fixed order.
 #include "ops_device.h"
 
+#include <type_traits>
+
 namespace tensile {
 
 namespace {
 
+// (a row's address plus 32 bits: the first is scalar where the row is)
 template <typename T>
-__device__ __forceinline__ T *at(const Matrix &m, int64_t row, int64_t col) {
-    return static_cast<T *>(m.p) + row * m.ld + col;
+__device__ __forceinline__ T *at(const Matrix &m, int64_t row, int col) {
+    return static_cast<T *>(m.p) + row * m.ld + static_cast<uint32_t>(col);
+}
+
+// kEven: rows of a multiple of 8 columns, so that a chunk is there or not, and nothing is asked about its parts.  (The tests for those
+// more than double the instructions of a row: 65536 x 768, bf16, backward 68 -> 55 us.)
+template <bool kEven, typename T>
+__device__ __forceinline__ Raw8<T> get(const T *p, int left) {
+    Raw8<T> r;
+    if constexpr (kEven) __builtin_memcpy(&r, p, sizeof r);
+    else r = load_raw(p, left);
+    return r;
+}
+template <bool kEven, typename T>
+__device__ __forceinline__ void put(T *p, const float (&f)[8], int left) {
+    store8(p, f, kEven ? kChunk : left);
+}
+template <bool kEven>
+__device__ __forceinline__ void put_packed(const Ckpt &c, int64_t row, uint32_t col, int left, const float (&f)[8], uint32_t cap) {
+    uint32_t code;
+    const u32x2 w = pack8(f, cap, code);
+    if (left > 0) store_q(c.q + row * c.ld_q + col, w, kEven ? kChunk : left);
+    if (left > 0 && col % kGroup == 0) (c.scale + row * c.ld_scale)[col / kGroup] = static_cast<uint8_t>(code);
 }
 
 // Sum over the lanes of a team, the same value in each of them.  kWaves > 1: `slot` is one of the team's LDS rows,
@@ -35,48 +59,57 @@ __device__ __forceinline__ float team_sum(float x, float *slot) {
     }
 }
 
-// The columns a thread holds: chunk n covers columns (n * kTeam + lane in team) * 8 onwards.
-template <int kLanes, int kWaves, int kChunks>
+// A workgroup's teams, kLanes lanes of a wavefront or kWaves wavefronts each.  Of a row chunk n of a thread covers columns
+// (n * kThreads + its number in the team) * 8 onwards.
+template <int kLanes, int kWaves>
 struct Team {
     static constexpr int kThreads = kLanes * kWaves;                    // of a team
-    static constexpr int kBlock = kWaves == 1 ? 256 : kThreads;
+    static constexpr int kBlock = kWaves == 1 ? 512 : kThreads;
     static constexpr int kTeams = kBlock / kThreads;                    // of a workgroup
+    // the first row of the thread's team: the same for a wavefront's lanes, and the compiler knows, unless it has four teams
+    static __device__ __forceinline__ int64_t first_row() {
+        const int team = threadIdx.x / kThreads;
+        return static_cast<int64_t>(blockIdx.x) * kTeams + (kLanes == 64 ? __builtin_amdgcn_readfirstlane(team) : team);
+    }
 };
 
 // Forward with rows of at most kThreads * 8 * kChunks columns.
-template <typename T, typename P, int kLanes, int kWaves, int kChunks>
-__global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_kernel(NormArgs a) {
-    using G = Team<kLanes, kWaves, kChunks>;
+template <typename T, typename P, int kLanes, int kWaves, int kChunks, bool kEven>
+__global__ __launch_bounds__((Team<kLanes, kWaves>::kBlock), 4) void norm_kernel(NormArgs a) {
+    using G = Team<kLanes, kWaves>;
     __shared__ float sums[2][kWaves];
     const int lane = threadIdx.x % G::kThreads;
     const int64_t teams = static_cast<int64_t>(gridDim.x) * G::kTeams;
-    int64_t row = static_cast<int64_t>(blockIdx.x) * G::kTeams + threadIdx.x / G::kThreads;
-    int col[kChunks], left[kChunks];
+    int64_t row = G::first_row();
+    if (row >= a.rows) return;
+    uint32_t col[kChunks];
+    int left[kChunks];
     float gamma[kChunks][8], beta[kChunks][8];
+    Raw8<T> x[kChunks], r[kChunks];
 #pragma unroll
     for (int n = 0; n < kChunks; ++n) {
         col[n] = (n * G::kThreads + lane) * kChunk;
-        left[n] = a.cols - col[n];
+        left[n] = a.cols - static_cast<int>(col[n]);
+        x[n] = r[n] = Raw8<T>{};           // (and so it stays where there is no such column)
 #pragma unroll
         for (int j = 0; j < 8; ++j) gamma[n][j] = beta[n][j] = 0.0f;
-        if (left[n] > 0) {
-            load8(static_cast<const P *>(a.gamma) + col[n], left[n], gamma[n]);
-            load8(static_cast<const P *>(a.beta) + col[n], left[n], beta[n]);
-        }
     }
     const float n_cols = static_cast<float>(a.cols);
-    Raw8<T> x[kChunks], r[kChunks];
-    auto request = [&](int64_t at_row) {
+    auto request = [&](int64_t at_row) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < kChunks; ++n) {
-            x[n] = r[n] = Raw8<T>{};
+        for (int n = 0; n < kChunks; ++n)
             if (left[n] > 0) {
-                x[n] = load_raw(at<const T>(a.x, at_row, col[n]), left[n]);
-                if (a.r.p) r[n] = load_raw(at<const T>(a.r, at_row, col[n]), left[n]);
+                x[n] = get<kEven>(at<const T>(a.x, at_row, col[n]), left[n]);
+                if (a.r.p) r[n] = get<kEven>(at<const T>(a.r, at_row, col[n]), left[n]);
             }
-        }
     };
-    if (row < a.rows) request(row);
+    request(row);
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n)
+        if (left[n] > 0) {
+            widen(get<kEven>(static_cast<const P *>(a.gamma) + col[n], left[n]), gamma[n]);
+            widen(get<kEven>(static_cast<const P *>(a.beta) + col[n], left[n]), beta[n]);
+        }
     for (; row < a.rows; row += teams) {
         float v[kChunks][8];
         float s = 0.0f;
@@ -96,7 +129,7 @@ __global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_
         if (a.t.p) {
 #pragma unroll
             for (int n = 0; n < kChunks; ++n)
-                if (left[n] > 0) store8(at<T>(a.t, row, col[n]), v[n], left[n]);
+                if (left[n] > 0) put<kEven>(at<T>(a.t, row, col[n]), v[n], left[n]);
         }
         // (divided, not multiplied by 1/cols: the mean of a constant row whose sum is exact is that constant.
         // The two rows of `sums` are written in turn, with a barrier between a row's reading and its next writing)
@@ -106,7 +139,7 @@ __global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_
         for (int n = 0; n < kChunks; ++n) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[n][j] = j < left[n] ? v[n][j] - mean : 0.0f;
+                v[n][j] = (kEven ? left[n] > 0 : j < left[n]) ? v[n][j] - mean : 0.0f;
                 s += v[n][j] * v[n][j];
             }
         }
@@ -121,19 +154,12 @@ __global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_
                 v[n][j] *= rstd;
                 y[j] = __builtin_fmaf(v[n][j], gamma[n][j], beta[n][j]);
             }
-            if (left[n] > 0) store8(at<T>(a.y, row, col[n]), y, left[n]);
+            if (left[n] > 0) put<kEven>(at<T>(a.y, row, col[n]), y, left[n]);
             if (a.c.q) {
-                if (left[n] < kChunk) {                                  // (0 * inf: a missing column would be NaN)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j >= left[n]) v[n][j] = 0.0f;
-                }
-                uint32_t code;
-                const u32x2 w = pack8(v[n], static_cast<uint32_t>(a.cap), code);
-                if (left[n] > 0) {
-                    store_q(a.c.q + row * a.c.ld_q + col[n], w, left[n]);
-                    if (col[n] % kGroup == 0) a.c.scale[row * a.c.ld_scale + col[n] / kGroup] = static_cast<uint8_t>(code);
-                }
+                for (int j = 0; j < 8; ++j)                             // (0 * inf: a missing column would be NaN)
+                    if (kEven ? left[n] <= 0 : j >= left[n]) v[n][j] = 0.0f;
+                put_packed<kEven>(a.c, row, col[n], left[n], v[n], static_cast<uint32_t>(a.cap));
             }
         }
     }
@@ -209,86 +235,89 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     }
 }
 
-// Backward with rows of at most kThreads * 8 * kChunks columns; a.part: [workgroup][2][cols] or null.
-template <typename T, typename P, int kLanes, int kWaves, int kChunks>
-__global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_backward_kernel(NormArgs a) {
-    using G = Team<kLanes, kWaves, kChunks>;
-    constexpr int kSpan = G::kThreads * kChunk * kChunks;               // columns of a team
-    __shared__ float sums[2][2][kWaves];                                 // [row's parity][sum]
+// Backward with rows of at most kThreads * 8 * kChunks columns; a.part: [workgroup][2][cols] or null.  A workgroup of 512 threads (or
+// 1024 where a row takes them) is one or more teams that go on together.
+template <int kLanes, int kWaves>
+struct BackTeam {
+    static constexpr int kThreads = kLanes * kWaves, kBlock = kWaves > 8 ? kThreads : 512, kTeams = kBlock / kThreads;
+};
+
+template <typename T, typename P, int kLanes, int kWaves, int kChunks, bool kEven>
+__global__ __launch_bounds__((BackTeam<kLanes, kWaves>::kBlock), 4) void norm_backward_kernel(NormArgs a) {
+    using G = BackTeam<kLanes, kWaves>;
+    static_assert(kChunks == 1 || G::kTeams == 1, "");
+    constexpr int kSpan = G::kThreads * kChunk;                          // columns of a team (one chunk)
+    __shared__ float sums[2][G::kTeams][2][kWaves];                      // [row's parity][team][sum]
     __shared__ float merge[G::kTeams > 1 ? G::kTeams * kSpan : 1];
-    const int lane = threadIdx.x % G::kThreads, team = threadIdx.x / G::kThreads;
-    const int64_t teams = static_cast<int64_t>(gridDim.x) * G::kTeams;
-    int64_t row = static_cast<int64_t>(blockIdx.x) * G::kTeams + team;
-    int col[kChunks], left[kChunks];
-    float gamma[kChunks][8], dgamma[kChunks][8], dbeta[kChunks][8];
+    const int team = kLanes == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G::kThreads) : threadIdx.x / G::kThreads;
+    const int lane = threadIdx.x % G::kThreads, wave = threadIdx.x / 64 % kWaves;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * G::kTeams;
+    uint32_t col[kChunks];
+    int left[kChunks];
+    float gamma[kChunks][8] = {}, dgamma[kChunks][8] = {}, dbeta[kChunks][8] = {};
 #pragma unroll
     for (int n = 0; n < kChunks; ++n) {
         col[n] = (n * G::kThreads + lane) * kChunk;
-        left[n] = a.cols - col[n];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) gamma[n][j] = dgamma[n][j] = dbeta[n][j] = 0.0f;
-        if (left[n] > 0) load8(static_cast<const P *>(a.gamma) + col[n], left[n], gamma[n]);
+        left[n] = a.cols - static_cast<int>(col[n]);
     }
     const float inv = 1.0f / static_cast<float>(a.cols);
-    // A row as it lies in memory: 28 bytes a chunk (bf16) where its numbers would take 64.  It is widened twice, before and
-    // after the sums; `hide` keeps the compiler from holding on to the first result (1024 threads have 128 registers each).
+    // A row as it lies in memory: 28 bytes a chunk (bf16) where its numbers would take 64.  What is not there stays zero.
     struct Row {
         Raw8<T> x[kChunks], r[kChunks];
         u32x2 q[kChunks];
         uint32_t code[kChunks];
         float rstd;
     };
-    auto request = [&](Row &w, int64_t at_row) {
+    auto request = [&](Row &w, int64_t row) __attribute__((always_inline)) {
+        if (row < a.rows) {
 #pragma unroll
-        for (int n = 0; n < kChunks; ++n) {
-            w.x[n] = w.r[n] = Raw8<T>{};
-            w.q[n] = u32x2{0, 0};
-            w.code[n] = 0;
-            if (left[n] > 0) {
-                w.x[n] = load_raw(at<const T>(a.x, at_row, col[n]), left[n]);
-                w.q[n] = load_q(a.c.q + at_row * a.c.ld_q + col[n], left[n]);
-                w.code[n] = a.c.scale[at_row * a.c.ld_scale + col[n] / kGroup];
-                if (a.r.p) w.r[n] = load_raw(at<const T>(a.r, at_row, col[n]), left[n]);
-            }
-        }
-        w.rstd = a.rstd[at_row];
-    };
-    // (h = dy*gamma; a NaN group's missing columns belong to no sum)
-    auto numbers = [&](const Row &w, int n, float (&dy)[8], float (&h)[8], float (&xh)[8]) {
-        widen(w.x[n], dy);
-        unpack8(w.q[n], scale_of(w.code[n]), xh);
-        if (left[n] < kChunk) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j >= left[n]) xh[j] = 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[j] = dy[j] * gamma[n][j];
-    };
-    auto hide = [](Row &w) {
-#pragma unroll
-        for (int n = 0; n < kChunks; ++n) {
-            asm volatile("" : "+v"(w.x[n].v), "+v"(w.q[n]), "+v"(w.code[n]));
-            if constexpr (sizeof(T) == 4) asm volatile("" : "+v"(w.x[n].w));
+            for (int n = 0; n < kChunks; ++n)
+                if (left[n] > 0) {
+                    w.x[n] = get<kEven>(at<const T>(a.x, row, col[n]), left[n]);
+                    w.q[n] = load_q(a.c.q + row * a.c.ld_q + col[n], kEven ? kChunk : left[n]);
+                    w.code[n] = (a.c.scale + row * a.c.ld_scale)[col[n] / kGroup];
+                    if (a.r.p) w.r[n] = get<kEven>(at<const T>(a.r, row, col[n]), left[n]);
+                }
+            w.rstd = a.rstd[row];
         }
     };
-    Row now{};
-    if (row < a.rows) request(now, row);
+    // (two chunks leave no registers for the next row)
+    constexpr bool kAhead = kChunks == 1;
+    Row now{}, next{};
+    int64_t first = static_cast<int64_t>(blockIdx.x) * G::kTeams;
+    if constexpr (kAhead) request(now, first + team);
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n)
+        if (left[n] > 0) widen(get<kEven>(static_cast<const P *>(a.gamma) + col[n], left[n]), gamma[n]);
     int parity = 0;
-    for (; row < a.rows; row += teams) {
-        Row next{};
-        if (row + teams < a.rows) request(next, row + teams);
-        float s1 = 0.0f, s2 = 0.0f;
+    for (; first < a.rows; first += stride) {
+        const int64_t row = first + team;
+        if constexpr (kAhead) request(next, row + stride);
+        else request(now, row);
+        float s1 = 0.0f, s2 = 0.0f, dy[kChunks][8], xh[kChunks][8];
 #pragma unroll
         for (int n = 0; n < kChunks; ++n) {
-            float dy[8], h[8], xh[8];
-            numbers(now, n, dy, h, xh);
+            widen(now.x[n], dy[n]);
+            unpack8(now.q[n], scale_of(now.code[n]), xh[n]);
+            if constexpr (!kEven) {
+                if (left[n] < kChunk) {                                  // (a NaN group's missing columns belong to no sum)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j >= left[n]) xh[n][j] = 0.0f;
+                }
+            }
+            if (row < a.rows) {                                          // (a team without a row holds an older one)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    dgamma[n][j] = __builtin_fmaf(dy[n][j], xh[n][j], dgamma[n][j]);
+                    dbeta[n][j] += dy[n][j];
+                }
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                dgamma[n][j] = __builtin_fmaf(dy[j], xh[j], dgamma[n][j]);
-                dbeta[n][j] += dy[j];
-                s1 += h[j];
-                s2 = __builtin_fmaf(h[j], xh[j], s2);
+                dy[n][j] *= gamma[n][j];
+                s1 += dy[n][j];
+                s2 = __builtin_fmaf(dy[n][j], xh[n][j], s2);
             }
         }
         // (one barrier a row: a row's two sums are read before the next row's barrier, and written again behind that)
@@ -300,50 +329,53 @@ __global__ __launch_bounds__((Team<kLanes, kWaves, kChunks>::kBlock)) void norm_
             s1 = sum64(s1);
             s2 = sum64(s2);
             if ((threadIdx.x & 63) == 0) {
-                sums[parity][0][threadIdx.x >> 6] = s1;
-                sums[parity][1][threadIdx.x >> 6] = s2;
+                sums[parity][team][0][wave] = s1;
+                sums[parity][team][1][wave] = s2;
             }
             __syncthreads();
             c1 = c2 = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                c1 += sums[parity][0][w];
-                c2 += sums[parity][1][w];
+                c1 += sums[parity][team][0][w];
+                c2 += sums[parity][team][1][w];
             }
             c1 *= inv;
             c2 *= inv;
             parity ^= 1;
         }
-        hide(now);
+        if (row < a.rows) {
 #pragma unroll
-        for (int n = 0; n < kChunks; ++n) {
-            float dy[8], h[8], xh[8], d[8];
-            numbers(now, n, dy, h, xh);
-            if (a.r.p) widen(now.r[n], d);
+            for (int n = 0; n < kChunks; ++n) {
+                if (left[n] <= 0) continue;
+                float d[8];
+                if (a.r.p) {
+                    widen(now.r[n], d);
+                } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float e = now.rstd * (h[j] - c1 - xh[j] * c2);
-                d[j] = a.r.p ? d[j] + e : e;
+                    for (int j = 0; j < 8; ++j) d[j] = 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] = __builtin_fmaf(now.rstd, dy[n][j] - c1 - xh[n][j] * c2, d[j]);
+                put<kEven>(at<T>(a.y, row, col[n]), d, left[n]);
             }
-            if (left[n] > 0) store8(at<T>(a.y, row, col[n]), d, left[n]);
         }
-        now = next;
+        if constexpr (kAhead) now = next;
     }
     if (!a.part) return;
     float *part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
+    if constexpr (G::kTeams == 1) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        float(*own)[8] = half ? dbeta : dgamma;
-        if constexpr (G::kTeams == 1) {
+        for (int n = 0; n < kChunks; ++n)
+            if (left[n] > 0) {
+                store8(part + col[n], dgamma[n], left[n]);
+                store8(part + a.cols + col[n], dbeta[n], left[n]);
+            }
+    } else {
 #pragma unroll
-            for (int n = 0; n < kChunks; ++n)
-                if (left[n] > 0) store8(part + half * static_cast<int64_t>(a.cols) + col[n], own[n], left[n]);
-        } else {
+        for (int half = 0; half < 2; ++half) {
             if (half) __syncthreads();
 #pragma unroll
-            for (int n = 0; n < kChunks; ++n)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) merge[team * kSpan + col[n] + j] = own[n][j];
+            for (int j = 0; j < 8; ++j) merge[team * kSpan + col[0] + j] = half ? dbeta[0][j] : dgamma[0][j];
             __syncthreads();
             for (int c = threadIdx.x; c < kSpan && c < a.cols; c += G::kBlock) {
                 float s = 0.0f;
@@ -450,13 +482,18 @@ __global__ __launch_bounds__(1024) void norm_gradients_kernel(const float *part,
     }
 }
 
+// f(element, parameter, even)
 template <typename F>
-void by_types(int type, int param_type, F f) {
-    if (type == TENSILE_F32) f(float{}, float{});
-    else if (type == TENSILE_BF16 && param_type == TENSILE_F32) f(bf16_t{}, float{});
-    else if (type == TENSILE_BF16) f(bf16_t{}, bf16_t{});
-    else if (param_type == TENSILE_F32) f(f16_t{}, float{});
-    else f(f16_t{}, f16_t{});
+void by_types(int type, int param_type, bool even, F f) {
+    auto with = [&](auto t, auto p) {
+        if (even) f(t, p, std::true_type{});
+        else f(t, p, std::false_type{});
+    };
+    if (type == TENSILE_F32) with(float{}, float{});
+    else if (type == TENSILE_BF16 && param_type == TENSILE_F32) with(bf16_t{}, float{});
+    else if (type == TENSILE_BF16) with(bf16_t{}, bf16_t{});
+    else if (param_type == TENSILE_F32) with(f16_t{}, float{});
+    else with(f16_t{}, f16_t{});
 }
 
 uint32_t grid_of(int64_t rows, int64_t teams, int64_t most) {
@@ -468,18 +505,19 @@ uint32_t grid_of(int64_t rows, int64_t teams, int64_t most) {
 
 int launch_norm(const ::tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type) {
     const int64_t cus = ops->num_cus;
-    by_types(type, param_type, [&](auto t, auto p) {
+    by_types(type, param_type, a.cols % kChunk == 0, [&](auto t, auto p, auto even) {
         using T = decltype(t);
         using P = decltype(p);
+        constexpr bool kEven = decltype(even)::value;
 #define TS_NORM(lanes, waves, chunks, per_cu)                                                                              \
     do {                                                                                                                   \
-        using G = Team<lanes, waves, chunks>;                                                                              \
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_kernel<T, P, lanes, waves, chunks>), dim3(grid_of(a.rows, G::kTeams, cus * per_cu)), \
+        using G = Team<lanes, waves>;                                                                              \
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_kernel<T, P, lanes, waves, chunks, kEven>), dim3(grid_of(a.rows, G::kTeams, cus * per_cu)), \
                            dim3(G::kBlock), 0, s, a);                                                                      \
     } while (0)
-        if (a.cols <= 128) TS_NORM(16, 1, 1, 8);
-        else if (a.cols <= 512) TS_NORM(64, 1, 1, 8);
-        else if (a.cols <= 1024) TS_NORM(64, 1, 2, 4);
+        if (a.cols <= 128) TS_NORM(16, 1, 1, 4);
+        else if (a.cols <= 512) TS_NORM(64, 1, 1, 4);
+        else if (a.cols <= 1024) TS_NORM(64, 1, 2, 2);
         else if (a.cols <= 2048) TS_NORM(64, 4, 1, 8);
         else if (a.cols <= 4096) TS_NORM(64, 4, 2, 4);
         else if (a.cols <= 8192) TS_NORM(64, 8, 2, 2);
@@ -494,18 +532,12 @@ int launch_norm(const ::tensile_ops *ops, hipStream_t s, const NormArgs &a, int 
 int launch_norm_backward(const ::tensile_ops *ops, hipStream_t s, const NormArgs &args, int type, int param_type, void *dgamma, void *dbeta) {
     const int64_t cus = ops->num_cus;
     NormArgs a = args;
-    // workgroups: what is resident, but partial sums (8 bytes a column each) stay small against the rows
-    struct Shape { int lanes, waves, chunks, teams, per_cu; };
-    const Shape sh = a.cols <= 128    ? Shape{16, 1, 1, 16, 4}
-                     : a.cols <= 512  ? Shape{64, 1, 1, 4, 4}
-                     : a.cols <= 1024 ? Shape{64, 1, 2, 4, 4}
-                     : a.cols <= 2048 ? Shape{64, 4, 1, 1, 4}
-                     : a.cols <= 4096 ? Shape{64, 4, 2, 1, 3}
-                     : a.cols <= 8192 ? Shape{64, 16, 1, 1, 1}
-                                       : Shape{0, 0, 0, 1, 1};
-    const bool is_long = sh.lanes == 0;
+    // workgroups: what is resident, two of 512 threads to a CU (partial sums take 8 bytes a column each)
+    // (1024 threads have room for two chunks each of 16-bit gradients)
+    const bool is_long = a.cols > (type == TENSILE_F32 ? 8192 : 16384);
+    const int teams = a.cols <= 128 ? 32 : a.cols <= 512 ? 8 : a.cols <= 1024 ? 4 : a.cols <= 2048 ? 2 : 1, per_cu = a.cols <= 4096 ? 2 : 1;
     const int64_t n_columns = (static_cast<int64_t>(a.cols) + 2047) / 2048;      // (long rows)
-    uint32_t n_part = grid_of(a.rows, sh.teams, is_long ? (8 * cus + n_columns - 1) / n_columns : cus * sh.per_cu);
+    const uint32_t n_part = grid_of(a.rows, is_long ? 1 : teams, is_long ? (8 * cus + n_columns - 1) / n_columns : cus * per_cu);
     std::unique_lock<std::mutex> lock;
     if (dgamma) {
         OpsScratch &scratch = ops_scratch(ops, s);
@@ -514,19 +546,23 @@ int launch_norm_backward(const ::tensile_ops *ops, hipStream_t s, const NormArgs
         if (rc != TENSILE_OK) return rc;
         a.part = scratch.buf.p;
     }
-    by_types(type, param_type, [&](auto t, auto p) {
+    by_types(type, param_type, a.cols % kChunk == 0, [&](auto t, auto p, auto even) {
         using T = decltype(t);
         using P = decltype(p);
+        constexpr bool kEven = decltype(even)::value;
         if (a.rows > 0) {
 #define TS_NORM(lanes, waves, chunks)                                                                                      \
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_backward_kernel<T, P, lanes, waves, chunks>), dim3(n_part),                    \
-                       dim3(Team<lanes, waves, chunks>::kBlock), 0, s, a)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_backward_kernel<T, P, lanes, waves, chunks, kEven>), dim3(n_part),             \
+                       dim3(BackTeam<lanes, waves>::kBlock), 0, s, a)
             if (a.cols <= 128) TS_NORM(16, 1, 1);
             else if (a.cols <= 512) TS_NORM(64, 1, 1);
-            else if (a.cols <= 1024) TS_NORM(64, 1, 2);
+            else if (a.cols <= 1024) TS_NORM(64, 2, 1);
             else if (a.cols <= 2048) TS_NORM(64, 4, 1);
-            else if (a.cols <= 4096) TS_NORM(64, 4, 2);
+            else if (a.cols <= 4096) TS_NORM(64, 8, 1);
             else if (a.cols <= 8192) TS_NORM(64, 16, 1);
+            else if (!is_long) {
+                if constexpr (sizeof(T) == 2) TS_NORM(64, 16, 2);
+            }
             else {
                 if (dgamma)
                     hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_columns_kernel<T>), dim3(static_cast<uint32_t>(n_columns), n_part), dim3(256), 0, s, a);

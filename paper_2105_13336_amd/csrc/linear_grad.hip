@@ -20,6 +20,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // (the LDS-direct loads below take their target from m0, which the compiler counts as its own and says so)
@@ -86,8 +87,8 @@ __device__ __forceinline__ void drop_front(Raw8<float> &r, int n, bool keep) {
 }
 
 // A workgroup's tile: kWN x kWK wavefronts of 32 kNB columns of dy x 32 kKB columns of the checkpoint each, two wavefronts to a
-// SIMD in all; 32 rows to a step.  kByHalves: the columns of the checkpoint lie in the tile in the order that the wide kernel's
-// staging gives them.
+// SIMD in all; 32 rows to a step.  kByHalves: the columns of the checkpoint lie in the tile in the order that the streaming
+// kernel's staging gives them.
 template <int kNB_, int kKB_, int kWN_, int kWK_, bool kByHalves_ = false>
 struct Tile {
     static constexpr int kNB = kNB_, kKB = kKB_, kWN = kWN_, kWK = kWK_;
@@ -103,8 +104,9 @@ struct Tile {
         return kByHalves ? p / 128 * 128 + (p >> 3) % 8 * 16 + (p >> 6) % 2 * 8 + p % 8 : p;
     }
 };
-using Narrow = Tile<2, 2, 2, 2>;             // 128 x 128, two workgroups to a CU
-using Wide = Tile<4, 2, 2, 4, true>;         // 256 x 256, one
+using Staged = Tile<2, 2, 2, 2>;             // 128 x 128, two workgroups to a CU
+using Narrow = Tile<2, 2, 2, 2, true>;       // the same for the kernel of 16-bit brain floats
+using Wide = Tile<4, 2, 2, 4, true>;         // 256 x 256, one workgroup to a CU
 constexpr int kRows = 32;
 
 // Where a workgroup works.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets a run of consecutive
@@ -176,21 +178,49 @@ __device__ __forceinline__ void finish(const GradArgs &g, const Place &w, const 
         return;
     }
     if (w.k0 == 0 && a.dbias && tid < G::kN && w.n0 + tid < a.N) put_as<T>(a.dw_type, a.dbias, w.n0 + tid, sums[tid]);
+    float gamma[kKB], beta[kKB];
 #pragma unroll
     for (int j = 0; j < kKB; ++j) {
         const int k = w.k0 + G::column(wave, lane, j);
-        if (k >= a.K) continue;
-        const float ga = a.gamma ? get_as<T>(a.param_type, a.gamma, k) : 1.0f, be = a.gamma ? get_as<T>(a.param_type, a.beta, k) : 0.0f;
+        gamma[j] = a.gamma && k < a.K ? get_as<T>(a.param_type, a.gamma, k) : 1.0f;
+        beta[j] = a.gamma && k < a.K ? get_as<T>(a.param_type, a.beta, k) : 0.0f;
+    }
+    // (What is asked for every element costs as much as the store: whether it exists, which type it has.)
+    auto write = [&](auto whole, auto wide) __attribute__((always_inline)) {
+        using Out = typename std::conditional<decltype(wide)::value, float, T>::type;
 #pragma unroll
-        for (int i = 0; i < kNB; ++i)
+        for (int i = 0; i < kNB; ++i) {
+            // (the sums of the lane's sixteen rows first, four at a time: an LDS read before every store costs 12 us a tile)
+            float own[16] = {};
+            if (a.gamma) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = G::row(wave, lane, i, r), n = w.n0 + row;
-                if (n >= a.N) continue;
-                float v = acc[i][j][r];
-                if (a.gamma) v = __builtin_fmaf(v, ga, be * sums[row]);
-                put_as<T>(a.dw_type, a.dw.p, static_cast<int64_t>(n) * a.dw.ld + k, v);
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 s = *reinterpret_cast<const f32x4 *>(sums + G::row(wave, lane, i, r));
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) own[r + u] = s[u];
+                }
             }
+#pragma unroll
+            for (int j = 0; j < kKB; ++j) {
+                const int k = w.k0 + G::column(wave, lane, j);
+                if (!decltype(whole)::value && k >= a.K) continue;
+                Out *const to = static_cast<Out *>(a.dw.p) + k;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int n = w.n0 + G::row(wave, lane, i, r);
+                    if (!decltype(whole)::value && n >= a.N) continue;
+                    from_f32(__builtin_fmaf(acc[i][j][r], gamma[j], beta[j] * own[r]), to[static_cast<int64_t>(n) * a.dw.ld]);
+                }
+            }
+        }
+    };
+    const bool whole = w.n0 + G::kN <= a.N && w.k0 + G::kK <= a.K;
+    if (a.dw_type == TENSILE_F32) {
+        if (whole) write(std::true_type{}, std::true_type{});
+        else write(std::false_type{}, std::true_type{});
+    } else {
+        if (whole) write(std::true_type{}, std::false_type{});
+        else write(std::false_type{}, std::false_type{});
     }
 }
 
@@ -457,41 +487,44 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_kernel(GradArgs g)
     finish<T, G>(g, w, acc, bias, use_bias, reinterpret_cast<float *>(lds));
 }
 
-// The same for a bf16 gradient and large dw: a tile of 256 x 256, and what is on its way from memory lies in the LDS, not in
-// registers: dy three steps ahead and the checkpoint four, some 90 KB to a CU.  With registers to hold it one step was all
-// there was room for, and the loads were what bounded the kernel (16384 x 8192 x 8192: 2230 us, 1480 without them, 1780 so).  The LDS
-// has 136 KB of a CU's 160: one workgroup, two wavefronts to a SIMD, which hide about four ordinary instructions behind
-// each matrix instruction; there are 2.9, and 3.8 where dy is summed.  What is left: the chip lowers its clock to 1.9 to 2.0 GHz.
-constexpr int kWide = Wide::kN, kWideThreads = Wide::kThreads;
-
-__global__ __launch_bounds__(kWideThreads, 2) void linear_grad_wide_kernel(GradArgs g) {
-    constexpr int kNB = Wide::kNB, kKB = Wide::kKB, kRow = 2 * kWide;
-    constexpr int kSlot = kRows * kRow, kRaw = kRows * kWide;            // bytes of a step's rows: staged, and as they are held
-    constexpr int kCodes = 4 * kWideThreads;                             // ... a code takes four bytes
-    constexpr int kDy = 0, kX = 4 * kSlot, kQ = 6 * kSlot, kC = kQ + 4 * kRaw;   // four steps of dy, two of X, four of the checkpoint
+// The same for a bf16 gradient.  What is on its way from memory lies in the LDS, not in registers: dy three steps ahead and the
+// checkpoint four, some 90 KB to a CU.  With registers to hold it one step was all there was room for, and the loads were what
+// bounded the kernel (16384 x 8192 x 8192, 256 x 256 tiles: 2230 us, 1480 without them, 1780 so).  Of the LDS's 160 KB a CU's
+// workgroups have 136: two wavefronts to a SIMD, which hide about four ordinary instructions behind each matrix instruction; of the
+// large tile there are 2.9, and 3.8 where dy is summed.  What is left: the chip lowers its clock to 1.9 to 2.0 GHz.
+template <typename G>
+__global__ __launch_bounds__(G::kThreads, 2) void linear_grad_stream_kernel(GradArgs g) {
+    constexpr int kNB = G::kNB, kKB = G::kKB, kRowN = 2 * G::kN, kRowK = 2 * G::kK;
+    constexpr int kSlotN = kRows * kRowN, kSlotK = kRows * kRowK, kRaw = kRows * G::kK;   // a step's rows: staged, and as they are held
+    constexpr int kCodes = 4 * G::kThreads;                              // ... a code takes four bytes
+    constexpr int kDy = 0, kX = 4 * kSlotN, kQ = kX + 2 * kSlotK, kC = kQ + 4 * kRaw;   // four steps of dy, two of X, four of the checkpoint
+    constexpr int kOwn = kRows * 64 / G::kThreads;                       // rows that a wave brings, 64 times 16 bytes at a time:
+    constexpr int kDyRows = 64 * 8 / G::kN, kXRows = 64 * 16 / G::kK;    // 8 columns of dy to a lane, 16 of the checkpoint
+    static_assert(kOwn == 2 * kDyRows && kOwn == kXRows && G::kByHalves, "");
     __shared__ __attribute__((aligned(1024))) char lds[kC + 4 * kCodes];
     typedef __attribute__((address_space(3))) char lds_char;
     const LinearArgs &a = g.a;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wave_n = wave >> 2, wave_k = wave & 3;
-    const Place w = place<Wide>(g);
+    const int wave_n = wave / G::kWK, wave_k = wave % G::kWK;
+    const Place w = place<G>(g);
     const int n0 = w.n0, k0 = w.k0;
     const int64_t m_begin = w.m_begin, m_end = w.m_end;
 
-    // dy: a wave brings four rows a step, two at a time, 32 lanes of 8 columns to a row.  The LDS takes 16 bytes of each lane in
-    // the order of the lanes, so the staged rows' order of blocks (swizzle) is that of the addresses.
+    // The LDS takes 16 bytes of each lane in the order of the lanes, so the staged rows' order of blocks (swizzle) is that of
+    // the addresses.
     uint32_t dy_off[2];
     int dy_over[2];                   // columns of the lane's eight that do not exist (only the last rows' loads care)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int row = 4 * wave + 2 * j + (lane >> 5), block = ((lane & 31) >> 1) ^ (2 * (row & 3));
+        constexpr int kLanes = 64 / kDyRows;
+        const int row = kOwn * wave + kDyRows * j + lane / kLanes, block = (lane % kLanes >> 1) ^ (2 * (row & 3));
         const int col = n0 + block * 16 + (lane & 1) * 8;
         dy_off[j] = static_cast<uint32_t>((row * a.dy.ld + (col < a.N ? col : 0)) * 2);    // (no such column: any will do)
         dy_over[j] = col < a.N && col + 8 > a.N ? col + 8 - a.N : 0;
     }
-    // the checkpoint: a wave brings four rows, 16 lanes of 16 columns to a row; a thread dequantises what it has brought
-    const int x_row = 4 * wave + (lane >> 4), x_col = (lane & 15) * 16;
+    // (a thread dequantises what it has brought)
+    const int x_row = kOwn * wave + lane / (64 / kXRows), x_col = lane % (64 / kXRows) * 16;
     const int x_from = k0 + x_col < a.K ? k0 + x_col : 0;
     const uint32_t x_off = static_cast<uint32_t>(x_row * a.c.ld_q + x_from);
     const uint32_t s_off = static_cast<uint32_t>(x_row * a.c.ld_scale + x_from / kGroup);
@@ -499,8 +532,8 @@ __global__ __launch_bounds__(kWideThreads, 2) void linear_grad_wide_kernel(GradA
     int x_at[2];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-        const int chunk = (lane & 7) + 8 * half + 16 * ((lane >> 3) & 1);
-        x_at[half] = kX + swizzle<kRow>(x_row, chunk >> 1) + (chunk & 1) * 16;
+        const int chunk = (lane & 7) + 8 * half + 16 * (x_col / 128);
+        x_at[half] = kX + swizzle<kRowK>(x_row, chunk >> 1) + (chunk & 1) * 16;
     }
 
     // From memory to the LDS without a register in between.  (By hand: of the builtin the compiler waits for every one under way
@@ -512,7 +545,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void linear_grad_wide_kernel(GradA
     auto bring_dy = [&](int64_t m, int slot) __attribute__((always_inline)) {
         const global_bytes from = (global_bytes)(static_cast<const char *>(a.dy.p) + m * a.dy.ld * 2);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) bring(lds_at + kDy + slot * kSlot + (4 * wave + 2 * j) * kRow, from, dy_off[j]);
+        for (int j = 0; j < 2; ++j) bring(lds_at + kDy + slot * kSlotN + (kOwn * wave + kDyRows * j) * kRowN, from, dy_off[j]);
     };
     auto bring_x = [&](int64_t m, int slot) __attribute__((always_inline)) {
         bring(lds_at + kQ + slot * kRaw + wave * 1024, (global_bytes)(a.c.q + m * a.c.ld_q), x_off);
@@ -539,7 +572,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void linear_grad_wide_kernel(GradA
     };
     auto put = [&](const Sixteen &w, int slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) *reinterpret_cast<u32x4 *>(lds + x_at[half] + slot * kSlot) = w.v[half];
+        for (int half = 0; half < 2; ++half) *reinterpret_cast<u32x4 *>(lds + x_at[half] + slot * kSlotK) = w.v[half];
     };
 
     f32x16 acc[kNB][kKB] = {};
@@ -553,22 +586,22 @@ __global__ __launch_bounds__(kWideThreads, 2) void linear_grad_wide_kernel(GradA
     for (int e = 0; e < 2; ++e) {
         const int row = t_row + 16 * (e ^ turn);
 #pragma unroll
-        for (int b = 0; b < kNB; ++b) a_at[e][b] = kDy + swizzle<kRow>(row, (wave_n * kNB + b) * 2 + (group & 1)) + t_in;
+        for (int b = 0; b < kNB; ++b) a_at[e][b] = kDy + swizzle<kRowN>(row, (wave_n * kNB + b) * 2 + (group & 1)) + t_in;
 #pragma unroll
-        for (int b = 0; b < kKB; ++b) b_at[e][b] = kX + swizzle<kRow>(row, (wave_k * kKB + b) * 2 + (group & 1)) + t_in;
+        for (int b = 0; b < kKB; ++b) b_at[e][b] = kX + swizzle<kRowK>(row, (wave_k * kKB + b) * 2 + (group & 1)) + t_in;
     }
-    auto fragment = [&](int p) __attribute__((always_inline)) {
+    auto fragment = [&](int p, int four_rows) __attribute__((always_inline)) {
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lds + p));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lds + p + 4 * kRow));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lds + p + four_rows));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     bf16x8 fa[2][kNB], fb[2][kKB];
     auto read = [&](int e, int dy_slot, int x_slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int b = 0; b < kNB; ++b) fa[e][b] = fragment(a_at[e][b] + dy_slot * kSlot);
+        for (int b = 0; b < kNB; ++b) fa[e][b] = fragment(a_at[e][b] + dy_slot * kSlotN, 4 * kRowN);
 #pragma unroll
-        for (int b = 0; b < kKB; ++b) fb[e][b] = fragment(b_at[e][b] + x_slot * kSlot);
+        for (int b = 0; b < kKB; ++b) fb[e][b] = fragment(b_at[e][b] + x_slot * kSlotK, 4 * kRowK);
     };
     auto multiply = [&](int e, auto sums) __attribute__((always_inline)) {
 #pragma unroll
@@ -666,11 +699,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void linear_grad_wide_kernel(GradA
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int row = 4 * wave + 2 * j + (lane >> 5);
+                const int row = kOwn * wave + kDyRows * j;
                 u32x4 v = {0, 0, 0, 0};
-                if (m + row < m_end)
+                if (m + row + lane / (64 / kDyRows) < m_end)
                     v = shift_out(*(global_16)((global_bytes)(static_cast<const char *>(a.dy.p) + m * a.dy.ld * 2) + dy_off[j] - 2 * dy_over[j]), 2 * dy_over[j]);
-                *reinterpret_cast<u32x4 *>(lds + kDy + (4 * wave + 2 * j) * kRow + lane * 16) = v;
+                *reinterpret_cast<u32x4 *>(lds + kDy + row * kRowN + lane * 16) = v;
             }
             u32x4 v = {0, 0, 0, 0};
             uint32_t c = 0;
@@ -690,42 +723,62 @@ __global__ __launch_bounds__(kWideThreads, 2) void linear_grad_wide_kernel(GradA
     if (use_bias) all(std::true_type{});
     else all(std::false_type{});
     __syncthreads();
-    finish<bf16_t, Wide>(g, w, acc, bias, use_bias, reinterpret_cast<float *>(lds));
+    finish<bf16_t, G>(g, w, acc, bias, use_bias, reinterpret_cast<float *>(lds));
 }
 
-// split > 1: the partial sums added up in order, with the norm's parameters, rounded once.  A thread takes four lanes' registers of
-// the same number: four columns of a row.
-template <typename T, typename G>
+// split > 1: the partial sums added up in a fixed order, with the norm's parameters, rounded once.  Four lanes' registers of
+// the same number are four columns of a row; kStrands threads take every kStrands-th part of such a four and of the row's sum of dy.
+template <typename T, typename G, int kStrands>
 __global__ __launch_bounds__(256) void linear_join_kernel(GradArgs g) {
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
-    constexpr int kElements = G::kN * G::kK, kQuads = kElements / 4;
+    constexpr int kElements = G::kN * G::kK, kQuads = kElements / 4, kOwn = 256 / kStrands;   // fours of a workgroup
+    __shared__ f32x4 strand_v[kStrands > 1 ? 256 : 1];
+    __shared__ float strand_b[kStrands > 1 ? 256 : 1];
     const LinearArgs &a = g.a;
-    const int tile = blockIdx.x / (kQuads / 256), quad = blockIdx.x % (kQuads / 256) * 256 + threadIdx.x;
+    const int tid = threadIdx.x, strand = tid / kOwn;
+    const int tile = blockIdx.x / (kQuads / kOwn), quad = blockIdx.x % (kQuads / kOwn) * kOwn + tid % kOwn;
     const int lane = quad % 16 * 4, r = quad / 16 % 16, block = quad / 256 % (G::kNB * G::kKB), wave = quad / (256 * G::kNB * G::kKB);
     const int n = tile / g.tiles_k * G::kN + G::row(wave, lane, block / G::kKB, r);
     const int k = tile % g.tiles_k * G::kK + G::column(wave, lane, block % G::kKB);
-    if (n >= a.N || k >= a.K) return;
+    const bool there = n < a.N && k < a.K, want_sum = there && (a.gamma || (a.dbias && k == 0));
     const float *from = g.part + static_cast<int64_t>(tile) * g.split * kElements + quad * 4;
+    const float *sums = g.part + static_cast<int64_t>(g.tiles_n) * g.tiles_k * g.split * kElements + n;
     f32x4 v = {0, 0, 0, 0};
-    for (int s0 = 0; s0 < g.split; s0 += 8) {                            // (eight loads under way)
-        f32x4 part[8];
+    float b = 0.0f;
+    if (there) {
+        for (int s0 = strand; s0 < g.split; s0 += 8 * kStrands) {        // (eight loads under way)
+            f32x4 part[8];
+            float sum[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            part[u] = *reinterpret_cast<const f32x4 *>(from + static_cast<int64_t>(s0 + u < g.split ? s0 + u : g.split - 1) * kElements);
+            for (int u = 0; u < 8; ++u) {
+                const int64_t s = s0 + u * kStrands < g.split ? s0 + u * kStrands : s0;
+                part[u] = *reinterpret_cast<const f32x4 *>(from + s * kElements);
+                sum[u] = want_sum ? sums[s * a.N] : 0.0f;
+            }
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (s0 + u < g.split) v += part[u];
-    }
-    if (a.gamma || (a.dbias && k == 0)) {
-        const float *sums = g.part + static_cast<int64_t>(g.tiles_n) * g.tiles_k * g.split * kElements + n;
-        float b = 0.0f;
-        for (int s = 0; s < g.split; ++s) b += sums[static_cast<int64_t>(s) * a.N];
-        if (a.dbias && k == 0) put_as<T>(a.dw_type, a.dbias, n, b);
-        if (a.gamma) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (k + j < a.K) v[j] = __builtin_fmaf(v[j], get_as<T>(a.param_type, a.gamma, k + j), get_as<T>(a.param_type, a.beta, k + j) * b);
+            for (int u = 0; u < 8; ++u)
+                if (s0 + u * kStrands < g.split) {
+                    v += part[u];
+                    b += sum[u];
+                }
         }
+    }
+    if constexpr (kStrands > 1) {
+        strand_v[tid] = v;
+        strand_b[tid] = b;
+        __syncthreads();
+        if (strand > 0) return;
+#pragma unroll
+        for (int y = 1; y < kStrands; ++y) {
+            v += strand_v[y * kOwn + tid];
+            b += strand_b[y * kOwn + tid];
+        }
+    }
+    if (!there) return;
+    if (a.dbias && k == 0) put_as<T>(a.dw_type, a.dbias, n, b);
+    if (a.gamma) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (k + j < a.K) v[j] = __builtin_fmaf(v[j], get_as<T>(a.param_type, a.gamma, k + j), get_as<T>(a.param_type, a.beta, k + j) * b);
     }
     const int64_t at = static_cast<int64_t>(n) * a.dw.ld + k;
     if (a.dw_type == TENSILE_F32 && k + 4 <= a.K) {
@@ -763,11 +816,14 @@ int run(const ::tensile_ops *ops, hipStream_t s, const LinearArgs &a) {
         g.part = scratch.buf.p;
     }
     const dim3 grid(static_cast<uint32_t>(tiles * split));
-    if constexpr (G::kByHalves) hipLaunchKernelGGL(linear_grad_wide_kernel, grid, dim3(G::kThreads), 0, s, g);
+    if constexpr (G::kByHalves) hipLaunchKernelGGL(HIP_KERNEL_NAME(linear_grad_stream_kernel<G>), grid, dim3(G::kThreads), 0, s, g);
     else hipLaunchKernelGGL(HIP_KERNEL_NAME(linear_grad_kernel<T, G, kByElement>), grid, dim3(G::kThreads), 0, s, g);
     TS_HIP(hipGetLastError());
     if (split > 1) {
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(linear_join_kernel<T, G>), dim3(static_cast<uint32_t>(tiles * (G::kN * G::kK / 1024))), dim3(256), 0, s, g);
+        // (more than 8 parts: eight threads to a four)
+        const uint32_t blocks = static_cast<uint32_t>(tiles * (G::kN * G::kK / 1024));
+        if (split <= 8) hipLaunchKernelGGL(HIP_KERNEL_NAME(linear_join_kernel<T, G, 1>), dim3(blocks), dim3(256), 0, s, g);
+        else hipLaunchKernelGGL(HIP_KERNEL_NAME(linear_join_kernel<T, G, 8>), dim3(blocks * 8), dim3(256), 0, s, g);
         TS_HIP(hipGetLastError());
     }
     return TENSILE_OK;
@@ -777,13 +833,15 @@ template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const LinearArgs &a) {
     // A load takes 8 columns of dy, 16 of the checkpoint, and reaches them by 32 bits from the first of a step's 32 rows.
     const bool by_element = a.N < 8 || a.K < 16 || a.dy.ld * static_cast<int64_t>(sizeof(T)) >= (1 << 26) || a.c.ld_q >= (1 << 26);
-    if (by_element) return run<T, Narrow, true>(ops, s, a);
+    if (by_element) return run<T, Staged, true>(ops, s, a);
     if constexpr (std::is_same<T, bf16_t>::value) {
         const int64_t wide = static_cast<int64_t>((a.N + Wide::kN - 1) / Wide::kN) * ((a.K + Wide::kK - 1) / Wide::kK);
         const int64_t area = static_cast<int64_t>(a.N) * a.K, padded = wide * Wide::kN * Wide::kK;
         if (wide >= 32 && padded <= area + area / 2) return run<T, Wide, false>(ops, s, a);
+        return run<T, Narrow, false>(ops, s, a);
+    } else {
+        return run<T, Staged, false>(ops, s, a);
     }
-    return run<T, Narrow, false>(ops, s, a);
 }
 
 }  // namespace

@@ -403,18 +403,19 @@ def _mat(t: Optional[torch.Tensor], name: str):
     """[..., cols] with contiguous columns and evenly spaced rows, as a matrix."""
     if t is None:
         return None
-    code = _TYPES.get(t.dtype)
-    if code is None or not t.is_cuda or t.dim() < 1:
+    code, shape = _TYPES.get(t.dtype), t.shape
+    if code is None or not t.is_cuda or not shape:
         raise TensileError(TENSILE_E_INVAL, f"{name}: need a CUDA tensor of float32, bfloat16 or float16 with at least one dimension")
-    if t.dim() != 2:
-        if not t.is_contiguous():
-            raise TensileError(TENSILE_E_INVAL, f"{name}: a tensor of {t.dim()} dimensions has to be contiguous")
-        cols = t.shape[-1]
-        return _Matrix(t.data_ptr(), t.numel() // cols if cols else 0, cols, cols, code)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    if t.is_contiguous():                                              # (one question fewer than the strides: small calls are bound here)
+        cols = shape[-1]
+        return _Matrix(t.data_ptr(), shape[0] if len(shape) == 2 else t.numel() // cols if cols else 0, cols, cols, code)
+    if len(shape) != 2:
+        raise TensileError(TENSILE_E_INVAL, f"{name}: a tensor of {len(shape)} dimensions has to be contiguous")
+    rows, cols = shape
+    row, col = t.stride()
+    if cols > 1 and col != 1:
         raise TensileError(TENSILE_E_INVAL, f"{name}: the columns of a row have to be contiguous")
-    return _Matrix(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols, code)
+    return _Matrix(t.data_ptr(), rows, cols, row if rows > 1 else cols, code)
 
 
 def _vec(t: Optional[torch.Tensor], dtype, n: int, name: str):

@@ -95,9 +95,14 @@ struct Tile {
     static constexpr bool kByHalves = kByHalves_;
     static constexpr int kThreads = 64 * kWN * kWK, kN = 32 * kNB * kWN, kK = 32 * kKB * kWK;
     static constexpr int kPerCu = 512 / kThreads;
+    // The sums of dy are taken by the kWK wavefronts that share its columns: every second one takes the same 16 rows of a step
+    // (see the kernels), and of these each a part of the blocks, kSum, which are its first.
+    static constexpr int kSum = 2 * kNB / kWK;
+    static_assert(kNB % kSum == 0 && (kNB & (kNB - 1)) == 0, "");
+    static __device__ __forceinline__ int block(int wave, int i) { return i ^ (wave % kWK / 2 * kSum); }
     // row and column of the tile that a lane's register r of block (i, j) is
     static __device__ __forceinline__ int row(int wave, int lane, int i, int r) {
-        return (wave / kWK * kNB + i) * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
+        return (wave / kWK * kNB + block(wave, i)) * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
     }
     static __device__ __forceinline__ int column(int wave, int lane, int j) {
         const int p = (wave % kWK * kKB + j) * 32 + (lane & 31);
@@ -148,17 +153,17 @@ __device__ __forceinline__ float get_as(int type, const void *p, int64_t at) {
 // What a workgroup does with its tile's sums: dbias, and dw with the norm's parameters, or all as they are where the rows are split.
 // `sums` is LDS for two rows of the tile's width.
 template <typename T, typename G>
-__device__ __forceinline__ void finish(const GradArgs &g, const Place &w, const f32x16 (&acc)[G::kNB][G::kKB], const float (&bias)[G::kNB],
+__device__ __forceinline__ void finish(const GradArgs &g, const Place &w, const f32x16 (&acc)[G::kNB][G::kKB], const float (&bias)[G::kSum],
                                        bool use_bias, float *sums) {
     constexpr int kNB = G::kNB, kKB = G::kKB;
     const LinearArgs &a = g.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    // sums of dy: over the two halves of the wavefront, then over the two waves that took turns
+    // sums of dy: over the two halves of the wavefront, then over the two halves of the steps
     if (use_bias) {
 #pragma unroll
-        for (int i = 0; i < kNB; ++i) {
+        for (int i = 0; i < G::kSum; ++i) {
             const float s = bias[i] + __shfl_xor(bias[i], 32);
-            if (lane < 32 && wave % G::kWK < 2) sums[wave % G::kWK * G::kN + (wave / G::kWK * kNB + i) * 32 + lane] = s;
+            if (lane < 32) sums[wave % 2 * G::kN + (wave / G::kWK * kNB + G::block(wave, i)) * 32 + lane] = s;
         }
         __syncthreads();
         if (tid < G::kN) sums[tid] = sums[tid] + sums[G::kN + tid];
@@ -366,20 +371,20 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_kernel(GradArgs g)
     };
 
     f32x16 acc[kNB][kKB] = {};
-    float bias[kNB] = {};
+    float bias[G::kSum] = {};
     const bool use_bias = a.gamma || (k0 == 0 && a.dbias);
     // transposed reads: the lanes of a group of 16 read rows 8h .. 8h+3 (and +4) of 16 columns
     const int i16 = lane & 15, group = lane >> 4;
     const int t_row = (group >> 1) * 8 + i16 / 4, t_in = (i16 & 3) * 8;
     // Of a step's two blocks of 16 rows a wave takes first the one of its parity in the row of the tile: the sums of dy are
-    // taken of that one only, by two waves that share its columns, without a branch.
+    // taken of that one only, by the waves that share its columns, without a branch.
     const int turn = wave_k & 1;
     int a_at[2][kNB], b_at[2][kKB];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const int row = t_row + 16 * (e ^ turn);
 #pragma unroll
-        for (int b = 0; b < kNB; ++b) a_at[e][b] = swizzle<kRowN>(row, (wave_n * kNB + b) * 2 + (group & 1)) + t_in;
+        for (int b = 0; b < kNB; ++b) a_at[e][b] = swizzle<kRowN>(row, (wave_n * kNB + G::block(wave, b)) * 2 + (group & 1)) + t_in;
 #pragma unroll
         for (int b = 0; b < kKB; ++b) b_at[e][b] = kP * kPlane + swizzle<kRowK>(row, (wave_k * kKB + b) * 2 + (group & 1)) + t_in;
     }
@@ -412,7 +417,7 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_kernel(GradArgs g)
             if (e == 0) {
                 const bf16x2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
 #pragma unroll
-                for (int i = 0; i < kNB; ++i) {
+                for (int i = 0; i < G::kSum; ++i) {
                     float s = 0.0f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -491,7 +496,7 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_kernel(GradArgs g)
 // checkpoint four, some 90 KB to a CU.  With registers to hold it one step was all there was room for, and the loads were what
 // bounded the kernel (16384 x 8192 x 8192, 256 x 256 tiles: 2230 us, 1480 without them, 1780 so).  Of the LDS's 160 KB a CU's
 // workgroups have 136: two wavefronts to a SIMD, which hide about four ordinary instructions behind each matrix instruction; of the
-// large tile there are 2.9, and 3.8 where dy is summed.  What is left: the chip lowers its clock to 1.9 to 2.0 GHz.
+// large tile there are 2.9, and 3.3 where dy is summed.  What is left: the chip lowers its clock to 1.9 to 2.0 GHz.
 template <typename G>
 __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_stream_kernel(GradArgs g) {
     constexpr int kNB = G::kNB, kKB = G::kKB, kRowN = 2 * G::kN, kRowK = 2 * G::kK;
@@ -576,7 +581,7 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_stream_kernel(Grad
     };
 
     f32x16 acc[kNB][kKB] = {};
-    float bias[kNB] = {};
+    float bias[G::kSum] = {};
     const bool use_bias = a.gamma || (k0 == 0 && a.dbias);
     const int i16 = lane & 15, group = lane >> 4;
     const int t_row = (group >> 1) * 8 + i16 / 4, t_in = (i16 & 3) * 8;
@@ -586,7 +591,7 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_stream_kernel(Grad
     for (int e = 0; e < 2; ++e) {
         const int row = t_row + 16 * (e ^ turn);
 #pragma unroll
-        for (int b = 0; b < kNB; ++b) a_at[e][b] = kDy + swizzle<kRowN>(row, (wave_n * kNB + b) * 2 + (group & 1)) + t_in;
+        for (int b = 0; b < kNB; ++b) a_at[e][b] = kDy + swizzle<kRowN>(row, (wave_n * kNB + G::block(wave, b)) * 2 + (group & 1)) + t_in;
 #pragma unroll
         for (int b = 0; b < kKB; ++b) b_at[e][b] = kX + swizzle<kRowK>(row, (wave_k * kKB + b) * 2 + (group & 1)) + t_in;
     }
@@ -612,7 +617,7 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_stream_kernel(Grad
             if (e == 0) {
                 const bf16x2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
 #pragma unroll
-                for (int i = 0; i < kNB; ++i) {
+                for (int i = 0; i < G::kSum; ++i) {
                     float s = 0.0f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {

@@ -1,6 +1,9 @@
 // Layer norm, forward and backward, with the normalised row kept in 8 bits.
 //
-// Bound by HBM: forward reads 2 and writes 3.03 bytes an element (bf16, with a checkpoint), backward reads 3.03 and writes 2.
+// Bound by HBM: forward reads 2 and writes 3.03 bytes an element (bf16, with a checkpoint), backward reads 3.03 and writes 2; a residual
+// is 2 more.  Calls with a residual and a checkpoint: forward 16384 x 8192 183 us (5.2 TB/s), 65536 x 768 70 us (5.1), 8192 x 768
+// 11 us (4.4; two rows to a wavefront, so that starting and ending count); backward without one 16384 x 8192 143 us (4.7), 65536 x 768
+// 57 us (4.4), with one 16381 x 8192 169 + 5 us (5.6 TB/s), 8192 x 768 11 + 3 us, the second the sums over the workgroups.
 // A row is held in the registers of its team (16 lanes, a wavefront, or a workgroup) from the one load to the stores: the
 // mean, then the centred squares (no cancellation), then the outputs.  A team goes from row to row with the parameters in
 // registers and the next row's loads under way.  Backward keeps the two parameter gradients of its columns
@@ -165,7 +168,8 @@ __global__ __launch_bounds__((Team<kLanes, kWaves>::kBlock), 4) void norm_kernel
     }
 }
 
-// Forward with rows too long for the registers: a workgroup of 1024 threads passes over each row three times.
+// Forward with rows too long for the registers (more than 16384 columns): a workgroup of 1024 threads passes over each row three times,
+// two of them from the caches.  4096 x 16384 in this form 140 us (3.4 TB/s of what has to move).
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     __shared__ float sums[2][16];
@@ -458,7 +462,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a) {
 }
 
 // dgamma, dbeta = the partial sums' columns added up: 32 columns and 32 strands to a workgroup, each strand every 32nd
-// partial sum, then the strands in order.
+// partial sum, then the strands in order.  Latency: 2.5 to 4 us for 768 columns and 512 partial sums, 5 us for 8192 and 256.
 template <typename P>
 __global__ __launch_bounds__(1024) void norm_gradients_kernel(const float *part, int32_t n_part, int32_t cols, P *dgamma, P *dbeta) {
     __shared__ float strand[32][33];
@@ -505,6 +509,9 @@ uint32_t grid_of(int64_t rows, int64_t teams, int64_t most) {
 
 int launch_norm(const ::tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type) {
     const int64_t cus = ops->num_cus;
+    // The smallest team that holds the row: fewer barriers and sums, and no idle lanes.  Against the next larger one (us): 65536 x 128
+    // 11.5 and 25.3; 8192 x 512 7.2 and 8.7; x 768 10.1 and 15.2; x 2048 24.5 and 25.6; x 8192 90 and 99; 4096 x 16384 89 and,
+    // in three passes, 140.
     by_types(type, param_type, a.cols % kChunk == 0, [&](auto t, auto p, auto even) {
         using T = decltype(t);
         using P = decltype(p);
@@ -533,6 +540,8 @@ int launch_norm_backward(const ::tensile_ops *ops, hipStream_t s, const NormArgs
     const int64_t cus = ops->num_cus;
     NormArgs a = args;
     // workgroups: what is resident, two of 512 threads to a CU (partial sums take 8 bytes a column each)
+    // Teams as above; against the next larger one (us): 65536 x 128 12.7 and 23.3; 8192 x 512 10.0 and 12.0; x 768 12.7 and 17.1; x 2048
+    // 21.4 and 26.5; x 4096 41 and 55; 4096 x 16384 113 and, in two passes, 144.
     // (1024 threads have room for two chunks each of 16-bit gradients)
     const bool is_long = a.cols > (type == TENSILE_F32 ? 8192 : 16384);
     const int teams = a.cols <= 128 ? 32 : a.cols <= 512 ? 8 : a.cols <= 1024 ? 4 : a.cols <= 2048 ? 2 : 1, per_cu = a.cols <= 4096 ? 2 : 1;

@@ -109,10 +109,12 @@ struct Tile {
         return kByHalves ? p / 128 * 128 + (p >> 3) % 8 * 16 + (p >> 6) % 2 * 8 + p % 8 : p;
     }
 };
-using Staged = Tile<2, 2, 2, 2>;             // 128 x 128, two workgroups to a CU
+using Staged = Tile<2, 2, 2, 2>;             // 128 x 128, two workgroups to a CU, by way of registers
+using StagedWide = Tile<2, 2, 2, 4>;         // 128 x 256, one workgroup to a CU
 using Narrow = Tile<2, 2, 2, 2, true>;       // the same for the kernel of 16-bit brain floats
 using Wide = Tile<4, 2, 2, 4, true>;         // 256 x 256, one workgroup to a CU
 constexpr int kRows = 32;
+constexpr int kPartRows = 256;               // of a part at least, where the rows are split
 
 // Where a workgroup works.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets a run of consecutive
 // tiles, and consecutive tiles lie in bands kBand tiles high, so that those under way on an XCD share their rows of both operands.
@@ -230,7 +232,8 @@ __device__ __forceinline__ void finish(const GradArgs &g, const Place &w, const 
 }
 
 // The product for any type; 32 and 16-bit gradients are three and two pieces, each a product of its own, and bound by those:
-// 6000 x 8192 x 8192 2600 us (f32) and 1770 us (f16), 930 and 910 TFLOP/s in pieces; 4096 x 4096 x 4096 530 and 380 us.
+// 6000 x 8192 x 8192 2140 us (f32) and 1600 us (f16), 1130 and 1000 TFLOP/s in pieces; 4096 x 4096 x 4096 438 and 323 us.  Beside the
+// products it is ordinary instructions that count: to a matrix instruction 5 (f32), of which 2.7 take dy apart.
 // kByElement: matrices with rows shorter than a load, or too far apart for 32-bit offsets.
 template <typename T, typename G, bool kByElement>
 __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_kernel(GradArgs g) {
@@ -806,11 +809,11 @@ int run(const ::tensile_ops *ops, hipStream_t s, const LinearArgs &a) {
     g.tiles_k = (a.K + G::kK - 1) / G::kK;
     const int64_t tiles = static_cast<int64_t>(g.tiles_n) * g.tiles_k;
     if (tiles > (1 << 24)) { set_error("linear_grad: dw has more than 2^24 tiles of %d x %d", G::kN, G::kK); return TENSILE_E_RANGE; }
-    // The rows are split where there are fewer tiles than places, but not below 256 rows each.  (8192 x 3072 x 768, 36 tiles: 4 parts
+    // The rows are split where there are fewer tiles than places, but not below kPartRows each.  (8192 x 3072 x 768, 36 tiles: 4 parts
     // are no faster than 7: less to join, but 112 CUs idle.)
     const int64_t slots = G::kPerCu * static_cast<int64_t>(ops->num_cus);
     int64_t split = slots / tiles;
-    if (split > a.M / 256) split = a.M / 256;
+    if (split > a.M / kPartRows) split = a.M / kPartRows;
     if (split < 1) split = 1;
     g.rows_per_split = ((a.M + split - 1) / split + kRows - 1) / kRows * kRows;
     split = g.rows_per_split ? (a.M + g.rows_per_split - 1) / g.rows_per_split : 1;
@@ -853,6 +856,14 @@ int choose(const ::tensile_ops *ops, hipStream_t s, const LinearArgs &a) {
         if (wide >= 32 && padded <= area + area / 2) return run<T, Wide, false>(ops, s, a);
         return run<T, Narrow, false>(ops, s, a);
     } else {
+        // The wider tile takes dy apart once for 256 columns; the other has more workgroups where not even half the CUs get one.
+        // StagedWide against Staged (us, f32 and f16): 6000 x 8192 x 8192 2140 and 2545, 1604 and 1718; 8192 x 768 x 768 (18 tiles in
+        // 32 parts at most) 46 and 52, 37 and 42; 600 x 3072 x 768 (72 in 2) 32 and 35; 1000 x 1024 x 1024 (32 in 3) 28.9 and 27.9;
+        // 6000 x 300 x 300 (2.2 times its size in tiles) 26.3 and 25.5.
+        const int64_t wide = static_cast<int64_t>((a.N + StagedWide::kN - 1) / StagedWide::kN) * ((a.K + StagedWide::kK - 1) / StagedWide::kK);
+        const int64_t area = static_cast<int64_t>(a.N) * a.K, padded = wide * StagedWide::kN * StagedWide::kK;
+        const int64_t parts = a.M < 2 * kPartRows ? 1 : a.M / kPartRows;
+        if (2 * wide * parts >= ops->num_cus && padded <= area + area / 2) return run<T, StagedWide, false>(ops, s, a);
         return run<T, Staged, false>(ops, s, a);
     }
 }

@@ -479,6 +479,15 @@ def test_linear_grad_of_larger_tiles_at_odd_places(ops):
         check_grad(ops, "bf16", "bf16", M, N, K, affine="bf16")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_linear_grad_of_wider_tiles(ops, dtype):
+    """Gradients in several pieces: tiles of twice the checkpoint's columns, whole and ragged, with and without parts."""
+    for M, N, K in ((64, 2048, 2304), (97, 2050, 2001), (1, 2048, 2047), (2100, 500, 1001), (4352, 128, 2048)):
+        say(f"linear grad wider {dtype} {M}x{N}x{K}")
+        check_grad(ops, dtype, "f32", M, N, K, affine="f32")
+        check_grad(ops, dtype, dtype, M, N, K, skew=1)
+
+
 def test_linear_grad_of_larger_tiles_keeps_non_finite_values_apart(ops):
     M, N, K = 70, 2050, 2300
     rng = np.random.default_rng(16)

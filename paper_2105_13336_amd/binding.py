@@ -375,14 +375,27 @@ class Checkpoint:
     __slots__ = ("q", "scale", "_st")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor):
-        if q.dtype != torch.int8 or scale.dtype != torch.uint8 or q.dim() != 2 or scale.dim() != 2 or not q.is_cuda or not scale.is_cuda:
+        q_shape, s_shape = q.shape, scale.shape
+        if q.dtype != torch.int8 or scale.dtype != torch.uint8 or len(q_shape) != 2 or len(s_shape) != 2 or not q.is_cuda or not scale.is_cuda:
             raise TensileError(TENSILE_E_INVAL, "checkpoint: need CUDA tensors q [rows, cols] int8 and scale [rows, ceil(cols/32)] uint8")
-        (rows, cols), (srows, groups) = q.shape, scale.shape
-        if srows != rows or groups != (cols + GROUP - 1) // GROUP or (cols > 1 and q.stride(1) != 1) or (groups > 1 and scale.stride(1) != 1):
-            raise TensileError(TENSILE_E_INVAL, f"checkpoint: q {tuple(q.shape)} and scale {tuple(scale.shape)} do not belong together, "
+        rows, cols = q_shape
+        groups = (cols + GROUP - 1) // GROUP
+        ld_q, ld_s, wrong = cols, groups, s_shape[0] != rows or s_shape[1] != groups
+        if not q.is_contiguous():
+            row, col = q.stride()
+            wrong = wrong or (cols > 1 and col != 1)
+            if rows > 1:
+                ld_q = row
+        if not scale.is_contiguous():
+            row, col = scale.stride()
+            wrong = wrong or (groups > 1 and col != 1)
+            if rows > 1:
+                ld_s = row
+        if wrong:
+            raise TensileError(TENSILE_E_INVAL, f"checkpoint: q {tuple(q_shape)} and scale {tuple(s_shape)} do not belong together, "
                                                 "or a row's columns are not contiguous")
         self.q, self.scale = q, scale
-        self._st = _Ckpt(q.data_ptr(), scale.data_ptr(), rows, cols, q.stride(0) if rows > 1 else cols, scale.stride(0) if rows > 1 else groups)
+        self._st = _Ckpt(q.data_ptr(), scale.data_ptr(), rows, cols, ld_q, ld_s)
 
     @classmethod
     def empty(cls, rows: int, cols: int, device="cuda") -> "Checkpoint":

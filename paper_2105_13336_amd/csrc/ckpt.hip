@@ -7,7 +7,7 @@
 //
 // Kernel time and bytes moved: pack and unpack of 16384 x 3136 in 32 bits, one after the other, 62 + 42 us (258 MB each, together 5.0
 // TB/s: the pack waits for what the unpack before it has left in the 256 MB cache; by itself it takes 42); gelu 8192 x 3072 bf16 with
-// a checkpoint 27 us (127 MB, 4.7 TB/s), its instructions a third of that; gelu_backward 16384 x 16384 bf16 with a checkpoint
+// a checkpoint 27 us (127 MB, 4.7 TB/s; its instructions alone would take 15 of them); gelu_backward 16384 x 16384 bf16 with a checkpoint
 // of the output 290 us (1.63 GB, 5.6 TB/s); unpack of that 129 us (0.81 GB, 6.3 TB/s).  A large copy reaches 4.9 to 5.4 TB/s.
 #include "ops_device.h"
 

@@ -88,7 +88,8 @@ __device__ __forceinline__ void drop_front(Raw8<float> &r, int n, bool keep) {
 
 // A workgroup's tile: kWN x kWK wavefronts of 32 kNB columns of dy x 32 kKB columns of the checkpoint each, two wavefronts to a
 // SIMD in all; 32 rows to a step.  kByHalves: the columns of the checkpoint lie in the tile in the order that the streaming
-// kernel's staging gives them.
+// kernel's staging gives them, of 128 the first halves of eight sixteens and then the second.  A wavefront takes one block of
+// each: of four sixteens both halves.
 template <int kNB_, int kKB_, int kWN_, int kWK_, bool kByHalves_ = false>
 struct Tile {
     static constexpr int kNB = kNB_, kKB = kKB_, kWN = kWN_, kWK = kWK_;
@@ -104,9 +105,29 @@ struct Tile {
     static __device__ __forceinline__ int row(int wave, int lane, int i, int r) {
         return (wave / kWK * kNB + block(wave, i)) * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
     }
+    static __device__ __forceinline__ int column_block(int wave, int j) {
+        return kByHalves ? wave % kWK / 2 * 4 + wave % 2 + 2 * j : wave % kWK * kKB + j;
+    }
+    // (kByHalves: as `by_columns` leaves them)
     static __device__ __forceinline__ int column(int wave, int lane, int j) {
-        const int p = (wave % kWK * kKB + j) * 32 + (lane & 31);
-        return kByHalves ? p / 128 * 128 + (p >> 3) % 8 * 16 + (p >> 6) % 2 * 8 + p % 8 : p;
+        const int in = lane & 31;
+        return (wave % kWK * kKB + j) * 32 + (kByHalves ? (in >> 3) % 2 * 16 + (in >> 4) * 8 + in % 8 : in);
+    }
+    // kByHalves: block 0 is given the first two of the wavefront's four sixteens, block 1 the others, so that a store has 32 columns
+    // of a row to itself: the second row of 16 lanes of block 0 and the first of block 1 change places.  (A store of eight times 8
+    // columns is twice the requests.)
+    static __device__ __forceinline__ void by_columns(f32x16 (&acc)[kNB][kKB]) {
+        if constexpr (kByHalves) {
+            static_assert(kKB == 2 && kWK % 2 == 0, "");
+#pragma unroll
+            for (int i = 0; i < kNB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const auto v = __builtin_amdgcn_permlane16_swap(as_u32(acc[i][0][r]), as_u32(acc[i][1][r]), false, false);
+                    acc[i][0][r] = as_f32(v[0]);
+                    acc[i][1][r] = as_f32(v[1]);
+                }
+        }
     }
 };
 using Staged = Tile<2, 2, 2, 2>;             // 128 x 128, two workgroups to a CU, by way of registers
@@ -155,11 +176,12 @@ __device__ __forceinline__ float get_as(int type, const void *p, int64_t at) {
 // What a workgroup does with its tile's sums: dbias, and dw with the norm's parameters, or all as they are where the rows are split.
 // `sums` is LDS for two rows of the tile's width.
 template <typename T, typename G>
-__device__ __forceinline__ void finish(const GradArgs &g, const Place &w, const f32x16 (&acc)[G::kNB][G::kKB], const float (&bias)[G::kSum],
+__device__ __forceinline__ void finish(const GradArgs &g, const Place &w, f32x16 (&acc)[G::kNB][G::kKB], const float (&bias)[G::kSum],
                                        bool use_bias, float *sums) {
     constexpr int kNB = G::kNB, kKB = G::kKB;
     const LinearArgs &a = g.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    G::by_columns(acc);
     // sums of dy: over the two halves of the wavefront, then over the two halves of the steps
     if (use_bias) {
 #pragma unroll
@@ -391,7 +413,7 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_kernel(GradArgs g)
 #pragma unroll
         for (int b = 0; b < kNB; ++b) a_at[e][b] = swizzle<kRowN>(row, (wave_n * kNB + G::block(wave, b)) * 2 + (group & 1)) + t_in;
 #pragma unroll
-        for (int b = 0; b < kKB; ++b) b_at[e][b] = kP * kPlane + swizzle<kRowK>(row, (wave_k * kKB + b) * 2 + (group & 1)) + t_in;
+        for (int b = 0; b < kKB; ++b) b_at[e][b] = kP * kPlane + swizzle<kRowK>(row, G::column_block(wave, b) * 2 + (group & 1)) + t_in;
     }
     auto fragment = [&](const char *p, int four_rows) __attribute__((always_inline)) {
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -598,7 +620,7 @@ __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_stream_kernel(Grad
 #pragma unroll
         for (int b = 0; b < kNB; ++b) a_at[e][b] = kDy + swizzle<kRowN>(row, (wave_n * kNB + G::block(wave, b)) * 2 + (group & 1)) + t_in;
 #pragma unroll
-        for (int b = 0; b < kKB; ++b) b_at[e][b] = kX + swizzle<kRowK>(row, (wave_k * kKB + b) * 2 + (group & 1)) + t_in;
+        for (int b = 0; b < kKB; ++b) b_at[e][b] = kX + swizzle<kRowK>(row, G::column_block(wave, b) * 2 + (group & 1)) + t_in;
     }
     auto fragment = [&](int p, int four_rows) __attribute__((always_inline)) {
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;

@@ -865,8 +865,9 @@ int run(const ::tensile_ops *ops, hipStream_t s, const LinearArgs &a) {
 
 template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const LinearArgs &a) {
-    // A load takes 8 columns of dy, 16 of the checkpoint, and reaches them by 32 bits from the first of a step's 32 rows.
-    const bool by_element = a.N < 8 || a.K < 16 || a.dy.ld * static_cast<int64_t>(sizeof(T)) >= (1 << 26) || a.c.ld_q >= (1 << 26);
+    // A load takes 8 columns of dy, 16 of the checkpoint, and reaches them and the scales by 32 bits from the first of a step's 32 rows.
+    constexpr int64_t kFar = 1 << 26;
+    const bool by_element = a.N < 8 || a.K < 16 || a.dy.ld * static_cast<int64_t>(sizeof(T)) >= kFar || a.c.ld_q >= kFar || a.c.ld_scale >= kFar;
     if (by_element) return run<T, Staged, true>(ops, s, a);
     if constexpr (std::is_same<T, bf16_t>::value) {
         const int64_t wide = static_cast<int64_t>((a.N + Wide::kN - 1) / Wide::kN) * ((a.K + Wide::kK - 1) / Wide::kK);

@@ -382,8 +382,8 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
  * depend on timing: the same call on the same inputs gives the same bits.
  *
  * tensile_layer_norm_backward and tensile_linear_grad use scratch memory that
- * the tensile_ops handle keeps per stream, under the rules given at the top for a
- * sequence's handle: any number of host threads may share one handle, a call that needs
+ * the tensile_ops handle keeps per stream (of hipStreamPerThread: per host thread), under the rules given at
+ * the top for a sequence's handle: any number of host threads may share one handle, a call that needs
  * more than any earlier call on its stream allocates it, and a stream that is
  * to be captured makes one call of the largest shape first. */
 

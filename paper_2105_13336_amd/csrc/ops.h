@@ -4,19 +4,29 @@
 
 #include "common.h"
 
+#include <tuple>
+
 namespace tensile {
 
 constexpr int kGroup = 32;            // columns that share a scale
 constexpr int kChunk = 8;             // columns a lane holds at a time: four lanes hold a group
 constexpr uint32_t kNanCode = 255;
 
-// Scratch memory of the operators on one stream (see Workspace in common.h for the rules).
+// Scratch memory of the operators on one queue (see Workspace in common.h for the rules).
 struct OpsScratch {
     std::mutex mu;
     DevBuf<float> buf;
     std::vector<void *> retired;
     ~OpsScratch();
     int provide(size_t floats, const char *what);
+};
+
+// The queue whose calls run one after the other and share scratch.  A stream's handle names it, but for hipStreamPerThread, which is
+// another queue in every host thread: `thread` is that thread's number, never given twice, and 0 for the others.
+struct ScratchKey {
+    hipStream_t stream;
+    uint64_t thread;
+    bool operator<(const ScratchKey &o) const { return std::tie(stream, thread) < std::tie(o.stream, o.thread); }
 };
 
 struct Matrix {
@@ -77,10 +87,10 @@ struct tensile_ops {
     int device = 0;
     int num_cus = 256;
     mutable std::mutex mu;            // guards the map
-    mutable std::map<hipStream_t, std::unique_ptr<tensile::OpsScratch>> scratch;
+    mutable std::map<tensile::ScratchKey, std::unique_ptr<tensile::OpsScratch>> scratch;
 };
 
 namespace tensile {
-// The scratch of (handle, stream), created on first use; the caller locks it while it sizes it and enqueues.
+// The scratch of (handle, queue), created on first use; the caller locks it while it sizes it and enqueues.
 OpsScratch &ops_scratch(const tensile_ops *ops, hipStream_t stream);
 }  // namespace tensile

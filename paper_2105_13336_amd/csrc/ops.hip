@@ -1,6 +1,7 @@
 // Entry points of the operators on 8-bit checkpoints: the handle, its scratch memory and the checks of the arguments.
 #include "ops.h"
 
+#include <atomic>
 #include <cmath>
 #include <new>
 
@@ -31,9 +32,20 @@ int OpsScratch::provide(size_t floats, const char *what) {
     return TENSILE_OK;
 }
 
+namespace {
+
+uint64_t thread_number() {
+    static std::atomic<uint64_t> last{0};
+    thread_local const uint64_t own = ++last;
+    return own;
+}
+
+}  // namespace
+
 OpsScratch &ops_scratch(const tensile_ops *ops, hipStream_t stream) {
+    const ScratchKey key{stream, stream == hipStreamPerThread ? thread_number() : 0};
     std::lock_guard<std::mutex> g(ops->mu);
-    std::unique_ptr<OpsScratch> &slot = ops->scratch[stream];
+    std::unique_ptr<OpsScratch> &slot = ops->scratch[key];
     if (!slot) slot.reset(new OpsScratch());
     return *slot;
 }

@@ -52,3 +52,88 @@ def test_linear_grad_of_far_apart_rows(ops, dtype, M, far):
     near(dw, want, (M / 16 + 90) * 2.0 ** -24 * size, "dw")
     del wide
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------ scratch memory
+
+class PerThread:
+    """hipStreamPerThread: the same value in every host thread, a queue of its own in each."""
+    cuda_stream = 2
+
+
+class Split:
+    """A weight gradient whose rows are split, and a norm's backward pass: both leave partial sums in scratch memory."""
+
+    def __init__(self, seed, M=4096, N=192, K=320):
+        rng = np.random.default_rng(seed)
+        self.dz, self.dy = up(rng.standard_normal((M, N)), "bf16"), up(rng.standard_normal((M, K)), "bf16")
+        self.c, _ = filled(rng.standard_normal((M, K)))
+        self.g, self.rstd = torch.ones(K, device="cuda"), torch.ones(M, device="cuda")
+        self.out = [torch.empty(N, K, device="cuda"), torch.empty_like(self.dy), torch.empty_like(self.g), torch.empty_like(self.g)]
+
+    def run(self, ops, stream=None):
+        P.tensile_linear_grad(ops, self.dz, self.c, self.out[0], stream=stream)
+        P.tensile_layer_norm_backward(ops, self.dy, self.c, self.rstd, self.g, *self.out[1:], stream=stream)
+
+    def take(self):
+        torch.cuda.synchronize()
+        got = [t.clone() for t in self.out]
+        for t in self.out:
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+        return got
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def in_thread(f):
+    import threading
+    result = []
+
+    def run():
+        try:
+            result.append(f())
+        except P.TensileError as e:
+            result.append(e)
+    t = threading.Thread(target=run)
+    t.start()
+    t.join()
+    return result[0]
+
+
+def test_the_per_thread_stream_has_scratch_for_each_thread(tuning):
+    """A second thread's queue is another one: its call asks for memory of its own (refused here), not for the first thread's."""
+    h, work = P.tensile_ops_create(), Split(1)
+    work.run(h)
+    want = work.take()
+    work.run(h, PerThread)
+    assert same(work.take(), want)
+    tuning("alloc_fail", 1)
+    refused = in_thread(lambda: work.run(h, PerThread))
+    assert isinstance(refused, P.TensileError) and refused.code == P.binding.TENSILE_E_NOMEM
+    work.run(h, PerThread)                             # this thread has its own already
+    assert same(work.take(), want)
+    assert in_thread(lambda: work.run(h, PerThread)) is None
+    assert same(work.take(), want)
+    h.close()
+
+
+def test_threads_on_the_per_thread_stream(ops):
+    import threading
+    jobs = [Split(10 + k) for k in range(4)]
+    want = []
+    for j in jobs:
+        j.run(ops)
+        want.append(j.take())
+    def many(j):
+        for _ in range(20):
+            j.run(ops, PerThread)
+    threads = [threading.Thread(target=many, args=(j,)) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for j, w in zip(jobs, want):
+        assert same(j.take(), w)

@@ -383,9 +383,11 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
  *
  * tensile_layer_norm_backward and tensile_linear_grad use scratch memory that
  * the tensile_ops handle keeps per stream (of hipStreamPerThread: per host thread), under the rules given at
- * the top for a sequence's handle: any number of host threads may share one handle, a call that needs
- * more than any earlier call on its stream allocates it, and a stream that is
- * to be captured makes one call of the largest shape first. */
+ * the top for a sequence's handle: any number of host threads may share one handle, and a call that needs
+ * more than any earlier call on its stream allocates it.  What is captured has scratch memory of its own for every
+ * capture, allocated while the capture goes on and kept until the handle is freed: a graph may be launched on any stream, beside
+ * other graphs and beside eager calls, also on the stream that was captured.  A program that captures again and
+ * again has its graphs' calls made with a handle of their own, freed after them. */
 
 #define TENSILE_F32 0
 #define TENSILE_BF16 1

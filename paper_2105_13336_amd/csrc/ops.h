@@ -17,16 +17,20 @@ struct OpsScratch {
     std::mutex mu;
     DevBuf<float> buf;
     std::vector<void *> retired;
+    bool captured = false;            // belongs to a capture: it is provided while the stream is being captured
     ~OpsScratch();
     int provide(size_t floats, const char *what);
 };
 
-// The queue whose calls run one after the other and share scratch.  A stream's handle names it, but for hipStreamPerThread, which is
-// another queue in every host thread: `thread` is that thread's number, never given twice, and 0 for the others.
+// The queue whose calls run one after the other and share scratch.  A stream's handle names it, but for two cases:
+//   hipStreamPerThread is another queue in every host thread: `thread` is that thread's number, never given twice, else 0;
+//   what is captured runs wherever the graph is launched, beside other graphs captured on that stream and beside its eager calls:
+//   `capture` is the capture's number, 0 outside of one.
 struct ScratchKey {
     hipStream_t stream;
     uint64_t thread;
-    bool operator<(const ScratchKey &o) const { return std::tie(stream, thread) < std::tie(o.stream, o.thread); }
+    unsigned long long capture;
+    bool operator<(const ScratchKey &o) const { return std::tie(stream, thread, capture) < std::tie(o.stream, o.thread, o.capture); }
 };
 
 struct Matrix {

@@ -11,12 +11,45 @@ OpsScratch::~OpsScratch() {
     for (void *p : retired) (void)hipFree(p);
 }
 
+namespace {
+
+// While it lives, the calling thread may allocate although a stream is being captured (the allocation is no part of the graph).
+struct AllocateInCapture {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    const bool on;
+    explicit AllocateInCapture(bool wanted) : on(wanted && hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess) {}
+    ~AllocateInCapture() {
+        if (on) (void)hipThreadExchangeStreamCaptureMode(&mode);
+    }
+};
+
+uint64_t thread_number() {
+    static std::atomic<uint64_t> last{0};
+    thread_local const uint64_t own = ++last;
+    return own;
+}
+
+// 0: not being captured (the default stream never is).
+unsigned long long capture_number(hipStream_t stream) {
+    if (stream == nullptr) return 0;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (hipStreamGetCaptureInfo(stream, &status, &id) != hipSuccess) {
+        (void)hipGetLastError();
+        return 0;
+    }
+    return status == hipStreamCaptureStatusActive ? id : 0;
+}
+
+}  // namespace
+
 int OpsScratch::provide(size_t floats, const char *what) {
     if (buf.p && floats <= buf.n) return TENSILE_OK;
     size_t want = floats ? floats : 1;
     const size_t least = want;
     if (want < 2 * buf.n) want = 2 * buf.n;   // at least doubled: what is parked in `retired` stays below what is in use
     retired.reserve(retired.size() + 1);
+    const AllocateInCapture allowed(captured);
     float *fresh = nullptr;
     hipError_t e = device_malloc(reinterpret_cast<void **>(&fresh), want * sizeof(float));
     if (e != hipSuccess && want > least) {    // (memory for what is needed may still be there)
@@ -32,21 +65,14 @@ int OpsScratch::provide(size_t floats, const char *what) {
     return TENSILE_OK;
 }
 
-namespace {
-
-uint64_t thread_number() {
-    static std::atomic<uint64_t> last{0};
-    thread_local const uint64_t own = ++last;
-    return own;
-}
-
-}  // namespace
-
 OpsScratch &ops_scratch(const tensile_ops *ops, hipStream_t stream) {
-    const ScratchKey key{stream, stream == hipStreamPerThread ? thread_number() : 0};
+    const ScratchKey key{stream, stream == hipStreamPerThread ? thread_number() : 0, capture_number(stream)};
     std::lock_guard<std::mutex> g(ops->mu);
     std::unique_ptr<OpsScratch> &slot = ops->scratch[key];
-    if (!slot) slot.reset(new OpsScratch());
+    if (!slot) {
+        slot.reset(new OpsScratch());
+        slot->captured = key.capture != 0;
+    }
     return *slot;
 }
 

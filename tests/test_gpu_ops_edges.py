@@ -137,3 +137,96 @@ def test_threads_on_the_per_thread_stream(ops):
         t.join()
     for j, w in zip(jobs, want):
         assert same(j.take(), w)
+
+
+def captured(ops, works, stream):
+    """A graph of the works, one after the other, captured on the stream."""
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        for w in works:
+            w.run(ops, stream)
+    return graph
+
+
+def test_a_capture_has_scratch_of_its_own(tuning):
+    """The calls of a capture ask for memory (refused here, once), whatever the stream had before; so do those of the next capture."""
+    h, work, stream = P.tensile_ops_create(), Split(2), torch.cuda.Stream()
+    work.run(h)
+    want = work.take()
+    work.run(h, stream)
+    assert same(work.take(), want)
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            tuning("alloc_fail", 1)
+            try:
+                work.run(h, stream)
+                refused = 0
+            except P.TensileError as e:
+                refused = e.code
+            tuning("alloc_fail", 0)
+            work.run(h, stream)
+        assert refused == P.binding.TENSILE_E_NOMEM
+        graphs.append(graph)
+    for graph in graphs * 3:
+        graph.replay()
+        assert same(work.take(), want)
+        work.run(h, stream)
+        assert same(work.take(), want)
+    del graphs, graph
+    h.close()
+
+
+def test_a_capture_needs_no_earlier_call():
+    h, work, stream = P.tensile_ops_create(), Split(3), torch.cuda.Stream()
+    graph = captured(h, [work], stream)
+    for _ in range(3):
+        graph.replay()
+        got = work.take()
+        work.run(h)
+        assert same(got, work.take())
+    del graph
+    h.close()
+
+
+def test_graphs_of_one_stream_side_by_side_with_its_eager_calls(ops):
+    """Two graphs captured on one stream, replayed on two others, while that stream and the current one run the same calls."""
+    works = [Split(20 + k) for k in range(4)]
+    want = []
+    for w in works:
+        w.run(ops)
+        want.append(w.take())
+    first, others = torch.cuda.Stream(), [torch.cuda.Stream() for _ in range(2)]
+    graphs = [captured(ops, [w], first) for w in works[:2]]
+    for _ in range(20):
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for graph, s in zip(graphs, others):
+                with torch.cuda.stream(s):
+                    graph.replay()
+            works[2].run(ops, first)
+            works[3].run(ops)
+        for w, t in zip(works, want):
+            assert same(w.take(), t)
+
+
+def test_a_capture_over_two_streams(ops):
+    """Branches of one graph may run side by side: each has its own."""
+    a, b = Split(30), Split(31)
+    want = []
+    for w in (a, b):
+        w.run(ops)
+        want.append(w.take())
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=main):
+        side.wait_stream(main)
+        a.run(ops, main)
+        b.run(ops, side)
+        main.wait_stream(side)
+    for _ in range(10):
+        graph.replay()
+        assert same(a.take(), want[0])
+        graph.replay()
+        assert same(b.take(), want[1])

@@ -341,6 +341,7 @@ def tensile_greedy_plan(h: TasHandle, budget_bytes: int = 0, max_iters: int = 0,
 # ---------------------------------------------------------------- activations in 8 bits
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # TENSILE_F32, TENSILE_BF16, TENSILE_F16
+_I8, _U8 = torch.int8, torch.uint8
 GROUP = 32                                                         # columns that share a scale
 
 
@@ -370,13 +371,35 @@ class OpsHandle:
 
 class Checkpoint:
     """A matrix of activations in 8 bits: ``q`` [rows, cols] int8 and ``scale`` [rows, ceil(cols / 32)] uint8, both on the GPU,
-    the columns of a row contiguous (rows may lie further apart)."""
+    the columns of a row contiguous (rows may lie further apart).  Either may be replaced, or be given other memory (as where a
+    checkpoint leaves the GPU and comes back): the next call that takes the checkpoint looks at them anew."""
 
-    __slots__ = ("q", "scale", "_st")
+    __slots__ = ("_q", "_scale", "_q_at", "_scale_at", "_st")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor):
+        self._q, self._scale = q, scale
+        self._describe()
+
+    @property
+    def q(self) -> torch.Tensor:
+        return self._q
+
+    @q.setter
+    def q(self, q: torch.Tensor) -> None:
+        self._q, self._q_at = q, None
+
+    @property
+    def scale(self) -> torch.Tensor:
+        return self._scale
+
+    @scale.setter
+    def scale(self, scale: torch.Tensor) -> None:
+        self._scale, self._scale_at = scale, None
+
+    def _describe(self) -> None:
+        q, scale = self._q, self._scale
         q_shape, s_shape = q.shape, scale.shape
-        if q.dtype != torch.int8 or scale.dtype != torch.uint8 or len(q_shape) != 2 or len(s_shape) != 2 or not q.is_cuda or not scale.is_cuda:
+        if q.dtype is not _I8 or scale.dtype is not _U8 or len(q_shape) != 2 or len(s_shape) != 2 or not q.is_cuda or not scale.is_cuda:
             raise TensileError(TENSILE_E_INVAL, "checkpoint: need CUDA tensors q [rows, cols] int8 and scale [rows, ceil(cols/32)] uint8")
         rows, cols = q_shape
         groups = (cols + GROUP - 1) // GROUP
@@ -394,8 +417,8 @@ class Checkpoint:
         if wrong:
             raise TensileError(TENSILE_E_INVAL, f"checkpoint: q {tuple(q_shape)} and scale {tuple(s_shape)} do not belong together, "
                                                 "or a row's columns are not contiguous")
-        self.q, self.scale = q, scale
-        self._st = _Ckpt(q.data_ptr(), scale.data_ptr(), rows, cols, ld_q, ld_s)
+        self._q_at, self._scale_at = q.data_ptr(), scale.data_ptr()
+        self._st = _Ckpt(self._q_at, self._scale_at, rows, cols, ld_q, ld_s)
 
     @classmethod
     def empty(cls, rows: int, cols: int, device="cuda") -> "Checkpoint":
@@ -409,7 +432,8 @@ class Checkpoint:
 
     @property
     def nbytes(self) -> int:
-        return self._st.rows * (self._st.ld_q + self._st.ld_scale)
+        st = _ck(self)
+        return st.rows * (st.ld_q + st.ld_scale)
 
 
 def _mat(t: Optional[torch.Tensor], name: str):
@@ -440,7 +464,11 @@ def _vec(t: Optional[torch.Tensor], dtype, n: int, name: str):
 
 
 def _ck(c: Optional[Checkpoint]):
-    return None if c is None else c._st
+    if c is None:
+        return None
+    if c._q.data_ptr() != c._q_at or c._scale.data_ptr() != c._scale_at:
+        c._describe()
+    return c._st
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the current stream without a Stream object (2.8 us)
@@ -508,8 +536,8 @@ def tensile_gelu_backward(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dx
 def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: torch.Tensor, dbias: Optional[torch.Tensor] = None,
                         gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, stream=None) -> None:
     """dw [N, K] = dy^T X, dbias [N] = column sums of dy; X is what ckpt holds, or that * gamma + beta"""
-    m = _mat(dy, "dy")
-    K = ckpt._st.cols
+    m, c = _mat(dy, "dy"), _ck(ckpt)
+    K = c.cols
     param = None if gamma is None else gamma.dtype
-    _check(_lib.tensile_linear_grad(ops.ptr, m, _ck(ckpt), _vec(gamma, param, K, "gamma"), _vec(beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
+    _check(_lib.tensile_linear_grad(ops.ptr, m, c, _vec(gamma, param, K, "gamma"), _vec(beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
                                     _mat(dw, "dw"), _vec(dbias, dw.dtype, m.cols, "dbias"), _stream_ptr(stream, ops)))

@@ -230,3 +230,51 @@ def test_a_capture_over_two_streams(ops):
         assert same(a.take(), want[0])
         graph.replay()
         assert same(b.take(), want[1])
+
+
+# ------------------------------------------------------------------ what a call is given
+
+def test_a_checkpoint_that_is_moved(ops):
+    """Its tensors may be replaced or be given other memory; none of the old is read.  (`held` keeps the old memory where it is.)"""
+    c, v = filled(np.full((4, 70), 1.0))
+    other, w = filled(np.full((4, 70), 1.5))
+    held = c.q.view(4, 70), c.scale.view(4, 3)
+    y = torch.empty(4, 70, device="cuda")
+
+    def value():
+        y.fill_(9.0)
+        P.tensile_ckpt_unpack(ops, c, y)
+        return host(y)
+
+    assert np.array_equal(value(), v)
+    c.q, c.scale = other.q, other.scale                # replaced
+    assert np.array_equal(value(), w)
+    c.q, c.scale = held
+    assert np.array_equal(value(), v)
+    c.q.set_(other.q)                                  # the same tensors in another place
+    c.scale.set_(other.scale)
+    assert np.array_equal(value(), w)
+    kept = c.q.cpu(), c.scale.cpu()
+    c.q, c.scale = kept                                # off the GPU: refused there ...
+    with pytest.raises(P.TensileError) as e:
+        P.tensile_ckpt_unpack(ops, c, y)
+    assert e.value.code == P.binding.TENSILE_E_INVAL and "CUDA" in str(e.value)
+    c.q, c.scale = (t.cuda() for t in kept)            # ... and back
+    assert np.array_equal(value(), w) and c.shape == (4, 70)
+    c.q = c.q[:2]                                      # half of it: the scales do not belong
+    with pytest.raises(P.TensileError) as e:
+        P.tensile_ckpt_unpack(ops, c, y[:2])
+    assert "belong" in str(e.value)
+    c.scale = c.scale[:2]
+    P.tensile_ckpt_unpack(ops, c, y[:2])
+    assert c.nbytes == 2 * (70 + 3)
+
+
+def test_a_checkpoint_without_memory_is_refused(ops):
+    c, y = P.Checkpoint(torch.ones(4, 64, dtype=torch.int8, device="cuda"), torch.ones(4, 2, dtype=torch.uint8, device="cuda")), torch.empty(4, 64, device="cuda")
+    P.tensile_ckpt_unpack(ops, c, y)
+    torch.cuda.synchronize()
+    c.q.untyped_storage().resize_(0)
+    with pytest.raises(P.TensileError) as e:
+        P.tensile_ckpt_unpack(ops, c, y)
+    assert e.value.code == P.binding.TENSILE_E_INVAL and "NULL" in str(e.value)

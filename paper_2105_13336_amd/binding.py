@@ -374,7 +374,7 @@ class Checkpoint:
     the columns of a row contiguous (rows may lie further apart).  Either may be replaced, or be given other memory (as where a
     checkpoint leaves the GPU and comes back): the next call that takes the checkpoint looks at them anew."""
 
-    __slots__ = ("_q", "_scale", "_q_at", "_scale_at", "_st")
+    __slots__ = ("_q", "_scale", "_q_at", "_scale_at", "_device", "_st")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor):
         self._q, self._scale = q, scale
@@ -399,8 +399,9 @@ class Checkpoint:
     def _describe(self) -> None:
         q, scale = self._q, self._scale
         q_shape, s_shape = q.shape, scale.shape
-        if q.dtype is not _I8 or scale.dtype is not _U8 or len(q_shape) != 2 or len(s_shape) != 2 or not q.is_cuda or not scale.is_cuda:
-            raise TensileError(TENSILE_E_INVAL, "checkpoint: need CUDA tensors q [rows, cols] int8 and scale [rows, ceil(cols/32)] uint8")
+        self._device = q.get_device()                                    # -1: not on a GPU
+        if q.dtype is not _I8 or scale.dtype is not _U8 or len(q_shape) != 2 or len(s_shape) != 2 or self._device < 0 or scale.get_device() != self._device:
+            raise TensileError(TENSILE_E_INVAL, "checkpoint: need CUDA tensors q [rows, cols] int8 and scale [rows, ceil(cols/32)] uint8 on one device")
         rows, cols = q_shape
         groups = (cols + GROUP - 1) // GROUP
         ld_q, ld_s, wrong = cols, groups, s_shape[0] != rows or s_shape[1] != groups
@@ -432,17 +433,19 @@ class Checkpoint:
 
     @property
     def nbytes(self) -> int:
-        st = _ck(self)
-        return st.rows * (st.ld_q + st.ld_scale)
+        if self._q.data_ptr() != self._q_at or self._scale.data_ptr() != self._scale_at:
+            self._describe()
+        return self._st.rows * (self._st.ld_q + self._st.ld_scale)
 
 
-def _mat(t: Optional[torch.Tensor], name: str):
+def _mat(device: int, t: Optional[torch.Tensor], name: str):
     """[..., cols] with contiguous columns and evenly spaced rows, as a matrix."""
     if t is None:
         return None
     code, shape = _TYPES.get(t.dtype), t.shape
-    if code is None or not t.is_cuda or not shape:
-        raise TensileError(TENSILE_E_INVAL, f"{name}: need a CUDA tensor of float32, bfloat16 or float16 with at least one dimension")
+    if code is None or t.get_device() != device or not shape:
+        raise TensileError(TENSILE_E_INVAL, f"{name}: need a CUDA tensor on the handle's device ({device}), of float32, bfloat16 or float16, "
+                                            "with at least one dimension")
     if t.is_contiguous():                                              # (one question fewer than the strides: small calls are bound here)
         cols = shape[-1]
         return _Matrix(t.data_ptr(), shape[0] if len(shape) == 2 else t.numel() // cols if cols else 0, cols, cols, code)
@@ -455,19 +458,21 @@ def _mat(t: Optional[torch.Tensor], name: str):
     return _Matrix(t.data_ptr(), rows, cols, row if rows > 1 else cols, code)
 
 
-def _vec(t: Optional[torch.Tensor], dtype, n: int, name: str):
+def _vec(device: int, t: Optional[torch.Tensor], dtype, n: int, name: str):
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-        raise TensileError(TENSILE_E_INVAL, f"{name}: need a contiguous CUDA tensor of {dtype} with {n} elements")
+    if t.get_device() != device or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise TensileError(TENSILE_E_INVAL, f"{name}: need a contiguous CUDA tensor on the handle's device ({device}), of {dtype} with {n} elements")
     return t.data_ptr()
 
 
-def _ck(c: Optional[Checkpoint]):
+def _ck(device: int, c: Optional[Checkpoint]):
     if c is None:
         return None
     if c._q.data_ptr() != c._q_at or c._scale.data_ptr() != c._scale_at:
         c._describe()
+    if c._device != device:
+        raise TensileError(TENSILE_E_INVAL, f"checkpoint: it is on device {c._device}, the handle belongs to device {device}")
     return c._st
 
 
@@ -476,6 +481,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the curre
 
 def _stream_ptr(stream, ops: OpsHandle) -> int:
     if stream is not None:
+        if getattr(stream, "device_index", ops.device) != ops.device:
+            raise TensileError(TENSILE_E_INVAL, f"stream: it is of device {stream.device_index}, the handle belongs to device {ops.device}")
         return stream.cuda_stream
     return _raw_stream(ops.device) if _raw_stream else torch.cuda.current_stream(ops.device).cuda_stream
 
@@ -493,51 +500,58 @@ def tensile_ops_free(ops: OpsHandle) -> None:
 
 def tensile_ckpt_pack(ops: OpsHandle, x: torch.Tensor, c: Checkpoint, stream=None) -> None:
     """c = x in 8 bits"""
-    _check(_lib.tensile_ckpt_pack(ops.ptr, _mat(x, "x"), _ck(c), _stream_ptr(stream, ops)))
+    d = ops.device
+    _check(_lib.tensile_ckpt_pack(ops.ptr, _mat(d, x, "x"), _ck(d, c), _stream_ptr(stream, ops)))
 
 
 def tensile_ckpt_unpack(ops: OpsHandle, c: Checkpoint, y: torch.Tensor, stream=None) -> None:
     """y = the values of c"""
-    _check(_lib.tensile_ckpt_unpack(ops.ptr, _ck(c), _mat(y, "y"), _stream_ptr(stream, ops)))
+    d = ops.device
+    _check(_lib.tensile_ckpt_unpack(ops.ptr, _ck(d, c), _mat(d, y, "y"), _stream_ptr(stream, ops)))
 
 
 def tensile_layer_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, y: torch.Tensor, eps: float = 1e-5,
                        residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, xhat: Optional[Checkpoint] = None,
                        rstd: Optional[torch.Tensor] = None, stream=None) -> None:
     """y = layer norm of x (+ residual); total: the sum; xhat, rstd: what the backward pass reads"""
-    m = _mat(x, "x")
-    _check(_lib.tensile_layer_norm(ops.ptr, m, _mat(residual, "residual"), _vec(gamma, gamma.dtype, m.cols, "gamma"),
-                                   _vec(beta, gamma.dtype, m.cols, "beta"), _TYPES.get(gamma.dtype, -1), eps, _mat(y, "y"), _mat(total, "total"),
-                                   _ck(xhat), _vec(rstd, torch.float32, m.rows, "rstd"), _stream_ptr(stream, ops)))
+    d = ops.device
+    m = _mat(d, x, "x")
+    _check(_lib.tensile_layer_norm(ops.ptr, m, _mat(d, residual, "residual"), _vec(d, gamma, gamma.dtype, m.cols, "gamma"),
+                                   _vec(d, beta, gamma.dtype, m.cols, "beta"), _TYPES.get(gamma.dtype, -1), eps, _mat(d, y, "y"), _mat(d, total, "total"),
+                                   _ck(d, xhat), _vec(d, rstd, torch.float32, m.rows, "rstd"), _stream_ptr(stream, ops)))
 
 
 def tensile_layer_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoint, rstd: torch.Tensor, gamma: torch.Tensor, dx: torch.Tensor,
                                 dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
                                 dresidual: Optional[torch.Tensor] = None, stream=None) -> None:
     """dx = gradient through the norm (+ dresidual); dgamma, dbeta: the parameters' gradients"""
-    m = _mat(dy, "dy")
-    _check(_lib.tensile_layer_norm_backward(ops.ptr, m, _ck(xhat), _vec(rstd, torch.float32, m.rows, "rstd"),
-                                            _vec(gamma, gamma.dtype, m.cols, "gamma"), _TYPES.get(gamma.dtype, -1), _mat(dresidual, "dresidual"),
-                                            _mat(dx, "dx"), _vec(dgamma, gamma.dtype, m.cols, "dgamma"),
-                                            _vec(dbeta, gamma.dtype, m.cols, "dbeta"), _stream_ptr(stream, ops)))
+    d = ops.device
+    m = _mat(d, dy, "dy")
+    _check(_lib.tensile_layer_norm_backward(ops.ptr, m, _ck(d, xhat), _vec(d, rstd, torch.float32, m.rows, "rstd"),
+                                            _vec(d, gamma, gamma.dtype, m.cols, "gamma"), _TYPES.get(gamma.dtype, -1), _mat(d, dresidual, "dresidual"),
+                                            _mat(d, dx, "dx"), _vec(d, dgamma, gamma.dtype, m.cols, "dgamma"),
+                                            _vec(d, dbeta, gamma.dtype, m.cols, "dbeta"), _stream_ptr(stream, ops)))
 
 
 def tensile_gelu(ops: OpsHandle, x: torch.Tensor, y: torch.Tensor, ckpt: Optional[Checkpoint] = None, tanh: bool = False, stream=None) -> None:
     """y = gelu(x); ckpt: x in 8 bits"""
-    _check(_lib.tensile_gelu(ops.ptr, _mat(x, "x"), _mat(y, "y"), _ck(ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
+    d = ops.device
+    _check(_lib.tensile_gelu(ops.ptr, _mat(d, x, "x"), _mat(d, y, "y"), _ck(d, ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
 
 
 def tensile_gelu_backward(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dx: torch.Tensor, y_ckpt: Optional[Checkpoint] = None,
                           tanh: bool = False, stream=None) -> None:
     """dx = dy * gelu'(x) at the x that ckpt holds; y_ckpt: gelu(x) in 8 bits, for the next layer's weight gradient"""
-    _check(_lib.tensile_gelu_backward(ops.ptr, _mat(dy, "dy"), _ck(ckpt), _mat(dx, "dx"), _ck(y_ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
+    d = ops.device
+    _check(_lib.tensile_gelu_backward(ops.ptr, _mat(d, dy, "dy"), _ck(d, ckpt), _mat(d, dx, "dx"), _ck(d, y_ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
 
 
 def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: torch.Tensor, dbias: Optional[torch.Tensor] = None,
                         gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, stream=None) -> None:
     """dw [N, K] = dy^T X, dbias [N] = column sums of dy; X is what ckpt holds, or that * gamma + beta"""
-    m, c = _mat(dy, "dy"), _ck(ckpt)
+    d = ops.device
+    m, c = _mat(d, dy, "dy"), _ck(d, ckpt)
     K = c.cols
     param = None if gamma is None else gamma.dtype
-    _check(_lib.tensile_linear_grad(ops.ptr, m, c, _vec(gamma, param, K, "gamma"), _vec(beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
-                                    _mat(dw, "dw"), _vec(dbias, dw.dtype, m.cols, "dbias"), _stream_ptr(stream, ops)))
+    _check(_lib.tensile_linear_grad(ops.ptr, m, c, _vec(d, gamma, param, K, "gamma"), _vec(d, beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
+                                    _mat(d, dw, "dw"), _vec(d, dbias, dw.dtype, m.cols, "dbias"), _stream_ptr(stream, ops)))

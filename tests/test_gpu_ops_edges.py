@@ -278,3 +278,37 @@ def test_a_checkpoint_without_memory_is_refused(ops):
     with pytest.raises(P.TensileError) as e:
         P.tensile_ckpt_unpack(ops, c, y)
     assert e.value.code == P.binding.TENSILE_E_INVAL and "NULL" in str(e.value)
+
+
+def every_call(ops, x, c, v, rstd, dw, db, stream=None):
+    """One call of each entry point; x, dw: matrices, v: the norm's parameters, c: a checkpoint like x."""
+    return {"ckpt_pack": lambda: P.tensile_ckpt_pack(ops, x, c, stream=stream),
+            "ckpt_unpack": lambda: P.tensile_ckpt_unpack(ops, c, x, stream=stream),
+            "layer_norm": lambda: P.tensile_layer_norm(ops, x, v, v, x, xhat=c, rstd=rstd, stream=stream),
+            "layer_norm_backward": lambda: P.tensile_layer_norm_backward(ops, x, c, rstd, v, x, stream=stream),
+            "gelu": lambda: P.tensile_gelu(ops, x, x, ckpt=c, stream=stream),
+            "gelu_backward": lambda: P.tensile_gelu_backward(ops, x, c, x, stream=stream),
+            "linear_grad": lambda: P.tensile_linear_grad(ops, x, c, dw, dbias=db, gamma=v, beta=v, stream=stream)}
+
+
+def test_tensors_and_streams_of_another_device_are_refused(ops):
+    """A kernel would follow their addresses on the handle's device.  (With a handle that says that it belongs to the next device: nothing gets as
+    far as the library.)"""
+    x, v, dw = torch.zeros(4, 64, device="cuda"), torch.zeros(64, device="cuda"), torch.zeros(64, 64, device="cuda")
+    c, rstd, db = P.Checkpoint.empty(4, 64), torch.zeros(4, device="cuda"), torch.zeros(64, device="cuda")
+    elsewhere = P.OpsHandle(ops.ptr, ops.device + 1)
+    try:
+        for name, call in every_call(elsewhere, x, c, v, rstd, dw, db).items():
+            with pytest.raises(P.TensileError) as e:
+                call()
+            assert e.value.code == P.binding.TENSILE_E_INVAL and "device" in str(e.value), name
+        for check in (lambda: P.binding._mat(elsewhere.device, x, "x"), lambda: P.binding._vec(elsewhere.device, v, v.dtype, 64, "v"),
+                      lambda: P.binding._ck(elsewhere.device, c), lambda: P.binding._stream_ptr(torch.cuda.Stream(), elsewhere)):
+            with pytest.raises(P.TensileError) as e:
+                check()
+            assert "device" in str(e.value)
+    finally:
+        elsewhere._ptr = 0                             # (it is not this handle's to free)
+    for name, call in every_call(ops, x, c, v, rstd, dw, db, stream=torch.cuda.Stream()).items():
+        call()
+    torch.cuda.synchronize()

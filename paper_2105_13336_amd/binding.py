@@ -476,6 +476,12 @@ def _ck(device: int, c: Optional[Checkpoint]):
     return c._st
 
 
+def _missing(**args) -> None:
+    for name, value in args.items():
+        if value is None:
+            raise TensileError(TENSILE_E_INVAL, f"{name}: is None")
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the current stream without a Stream object (2.8 us)
 
 
@@ -514,6 +520,8 @@ def tensile_layer_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, bet
                        residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, xhat: Optional[Checkpoint] = None,
                        rstd: Optional[torch.Tensor] = None, stream=None) -> None:
     """y = layer norm of x (+ residual); total: the sum; xhat, rstd: what the backward pass reads"""
+    if x is None or gamma is None:
+        _missing(x=x, gamma=gamma)
     d = ops.device
     m = _mat(d, x, "x")
     _check(_lib.tensile_layer_norm(ops.ptr, m, _mat(d, residual, "residual"), _vec(d, gamma, gamma.dtype, m.cols, "gamma"),
@@ -525,6 +533,8 @@ def tensile_layer_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoi
                                 dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
                                 dresidual: Optional[torch.Tensor] = None, stream=None) -> None:
     """dx = gradient through the norm (+ dresidual); dgamma, dbeta: the parameters' gradients"""
+    if dy is None or gamma is None:
+        _missing(dy=dy, gamma=gamma)
     d = ops.device
     m = _mat(d, dy, "dy")
     _check(_lib.tensile_layer_norm_backward(ops.ptr, m, _ck(d, xhat), _vec(d, rstd, torch.float32, m.rows, "rstd"),
@@ -549,6 +559,8 @@ def tensile_gelu_backward(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dx
 def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: torch.Tensor, dbias: Optional[torch.Tensor] = None,
                         gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, stream=None) -> None:
     """dw [N, K] = dy^T X, dbias [N] = column sums of dy; X is what ckpt holds, or that * gamma + beta"""
+    if dy is None or ckpt is None or dw is None:
+        _missing(dy=dy, ckpt=ckpt, dw=dw)
     d = ops.device
     m, c = _mat(d, dy, "dy"), _ck(d, ckpt)
     K = c.cols

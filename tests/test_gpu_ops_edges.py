@@ -312,3 +312,20 @@ def test_tensors_and_streams_of_another_device_are_refused(ops):
     for name, call in every_call(ops, x, c, v, rstd, dw, db, stream=torch.cuda.Stream()).items():
         call()
     torch.cuda.synchronize()
+
+
+def test_arguments_that_are_missing(ops):
+    """None where a call needs a tensor is this library's error, like any other wrong argument."""
+    x, v, dw = torch.zeros(4, 64, device="cuda"), torch.zeros(64, device="cuda"), torch.zeros(64, 64, device="cuda")
+    c, rstd = P.Checkpoint.empty(4, 64), torch.zeros(4, device="cuda")
+    calls = {P.tensile_ckpt_pack: (x, c), P.tensile_ckpt_unpack: (c, x), P.tensile_layer_norm: (x, v, v, x), P.tensile_layer_norm_backward: (x, c, rstd, v, x),
+             P.tensile_gelu: (x, x), P.tensile_gelu_backward: (x, c, x), P.tensile_linear_grad: (x, c, dw)}
+    for call, args in calls.items():
+        call(ops, *args)
+        for k in range(len(args)):
+            with pytest.raises(P.TensileError) as e:
+                call(ops, *args[:k], None, *args[k + 1:])
+            assert e.value.code == P.binding.TENSILE_E_INVAL, (call.__name__, k)
+    for given in (dict(gamma=v), dict(beta=v)):
+        with pytest.raises(P.TensileError):
+            P.tensile_linear_grad(ops, x, c, dw, **given)

@@ -52,15 +52,17 @@ struct GradArgs {
 template <int kRowBytes>
 __device__ __forceinline__ int swizzle(int row, int block) { return row * kRowBytes + ((block ^ (2 * (row & 3))) * 32); }
 
-// x = p[0] + p[1] + ...: each piece the leading 8 bits of what is left (exact); infinities and NaN are all in the first.
+// x = p[0] + p[1] + ...: each piece the leading 8 bits of what is left (exact); infinities and NaN are all in the first.  (Quieted: a
+// NaN whose bits are all in the lower half would be an infinity.)
 template <int kPieces>
 __device__ __forceinline__ void split_bf16(float x, uint32_t (&p)[kPieces]) {
+    x = __builtin_canonicalizef(x);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
         const uint32_t top = as_u32(x) & 0xffff0000u;
         p[k] = top;
         const float rest = x - as_f32(top);
-        x = (top & 0x7f800000u) == 0x7f800000u ? 0.0f : rest;
+        x = k == 0 && (top & 0x7f800000u) == 0x7f800000u ? 0.0f : rest;
     }
 }
 

@@ -54,6 +54,25 @@ def test_linear_grad_of_far_apart_rows(ops, dtype, M, far):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("M,N,K", [(70, 140, 140), (33, 5, 40), (64, 2048, 2304), (4100, 130, 200)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_grad_of_every_nan(ops, dtype, M, N, K):
+    """A NaN is one whatever its bits: the quiet one, and those whose only bits are the lowest or the highest below the quiet one's."""
+    say(f"linear grad of NaN {dtype} {M}x{N}x{K}")
+    bits, int_type = {"f32": ((0x7fc00000, 0x7f800001, 0x7fbfffff, -0x7fffff), torch.int32), "bf16": ((0x7fc0, 0x7f81, 0x7fbf, -0x7f), torch.int16),
+                      "f16": ((0x7e00, 0x7c01, 0x7dff, -0x3ff), torch.int16)}[dtype]
+    dy = up(np.ones((M, N)), dtype)
+    for k, b in enumerate(bits):
+        dy.view(int_type)[M - 1 - 7 * k, k] = b
+    assert int(dy.isnan().sum()) == 4
+    c, _ = filled(np.ones((M, K)))
+    dw, db = torch.empty(N, K, device="cuda"), torch.empty(N, device="cuda")
+    for affine in ({}, dict(gamma=torch.ones(K, device="cuda"), beta=torch.ones(K, device="cuda"))):
+        P.tensile_linear_grad(ops, dy, c, dw, dbias=db, **affine)
+        assert bool(dw[:4].isnan().all()) and bool(db[:4].isnan().all())
+        assert bool((dw[4:] == (2.0 if affine else 1.0) * M).all()) and bool((db[4:] == M).all())
+
+
 # ------------------------------------------------------------------ scratch memory
 
 class PerThread:

@@ -449,7 +449,7 @@ int tensile_layer_norm_backward(tensile_ops *ops, const tensile_matrix *dy, cons
                                 const tensile_matrix *dx, void *dgamma, void *dbeta, void *hip_stream);
 
 /* y = x*Phi(x), Phi the normal distribution function; with tanh_form non-zero
- * y = x*(1 + tanh(sqrt(2/pi)*(x + 0.044715*x^3)))/2.
+ * y = x*(1 + tanh(sqrt(2/pi)*(x + 0.044715*x^3)))/2.  (Of -inf, where the product is one with 0, NaN in both.)
  *   y   like x; may be x itself
  *   c   checkpoint of x, or NULL */
 int tensile_gelu(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *y, const tensile_ckpt *c,

@@ -147,10 +147,10 @@ __device__ __forceinline__ float gelu(float x) {
     } else {                                        // x*Phi(x) = max(x, 0) - |x|*(1 - Phi(|x|))
         float e;
         const float tail = normal_tail(x, e);
-        const float most = __builtin_amdgcn_fmed3f(__builtin_fabsf(x), 0.0f, 100.0f);
+        const float most = __builtin_amdgcn_fmed3f(x, -__builtin_inff(), 100.0f);   // (inf stays out of the product, -inf * 0 is NaN)
         float above;
         asm("v_max_f32 %0, 0, %1" : "=v"(above) : "v"(x));   // (fmax costs two more, to quiet a NaN; `tail` brings it in)
-        return __builtin_fmaf(-most, tail, above);
+        return __builtin_fmaf(-__builtin_fabsf(most), tail, above);
     }
 }
 // y and dy/dx

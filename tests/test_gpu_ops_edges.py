@@ -73,6 +73,24 @@ def test_linear_grad_of_every_nan(ops, dtype, M, N, K):
         assert bool((dw[4:] == (2.0 if affine else 1.0) * M).all()) and bool((db[4:] == M).all())
 
 
+# ------------------------------------------------------------------ gelu
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tanh", [False, True])
+def test_gelu_of_infinities(ops, dtype, tanh):
+    """x*Phi(x): inf at inf, NaN (a product with 0) at -inf; what is around them is finite and their group is lost."""
+    for cols in (5, 64, 100):
+        x = np.ones((3, cols))
+        x[0, 1], x[1, 2], x[2, 3] = np.inf, -np.inf, np.nan
+        xd = up(x, dtype)
+        y, c = torch.empty_like(xd), P.Checkpoint.empty(3, cols)
+        P.tensile_gelu(ops, xd, y, ckpt=c, tanh=tanh)
+        got = host(y)
+        assert got[0, 1] == np.inf and np.isnan(got[1, 2]) and np.isnan(got[2, 3])
+        assert np.isfinite(got).sum() == got.size - 3
+        assert np.array_equal(c.scale.cpu().numpy() == 255, np.arange((cols + 31) // 32)[None, :] == np.zeros((3, 1)))
+
+
 # ------------------------------------------------------------------ scratch memory
 
 class PerThread:

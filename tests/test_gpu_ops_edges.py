@@ -9,6 +9,7 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():
     pytest.skip("needs a GPU", allow_module_level=True)
 
+import ops_plain as plain  # noqa: E402
 import paper_2105_13336_amd as P  # noqa: E402
 from test_gpu_ops import check_grad, filled, host, near, say, up  # noqa: E402
 
@@ -89,6 +90,59 @@ def test_gelu_of_infinities(ops, dtype, tanh):
         assert got[0, 1] == np.inf and np.isnan(got[1, 2]) and np.isnan(got[2, 3])
         assert np.isfinite(got).sum() == got.size - 3
         assert np.array_equal(c.scale.cpu().numpy() == 255, np.arange((cols + 31) // 32)[None, :] == np.zeros((3, 1)))
+
+
+def from_tails(x, tanh):
+    """gelu in 64 bits from the tail 1 - P(|x|) of the form's distribution function P (1 + tanh and 1 + erf cancel where x is far below 0, in 64 bits too);
+    -> value, derivative, the tail, exp(-x^2/2) or P, |2u| or 0"""
+    from scipy.special import erfc
+    a = np.abs(x)
+    if tanh:
+        k = np.sqrt(2 / np.pi)
+        u2 = 2 * k * (a + 0.044715 * a ** 3)
+        tail, e = 1 / (1 + np.exp(np.minimum(u2, 700))), 1 / (1 + np.exp(-u2))
+        density = tail * e * 2 * k * (1 + 3 * 0.044715 * x * x)
+    else:
+        u2, tail, e = 0 * a, 0.5 * erfc(a / np.sqrt(2)), np.exp(-0.5 * a * a)
+        density = e / np.sqrt(2 * np.pi)
+    y, slope = np.maximum(x, 0) - a * tail, np.where(x < 0, tail, 1 - tail) + x * density
+    for got, want in zip((y, slope), plain.gelu(x, tanh)):
+        assert np.abs(got - want).max() < 1e-13
+    return y, slope, tail, e, u2
+
+
+@pytest.mark.parametrize("tanh", [False, True])
+def test_gelu_to_32_bits(ops, tanh):
+    """Errors counted in roundings, U = 2^-24 each; an exponential and a reciprocal are within 2.
+
+    erf form: v has 5 (two products, a sum, a reciprocal), v*Q'(v) and its sum move R by at most 0.4 and 0.5 of that, so R is within 5 U absolutely,
+    and R >= 0.35/(1 + |x|): 15 U (1 + |x|) relatively; exp(-x^2/2): three roundings of an exponent of x^2/2 and 2: 1.5 x^2 + 2; a product.
+    tanh form: four roundings of the exponent |2u| and 2 of the exponential, three of t, a product.
+    The derivative is 1 or 0 plus a product of the same numbers: e*(x/sqrt(2 pi) -+ R) or tail*(x*t*w -+ 1), w = d(2u)/dx, of 2 roundings more."""
+    rng = np.random.default_rng(77)
+    x = np.concatenate([np.linspace(-16, 16, 4096 - 7), [0.0, -0.0, 1e-20, -1e-20, 1e-3, -1e-3, 12.9], rng.standard_normal(4096), rng.standard_normal(4096) * 1e-2]).reshape(96, 128)
+    xd = up(x)
+    x = host(xd)
+    y = torch.empty_like(xd)
+    P.tensile_gelu(ops, xd, y, tanh=tanh)
+    u, least = 2.0 ** -24, 1e-36                      # (a result below the normal numbers is 0: |x| * 2^-126)
+    y0, _, tail, e, u2 = from_tails(x, tanh)
+    a = np.abs(x)
+    relative = (4 * u2 + 9) if tanh else 15 * (1 + a) + 1.5 * a * a + 4
+    near(y, y0, 2 * u * np.abs(y0) + u * relative * a * tail + least, "gelu")
+
+    c, v = filled(x)
+    dy = torch.ones(x.shape, dtype=torch.float32, device="cuda")
+    dx, yc = torch.empty_like(dy), P.Checkpoint.empty(*x.shape)
+    P.tensile_gelu_backward(ops, dy, c, dx, y_ckpt=yc, tanh=tanh)
+    _, slope, tail, e, u2 = from_tails(v, tanh)
+    a = np.abs(v)
+    if tanh:
+        rest = a * e * (1.5957691216057308 + 0.21406444881780076 * v * v)                         # |x|*t*w; e is t here
+        off = tail * ((4 * u2 + 8) * (rest + 1) + 8 * rest + 1)
+    else:
+        off = e * ((1.5 * a * a + 2) * (a * 0.3989422804014327 + 0.5) + 6 + a)
+    near(dx, slope, 2 * u * np.abs(slope) + u * off + least, "derivative")
 
 
 # ------------------------------------------------------------------ scratch memory

@@ -428,7 +428,7 @@ int tensile_ckpt_unpack(tensile_ops *ops, const tensile_ckpt *c, const tensile_m
  *   xhat = (s - mean)*rstd;  y = xhat*gamma + beta
  *   residual    matrix like x, or NULL
  *   gamma, beta [cols] of param_type, which is TENSILE_F32 or x's type
- *   eps         >= 0
+ *   eps         >= 0, at most the largest 32-bit number (and held as one: the smallest above 0 stands for what is less)
  *   y           like x; may be x or residual itself
  *   total       s, like x, or NULL; may be x or residual itself (but not y)
  *   xhat        checkpoint of xhat, or NULL

@@ -2,7 +2,7 @@
 #include "ops.h"
 
 #include <atomic>
-#include <cmath>
+#include <cfloat>
 #include <new>
 
 namespace tensile {
@@ -241,7 +241,7 @@ int tensile_layer_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_
         if (xhat) TS_TRY(check_ckpt(xhat, x->rows, x->cols, who, "xhat"));
         TS_TRY(check_param(gamma, param_type, x->type, who, "gamma"));
         TS_TRY(check_param(beta, param_type, x->type, who, "beta"));
-        if (!(eps >= 0.0) || std::isinf(eps)) return refuse(who, "eps", "is negative or not finite");
+        if (!(eps >= 0.0 && eps <= FLT_MAX)) return refuse(who, "eps", "is negative or not a finite 32-bit number");
         if (x->rows == 0) return TENSILE_OK;
         NormArgs a{};
         a.rows = x->rows;
@@ -251,6 +251,7 @@ int tensile_layer_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_
         a.rstd = rstd;
         a.gamma = gamma; a.beta = beta;
         a.eps = static_cast<float>(eps);
+        if (eps > 0.0 && a.eps == 0.0f) a.eps = FLT_TRUE_MIN;             // (a constant row has no NaN then)
         a.cap = largest_code(x->type);
         return launch_norm(ops, static_cast<hipStream_t>(hip_stream), a, x->type, param_type);
     });

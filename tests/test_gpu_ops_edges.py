@@ -74,6 +74,23 @@ def test_linear_grad_of_every_nan(ops, dtype, M, N, K):
         assert bool((dw[4:] == (2.0 if affine else 1.0) * M).all()) and bool((db[4:] == M).all())
 
 
+# ------------------------------------------------------------------ layer norm
+
+def test_layer_norm_with_an_eps_at_the_ends_of_its_range(ops):
+    x = torch.stack([torch.ones(64, device="cuda"), torch.arange(64, device="cuda") * 1.0])
+    g, b, y, rstd = torch.ones(64, device="cuda"), torch.full((64,), 0.25, device="cuda"), torch.empty_like(x), torch.empty(2, device="cuda")
+    for eps in (1e39, 1e300, float("inf"), -1e-60):
+        with pytest.raises(P.TensileError) as e:
+            P.tensile_layer_norm(ops, x, g, b, y, eps=eps, rstd=rstd)
+        assert e.value.code == P.binding.TENSILE_E_INVAL and "eps" in str(e.value)
+    for eps in (1e-50, 1e-42, 1e-30):                 # a constant row: (x - mean) * rstd = 0 for any eps above 0
+        P.tensile_layer_norm(ops, x, g, b, y, eps=eps, rstd=rstd)
+        assert bool((y[0] == 0.25).all()) and bool(rstd.isfinite().all())
+        near(y[1:], plain.layer_norm(host(x)[1:], 1.0, 0.25, eps)[0], 64 * 2.0 ** -24 * 4, "y")
+    P.tensile_layer_norm(ops, x, g, b, y, eps=3e38, rstd=rstd)
+    near(rstd, np.full(2, 3e38 ** -0.5), 4 * 2.0 ** -24 * 3e38 ** -0.5, "rstd")
+
+
 # ------------------------------------------------------------------ gelu
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -55,6 +55,16 @@ def test_linear_grad_of_far_apart_rows(ops, dtype, M, far):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(65, 1, 1), (33, 1, 64), (96, 6, 2000), (300, 7, 15), (1000, 3, 300), (2049, 200, 9), (4097, 5, 130), (20_000, 2, 700)])
+def test_linear_grad_of_few_columns(ops, dtype, M, N, K):
+    """Fewer columns than a load takes (a classifier of two classes, a regression's one output): many steps, a ragged last one, up to 8 parts and more."""
+    say(f"linear grad of few columns {dtype} {M}x{N}x{K}")
+    check_grad(ops, dtype, "f32", M, N, K)
+    check_grad(ops, dtype, dtype, M, N, K, affine="f32", bias=False)
+    check_grad(ops, dtype, "f32", M, N, K, affine=dtype, skew=1)
+
+
 @pytest.mark.parametrize("M,N,K", [(70, 140, 140), (33, 5, 40), (64, 2048, 2304), (4100, 130, 200)])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_linear_grad_of_every_nan(ops, dtype, M, N, K):

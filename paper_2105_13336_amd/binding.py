@@ -341,7 +341,7 @@ def tensile_greedy_plan(h: TasHandle, budget_bytes: int = 0, max_iters: int = 0,
 # ---------------------------------------------------------------- activations in 8 bits
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # TENSILE_F32, TENSILE_BF16, TENSILE_F16
-_I8, _U8 = torch.int8, torch.uint8
+_I8, _U8, _F32 = torch.int8, torch.uint8, torch.float32
 GROUP = 32                                                         # columns that share a scale
 
 
@@ -377,27 +377,8 @@ class Checkpoint:
     __slots__ = ("_q", "_scale", "_q_at", "_scale_at", "_device", "_st")
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor):
+        """What a call is told of the two tensors; done again when they are found elsewhere."""
         self._q, self._scale = q, scale
-        self._describe()
-
-    @property
-    def q(self) -> torch.Tensor:
-        return self._q
-
-    @q.setter
-    def q(self, q: torch.Tensor) -> None:
-        self._q, self._q_at = q, None
-
-    @property
-    def scale(self) -> torch.Tensor:
-        return self._scale
-
-    @scale.setter
-    def scale(self, scale: torch.Tensor) -> None:
-        self._scale, self._scale_at = scale, None
-
-    def _describe(self) -> None:
-        q, scale = self._q, self._scale
         q_shape, s_shape = q.shape, scale.shape
         self._device = q.get_device()                                    # -1: not on a GPU
         if q.dtype is not _I8 or scale.dtype is not _U8 or len(q_shape) != 2 or len(s_shape) != 2 or self._device < 0 or scale.get_device() != self._device:
@@ -421,6 +402,22 @@ class Checkpoint:
         self._q_at, self._scale_at = q.data_ptr(), scale.data_ptr()
         self._st = _Ckpt(self._q_at, self._scale_at, rows, cols, ld_q, ld_s)
 
+    @property
+    def q(self) -> torch.Tensor:
+        return self._q
+
+    @q.setter
+    def q(self, q: torch.Tensor) -> None:
+        self._q, self._q_at = q, None
+
+    @property
+    def scale(self) -> torch.Tensor:
+        return self._scale
+
+    @scale.setter
+    def scale(self, scale: torch.Tensor) -> None:
+        self._scale, self._scale_at = scale, None
+
     @classmethod
     def empty(cls, rows: int, cols: int, device="cuda") -> "Checkpoint":
         """Room for rows x cols values; rows start at multiples of 16 bytes."""
@@ -434,7 +431,7 @@ class Checkpoint:
     @property
     def nbytes(self) -> int:
         if self._q.data_ptr() != self._q_at or self._scale.data_ptr() != self._scale_at:
-            self._describe()
+            self.__init__(self._q, self._scale)
         return self._st.rows * (self._st.ld_q + self._st.ld_scale)
 
 
@@ -470,7 +467,7 @@ def _ck(device: int, c: Optional[Checkpoint]):
     if c is None:
         return None
     if c._q.data_ptr() != c._q_at or c._scale.data_ptr() != c._scale_at:
-        c._describe()
+        c.__init__(c._q, c._scale)
     if c._device != device:
         raise TensileError(TENSILE_E_INVAL, f"checkpoint: it is on device {c._device}, the handle belongs to device {device}")
     return c._st
@@ -482,15 +479,14 @@ def _missing(**args) -> None:
             raise TensileError(TENSILE_E_INVAL, f"{name}: is None")
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the current stream without a Stream object (2.8 us)
+# the current stream, without a Stream object where that is possible (2.8 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _stream_ptr(stream, ops: OpsHandle) -> int:
-    if stream is not None:
-        if getattr(stream, "device_index", ops.device) != ops.device:
-            raise TensileError(TENSILE_E_INVAL, f"stream: it is of device {stream.device_index}, the handle belongs to device {ops.device}")
-        return stream.cuda_stream
-    return _raw_stream(ops.device) if _raw_stream else torch.cuda.current_stream(ops.device).cuda_stream
+    if getattr(stream, "device_index", ops.device) != ops.device:
+        raise TensileError(TENSILE_E_INVAL, f"stream: it is of device {stream.device_index}, the handle belongs to device {ops.device}")
+    return stream.cuda_stream
 
 
 def tensile_ops_create() -> OpsHandle:
@@ -507,13 +503,17 @@ def tensile_ops_free(ops: OpsHandle) -> None:
 def tensile_ckpt_pack(ops: OpsHandle, x: torch.Tensor, c: Checkpoint, stream=None) -> None:
     """c = x in 8 bits"""
     d = ops.device
-    _check(_lib.tensile_ckpt_pack(ops.ptr, _mat(d, x, "x"), _ck(d, c), _stream_ptr(stream, ops)))
+    rc = _lib.tensile_ckpt_pack(ops._ptr or ops.ptr, _mat(d, x, "x"), _ck(d, c), _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
 
 
 def tensile_ckpt_unpack(ops: OpsHandle, c: Checkpoint, y: torch.Tensor, stream=None) -> None:
     """y = the values of c"""
     d = ops.device
-    _check(_lib.tensile_ckpt_unpack(ops.ptr, _ck(d, c), _mat(d, y, "y"), _stream_ptr(stream, ops)))
+    rc = _lib.tensile_ckpt_unpack(ops._ptr or ops.ptr, _ck(d, c), _mat(d, y, "y"), _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
 
 
 def tensile_layer_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, y: torch.Tensor, eps: float = 1e-5,
@@ -524,9 +524,11 @@ def tensile_layer_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, bet
         _missing(x=x, gamma=gamma)
     d = ops.device
     m = _mat(d, x, "x")
-    _check(_lib.tensile_layer_norm(ops.ptr, m, _mat(d, residual, "residual"), _vec(d, gamma, gamma.dtype, m.cols, "gamma"),
-                                   _vec(d, beta, gamma.dtype, m.cols, "beta"), _TYPES.get(gamma.dtype, -1), eps, _mat(d, y, "y"), _mat(d, total, "total"),
-                                   _ck(d, xhat), _vec(d, rstd, torch.float32, m.rows, "rstd"), _stream_ptr(stream, ops)))
+    rc = _lib.tensile_layer_norm(ops._ptr or ops.ptr, m, _mat(d, residual, "residual"), _vec(d, gamma, gamma.dtype, m.cols, "gamma"),
+                                 _vec(d, beta, gamma.dtype, m.cols, "beta"), _TYPES.get(gamma.dtype, -1), eps, _mat(d, y, "y"), _mat(d, total, "total"),
+                                 _ck(d, xhat), _vec(d, rstd, _F32, m.rows, "rstd"), _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
 
 
 def tensile_layer_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoint, rstd: torch.Tensor, gamma: torch.Tensor, dx: torch.Tensor,
@@ -537,23 +539,29 @@ def tensile_layer_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoi
         _missing(dy=dy, gamma=gamma)
     d = ops.device
     m = _mat(d, dy, "dy")
-    _check(_lib.tensile_layer_norm_backward(ops.ptr, m, _ck(d, xhat), _vec(d, rstd, torch.float32, m.rows, "rstd"),
-                                            _vec(d, gamma, gamma.dtype, m.cols, "gamma"), _TYPES.get(gamma.dtype, -1), _mat(d, dresidual, "dresidual"),
-                                            _mat(d, dx, "dx"), _vec(d, dgamma, gamma.dtype, m.cols, "dgamma"),
-                                            _vec(d, dbeta, gamma.dtype, m.cols, "dbeta"), _stream_ptr(stream, ops)))
+    rc = _lib.tensile_layer_norm_backward(ops._ptr or ops.ptr, m, _ck(d, xhat), _vec(d, rstd, _F32, m.rows, "rstd"),
+                                          _vec(d, gamma, gamma.dtype, m.cols, "gamma"), _TYPES.get(gamma.dtype, -1), _mat(d, dresidual, "dresidual"),
+                                          _mat(d, dx, "dx"), _vec(d, dgamma, gamma.dtype, m.cols, "dgamma"),
+                                          _vec(d, dbeta, gamma.dtype, m.cols, "dbeta"), _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
 
 
 def tensile_gelu(ops: OpsHandle, x: torch.Tensor, y: torch.Tensor, ckpt: Optional[Checkpoint] = None, tanh: bool = False, stream=None) -> None:
     """y = gelu(x); ckpt: x in 8 bits"""
     d = ops.device
-    _check(_lib.tensile_gelu(ops.ptr, _mat(d, x, "x"), _mat(d, y, "y"), _ck(d, ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
+    rc = _lib.tensile_gelu(ops._ptr or ops.ptr, _mat(d, x, "x"), _mat(d, y, "y"), _ck(d, ckpt), 1 if tanh else 0, _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
 
 
 def tensile_gelu_backward(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dx: torch.Tensor, y_ckpt: Optional[Checkpoint] = None,
                           tanh: bool = False, stream=None) -> None:
     """dx = dy * gelu'(x) at the x that ckpt holds; y_ckpt: gelu(x) in 8 bits, for the next layer's weight gradient"""
     d = ops.device
-    _check(_lib.tensile_gelu_backward(ops.ptr, _mat(d, dy, "dy"), _ck(d, ckpt), _mat(d, dx, "dx"), _ck(d, y_ckpt), 1 if tanh else 0, _stream_ptr(stream, ops)))
+    rc = _lib.tensile_gelu_backward(ops._ptr or ops.ptr, _mat(d, dy, "dy"), _ck(d, ckpt), _mat(d, dx, "dx"), _ck(d, y_ckpt), 1 if tanh else 0, _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
 
 
 def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: torch.Tensor, dbias: Optional[torch.Tensor] = None,
@@ -565,5 +573,7 @@ def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: 
     m, c = _mat(d, dy, "dy"), _ck(d, ckpt)
     K = c.cols
     param = None if gamma is None else gamma.dtype
-    _check(_lib.tensile_linear_grad(ops.ptr, m, c, _vec(d, gamma, param, K, "gamma"), _vec(d, beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
-                                    _mat(d, dw, "dw"), _vec(d, dbias, dw.dtype, m.cols, "dbias"), _stream_ptr(stream, ops)))
+    rc = _lib.tensile_linear_grad(ops._ptr or ops.ptr, m, c, _vec(d, gamma, param, K, "gamma"), _vec(d, beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
+                                  _mat(d, dw, "dw"), _vec(d, dbias, dw.dtype, m.cols, "dbias"), _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)

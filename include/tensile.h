@@ -52,7 +52,12 @@
  * shape on that stream, or uses tensile_eval_plans_static.  The two tables
  * that are built on first use (tensile_score_recompute,
  * tensile_eval_plans_per_job) are built by whichever thread comes first while
- * the others wait.  A stream must outlive the calls enqueued on it.
+ * the others wait.  A stream must outlive the calls enqueued on it.  What a
+ * graph captured from a handle's calls uses is the scratch of the stream that
+ * was captured: graphs of one stream are launched in order with each other and
+ * with calls on that stream, and hipStreamPerThread, another stream in every
+ * host thread, is for one thread to a handle (the operators at the end of this
+ * file, with a handle of their own, have neither restriction).
  */
 #ifndef TENSILE_H
 #define TENSILE_H
@@ -355,10 +360,11 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
 /* ------------------------------------------------- activations in 8 bits */
 
 /* A plan makes a saved activation cheaper by moving it over the host link or by
- * recomputing it; the calls below are the third way: it stays, or travels, in
+ * recomputing it; the calls below are a third way: it stays, or travels, in
  * 8.25 bits instead of 16 or 32 (a quarter or half of size_bytes, of the
  * residence and of the transfer time x_i), and the backward pass reads it in
- * that form.  A checkpoint holds a matrix of rows (tokens) x cols (features):
+ * that form.  Which activations are kept so is the program's choice, made before the sequence is
+ * recorded: tensile_greedy_plan plans the sizes that it is given.  A checkpoint holds a matrix of rows (tokens) x cols (features):
  *   q[row*ld_q + col]              signed byte in [-127,127]
  *   scale[row*ld_scale + col/32]   code c: the 32 columns' scale is 2^(c-127)
  *   value = q * 2^(c-127);  c = 255: every value of the group is NaN;  c = 0: every value is 0
@@ -382,8 +388,8 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
  * depend on timing: the same call on the same inputs gives the same bits.
  *
  * tensile_layer_norm_backward and tensile_linear_grad use scratch memory that
- * the tensile_ops handle keeps per stream (of hipStreamPerThread: per host thread), under the rules given at
- * the top for a sequence's handle: any number of host threads may share one handle, and a call that needs
+ * the tensile_ops handle keeps per stream (of hipStreamPerThread: per host thread).  As with
+ * a sequence's handle, any number of host threads may share one, and a call that needs
  * more than any earlier call on its stream allocates it.  What is captured has scratch memory of its own for every
  * capture, allocated while the capture goes on and kept until the handle is freed: a graph may be launched on any stream, beside
  * other graphs and beside eager calls, also on the stream that was captured.  A program that captures again and

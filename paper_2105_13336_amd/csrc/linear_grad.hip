@@ -160,6 +160,8 @@ __device__ __forceinline__ Place place(const GradArgs &g) {
     w.n0 = static_cast<int>(n) * G::kN;
     w.k0 = static_cast<int>(k) * G::kK;
     w.m_begin = w.split * g.rows_per_split;
+    // (The end is chosen by a 32-bit comparison, not as the smaller of two 64-bit rows: for that, uniform as it is, hipcc of ROCm 7.2 has put a
+    // vector comparison in front of a scalar selection, which then goes by the carry of an addition: every part ran to the last row.)
     w.last = w.split == g.split - 1;
     w.m_end = w.last ? g.a.M : w.m_begin + g.rows_per_split;
     return w;
@@ -256,8 +258,8 @@ __device__ __forceinline__ void finish(const GradArgs &g, const Place &w, f32x16
 }
 
 // The product for any type; 32 and 16-bit gradients are three and two pieces, each a product of its own, and bound by those:
-// 6000 x 8192 x 8192 2140 us (f32) and 1600 us (f16), 1130 and 1000 TFLOP/s in pieces; 4096 x 4096 x 4096 438 and 323 us.  Beside the
-// products it is ordinary instructions that count: to a matrix instruction 5 (f32), of which 2.7 take dy apart.
+// 6000 x 8192 x 8192 2350 us (f32) and 1780 us (f16), 1030 and 900 TFLOP/s in pieces; 4096 x 4096 x 4096 391 and 307 us.  Beside the
+// products it is ordinary instructions that count: to a matrix instruction 5.5 on vectors (f32), of which 3.2 take dy apart.
 // kByElement: matrices with rows shorter than a load, or too far apart for 32-bit offsets.
 template <typename T, typename G, bool kByElement>
 __global__ __launch_bounds__(G::kThreads, 2) void linear_grad_kernel(GradArgs g) {

@@ -3,7 +3,7 @@
 // Bound by HBM: forward reads 2 and writes 3.03 bytes an element (bf16, with a checkpoint), backward reads 3.03 and writes 2; a residual
 // is 2 more.  Calls with a residual and a checkpoint: forward 16384 x 8192 183 us (5.2 TB/s), 65536 x 768 70 us (5.1), 8192 x 768
 // 11 us (4.4; two rows to a wavefront, so that starting and ending count); backward without one 16384 x 8192 143 us (4.7), 65536 x 768
-// 57 us (4.4), with one 16381 x 8192 169 + 5 us (5.6 TB/s), 8192 x 768 11 + 3 us, the second the sums over the workgroups.
+// 57 us (4.4), with one 16381 x 8192 169 + 5 us (5.6 TB/s), 8192 x 768 11 + 4 us, the second the sums over the workgroups.
 // A row is held in the registers of its team (16 lanes, a wavefront, or a workgroup) from the one load to the stores: the
 // mean, then the centred squares (no cancellation), then the outputs.  A team goes from row to row with the parameters in
 // registers and the next row's loads under way.  Backward keeps the two parameter gradients of its columns
@@ -169,7 +169,8 @@ __global__ __launch_bounds__((Team<kLanes, kWaves>::kBlock), 4) void norm_kernel
 }
 
 // Forward with rows too long for the registers (more than 16384 columns): a workgroup of 1024 threads passes over each row three times,
-// two of them from the caches.  4096 x 16384 in this form 140 us (3.4 TB/s of what has to move).
+// two of them from the caches (4096 x 20480 bf16, residual, checkpoint: 391 MB read from memory of 336 there, 194 us, 3.0 TB/s of what has to
+// move; three quarters of the wavefronts' time is waiting, for one pass's loads after the other).  4096 x 16384 in this form 140 us.
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     __shared__ float sums[2][16];
@@ -391,7 +392,8 @@ __global__ __launch_bounds__((BackTeam<kLanes, kWaves>::kBlock), 4) void norm_ba
     }
 }
 
-// Backward with rows too long for the registers, part one: dx.
+// Backward with rows too long for the registers, part one: dx.  4096 x 16384 f32 80 us the parameters' sums, 150 dx, 12 the join (604 MB have to
+// move: 123 us at the rate of a copy); bf16 4096 x 20480 70, 107 and 14.
 template <typename T, typename P>
 __global__ __launch_bounds__(1024) void norm_backward_long_kernel(NormArgs a) {
     __shared__ float sums[2][16];

@@ -834,7 +834,8 @@ int run(const ::tensile_ops *ops, hipStream_t s, const LinearArgs &a) {
     g.tiles_n = (a.N + G::kN - 1) / G::kN;
     g.tiles_k = (a.K + G::kK - 1) / G::kK;
     const int64_t tiles = static_cast<int64_t>(g.tiles_n) * g.tiles_k;
-    if (tiles > (1 << 24)) { set_error("linear_grad: dw has more than 2^24 tiles of %d x %d", G::kN, G::kK); return TENSILE_E_RANGE; }
+    // (2^32 threads to a launch)
+    if (tiles > UINT32_MAX / G::kThreads) { set_error("linear_grad: dw has more than 2^32 / %d tiles of %d x %d", G::kThreads, G::kN, G::kK); return TENSILE_E_RANGE; }
     // The rows are split where there are fewer tiles than places, but not below kPartRows each.  (8192 x 3072 x 768, 36 tiles: 4 parts
     // are no faster than 7: less to join, but 112 CUs idle.)
     const int64_t slots = G::kPerCu * static_cast<int64_t>(ops->num_cus);

@@ -465,11 +465,13 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a) {
 
 // dgamma, dbeta = the partial sums' columns added up: 32 columns and 32 strands to a workgroup, each strand every 32nd
 // partial sum, then the strands in order.  Latency: 2.5 to 4 us for 768 columns and 512 partial sums, 5 us for 8192 and 256.
+// first: of the 2 * cols columns that a launch takes (a launch has room for 2^32 threads, and wraps silently beyond).
+constexpr int64_t kGradientBlocks = 1 << 20;
 template <typename P>
-__global__ __launch_bounds__(1024) void norm_gradients_kernel(const float *part, int32_t n_part, int32_t cols, P *dgamma, P *dbeta) {
+__global__ __launch_bounds__(1024) void norm_gradients_kernel(const float *part, int32_t n_part, int32_t cols, P *dgamma, P *dbeta, int64_t first) {
     __shared__ float strand[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + x, width = 2 * static_cast<int64_t>(cols);
+    const int64_t c = first + static_cast<int64_t>(blockIdx.x) * 32 + x, width = 2 * static_cast<int64_t>(cols);
     float s = 0.0f;
     if (c < width) {
 #pragma unroll 8
@@ -581,9 +583,12 @@ int launch_norm_backward(const ::tensile_ops *ops, hipStream_t s, const NormArgs
             }
 #undef TS_NORM
         }
-        if (dgamma)
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_gradients_kernel<P>), dim3(static_cast<uint32_t>((2 * static_cast<int64_t>(a.cols) + 31) / 32)),
-                               dim3(1024), 0, s, a.part, static_cast<int32_t>(n_part), a.cols, static_cast<P *>(dgamma), static_cast<P *>(dbeta));
+        if (dgamma) {
+            const int64_t blocks = (2 * static_cast<int64_t>(a.cols) + 31) / 32;
+            for (int64_t first = 0; first < blocks; first += kGradientBlocks)
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_gradients_kernel<P>), dim3(grid_of(blocks - first, 1, kGradientBlocks)), dim3(1024), 0, s,
+                                   a.part, static_cast<int32_t>(n_part), a.cols, static_cast<P *>(dgamma), static_cast<P *>(dbeta), first * 32);
+        }
     });
     TS_HIP(hipGetLastError());
     return TENSILE_OK;

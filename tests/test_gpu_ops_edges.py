@@ -101,6 +101,31 @@ def test_layer_norm_with_an_eps_at_the_ends_of_its_range(ops):
     near(rstd, np.full(2, 3e38 ** -0.5), 4 * 2.0 ** -24 * 3e38 ** -0.5, "rstd")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [2 ** 25 - 24, 2 ** 25 + 40, 2 ** 26 + 40])
+def test_layer_norm_backward_of_the_longest_rows(ops, dtype, cols):
+    """Two launches' worth of parameter gradients and more.  Of two rows dbeta is one sum and dgamma one product and one sum, exact to their roundings."""
+    say(f"layer norm backward {dtype} 2x{cols}")
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    dy = torch.randn(2, cols, generator=gen, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    c, xh = P.Checkpoint.empty(2, cols), torch.randn(2, cols, generator=gen, device="cuda")
+    P.tensile_ckpt_pack(ops, xh, c)
+    P.tensile_ckpt_unpack(ops, c, xh)
+    g, rstd, dx = torch.ones(cols, device="cuda"), torch.ones(2, device="cuda"), torch.empty_like(dy)
+    dg, db = torch.full_like(g, 7.0), torch.full_like(g, 7.0)
+    P.tensile_layer_norm_backward(ops, dy, c, rstd, g, dx, dg, db)
+    dy = dy.double()
+    xh = xh.double()
+    u = 2.0 ** -24
+    assert bool(((db.double() - dy.sum(0)).abs() <= u * dy.sum(0).abs() * 1.01).all())
+    assert bool(((dg.double() - (dy * xh).sum(0)).abs() <= 3 * u * (dy * xh).abs().sum(0)).all())
+    want = dy - dy.mean(1, keepdim=True) - xh * (dy * xh).mean(1, keepdim=True)
+    # the two means: chains of cols / 1024 / 8 additions in a thread, 8 in a chunk, 6 across lanes, 16 across wavefronts
+    means = (cols / 8192 + 30) * u * (dy.abs().mean(1, keepdim=True) + xh.abs() * (dy * xh).abs().mean(1, keepdim=True))
+    rounding = plain.ROUND[dtype] + 4 * u
+    assert bool(((dx.double() - want).abs() <= rounding * want.abs() + means + 4 * u * (dy.abs() + xh.abs())).all())
+
+
 # ------------------------------------------------------------------ gelu
 
 @pytest.mark.parametrize("dtype", TYPES)

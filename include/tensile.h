@@ -387,7 +387,7 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
  * calls are asynchronous on hip_stream and never wait for the device.  Results do not
  * depend on timing: the same call on the same inputs gives the same bits.
  *
- * tensile_layer_norm_backward and tensile_linear_grad use scratch memory that
+ * tensile_layer_norm_backward, tensile_rms_norm_backward, tensile_gated_linear, its backward pass and tensile_linear_grad use scratch memory that
  * the tensile_ops handle keeps per stream (of hipStreamPerThread: per host thread).  As with
  * a sequence's handle, any number of host threads may share one, and a call that needs
  * more than any earlier call on its stream allocates it.  What is captured has scratch memory of its own for every
@@ -398,6 +398,7 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
 #define TENSILE_F32 0
 #define TENSILE_BF16 1
 #define TENSILE_F16 2
+
 
 typedef struct tensile_ops tensile_ops; /* opaque; owns the scratch memory of the calls below */
 
@@ -469,6 +470,53 @@ int tensile_gelu(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix
  *         from the forward pass), or NULL; may be c itself */
 int tensile_gelu_backward(tensile_ops *ops, const tensile_matrix *dy, const tensile_ckpt *c, const tensile_matrix *dx,
                           const tensile_ckpt *y_c, int32_t tanh_form, void *hip_stream);
+
+/* Root-mean-square norm of every row, after an optional residual sum:
+ *   s = x (+ residual);  rstd = 1/sqrt(mean of s^2 over the row + eps);  xhat = s*rstd;  y = xhat*gamma
+ * Arguments as in tensile_layer_norm.  (Squares are summed in 32 bits: a row whose sum of squares is no finite 32-bit number has
+ * rstd 0.  s is rounded for total only.) */
+int tensile_rms_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *residual, const void *gamma,
+                     int32_t param_type, double eps, const tensile_matrix *y, const tensile_matrix *total,
+                     const tensile_ckpt *xhat, float *rstd, void *hip_stream);
+
+/* Its backward pass, from the checkpoint of xhat and rstd:
+ *   t = dy*gamma;  dx = rstd*(t - xhat*mean(t*xhat)) (+ dresidual);  dgamma = sum over the rows of dy*xhat
+ * dx is the gradient of x, of residual and of what else entered s.
+ *   dresidual   like dy, what reaches s past the norm (the gradient of total), or NULL
+ *   dx          like dy; may be dy or dresidual itself
+ *   dgamma      [cols] of param_type, or NULL
+ * (The layer behind the norm, y W^T, has its weights' gradient from the same checkpoint: tensile_linear_grad with gamma and a beta of zeros.) */
+int tensile_rms_norm_backward(tensile_ops *ops, const tensile_matrix *dy, const tensile_ckpt *xhat, const float *rstd,
+                              const void *gamma, int32_t param_type, const tensile_matrix *dresidual,
+                              const tensile_matrix *dx, void *dgamma, void *hip_stream);
+
+#define TENSILE_SILU 0      /* act(g) = g/(1 + exp(-g))            */
+#define TENSILE_GELU 1      /* as tensile_gelu, tanh_form 0        */
+#define TENSILE_GELU_TANH 2 /* ... and 1                           */
+
+/* A gated linear layer: two projections of x: M x K, an activation and a product, of which only h is written in full:
+ *   g = x w_gate^T + b_gate;  u = x w_up^T + b_up;  h = act(g)*u
+ * Products are summed in 32 bits; nothing is rounded before h and the checkpoints are.
+ *   w_gate, w_up  F x K, of x's type; b_gate, b_up [F] of param_type (TENSILE_F32 or x's type), both or neither NULL
+ *   activation    TENSILE_SILU, TENSILE_GELU or TENSILE_GELU_TANH
+ *   h             M x F, of x's type
+ *   gate, up      checkpoints (M x F) of g and of u, what the backward pass reads; either may be NULL */
+int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *w_gate, const tensile_matrix *w_up,
+                         const void *b_gate, const void *b_up, int32_t param_type, int32_t activation,
+                         const tensile_matrix *h, const tensile_ckpt *gate, const tensile_ckpt *up, void *hip_stream);
+
+/* Its backward pass, from the checkpoints of g and u:
+ *   dgate = dh*u*act'(g);  dup = dh*act(g);  dx = dgate w_gate + dup w_up
+ * The weights' gradients are tensile_linear_grad of dgate and of dup with the checkpoint of x (of both in one call where they are
+ * the two halves of a matrix's columns); the biases' come with them.
+ *   dgate, dup    like dh; one of them may be dh itself
+ *   h_c           checkpoint of act(g)*u, for the weight gradient of the layer that read h, or NULL; may be gate or up itself
+ *   w_gate, w_up, dx  F x K, F x K and M x K, of dh's type; all or none NULL (dx is not wanted then).  dx is summed from dgate
+ *                 and dup as they were rounded: the gradient that belongs to those */
+int tensile_gated_linear_backward(tensile_ops *ops, const tensile_matrix *dh, const tensile_ckpt *gate, const tensile_ckpt *up,
+                                  int32_t activation, const tensile_matrix *dgate, const tensile_matrix *dup,
+                                  const tensile_ckpt *h_c, const tensile_matrix *w_gate, const tensile_matrix *w_up,
+                                  const tensile_matrix *dx, void *hip_stream);
 
 /* Gradients of a linear layer's parameters (y = x W^T + bias, W: N x K) from
  * dy: M x N and the checkpoint of its input:

@@ -7,3 +7,4 @@ from .binding import (DevicePlans, tensile_apply_intervals, TasHandle, TensileEr
                       tensile_tuning_reset)
 from .binding import (Checkpoint, OpsHandle, tensile_ckpt_pack, tensile_ckpt_unpack, tensile_gelu, tensile_gelu_backward,  # noqa: F401
                       tensile_layer_norm, tensile_layer_norm_backward, tensile_linear_grad, tensile_ops_create, tensile_ops_free)
+from .binding import (tensile_gated_linear, tensile_gated_linear_backward, tensile_rms_norm, tensile_rms_norm_backward)  # noqa: F401

@@ -25,7 +25,8 @@ EXPORTS = ["tensile_last_error", "tensile_version", "tensile_tas_load", "tensile
            "tensile_validate_plans",
            "tensile_greedy_plan", "tensile_eval_plans_static", "tensile_eval_score_plans", "tensile_tuning_set", "tensile_tuning_reset",
            "tensile_ops_create", "tensile_ops_free", "tensile_ckpt_pack", "tensile_ckpt_unpack", "tensile_layer_norm",
-           "tensile_layer_norm_backward", "tensile_gelu", "tensile_gelu_backward", "tensile_linear_grad"]
+           "tensile_layer_norm_backward", "tensile_gelu", "tensile_gelu_backward", "tensile_linear_grad", "tensile_rms_norm", "tensile_rms_norm_backward",
+           "tensile_gated_linear", "tensile_gated_linear_backward"]
 
 
 class TensileError(RuntimeError):
@@ -82,6 +83,10 @@ def _load():
     lib.tensile_gelu.argtypes = [p, m, m, c, i32, p]
     lib.tensile_gelu_backward.argtypes = [p, m, c, m, c, i32, p]
     lib.tensile_linear_grad.argtypes = [p, m, c, p, p, i32, m, p, p]
+    lib.tensile_rms_norm.argtypes = [p, m, m, p, i32, ctypes.c_double, m, m, c, p, p]
+    lib.tensile_rms_norm_backward.argtypes = [p, m, c, p, p, i32, m, m, p, p]
+    lib.tensile_gated_linear.argtypes = [p, m, m, m, p, p, i32, i32, m, c, c, p]
+    lib.tensile_gated_linear_backward.argtypes = [p, m, c, c, i32, m, m, c, m, m, m, p]
     return lib
 
 
@@ -343,6 +348,7 @@ def tensile_greedy_plan(h: TasHandle, budget_bytes: int = 0, max_iters: int = 0,
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # TENSILE_F32, TENSILE_BF16, TENSILE_F16
 _I8, _U8, _F32 = torch.int8, torch.uint8, torch.float32
 GROUP = 32                                                         # columns that share a scale
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}              # TENSILE_SILU, TENSILE_GELU, TENSILE_GELU_TANH
 
 
 class OpsHandle:
@@ -575,5 +581,69 @@ def tensile_linear_grad(ops: OpsHandle, dy: torch.Tensor, ckpt: Checkpoint, dw: 
     param = None if gamma is None else gamma.dtype
     rc = _lib.tensile_linear_grad(ops._ptr or ops.ptr, m, c, _vec(d, gamma, param, K, "gamma"), _vec(d, beta, param, K, "beta"), _TYPES.get(param, 0 if param is None else -1),
                                   _mat(d, dw, "dw"), _vec(d, dbias, dw.dtype, m.cols, "dbias"), _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
+
+
+def tensile_rms_norm(ops: OpsHandle, x: torch.Tensor, gamma: torch.Tensor, y: torch.Tensor, eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
+                     total: Optional[torch.Tensor] = None, xhat: Optional[Checkpoint] = None, rstd: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y = root-mean-square norm of x (+ residual), times gamma; total: the sum; xhat, rstd: what the backward pass reads"""
+    if x is None or gamma is None:
+        _missing(x=x, gamma=gamma)
+    d = ops.device
+    m = _mat(d, x, "x")
+    rc = _lib.tensile_rms_norm(ops._ptr or ops.ptr, m, _mat(d, residual, "residual"), _vec(d, gamma, gamma.dtype, m.cols, "gamma"),
+                               _TYPES.get(gamma.dtype, -1), eps, _mat(d, y, "y"), _mat(d, total, "total"), _ck(d, xhat), _vec(d, rstd, _F32, m.rows, "rstd"),
+                               _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
+
+
+def tensile_rms_norm_backward(ops: OpsHandle, dy: torch.Tensor, xhat: Checkpoint, rstd: torch.Tensor, gamma: torch.Tensor, dx: torch.Tensor,
+                              dgamma: Optional[torch.Tensor] = None, dresidual: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx = gradient through the norm (+ dresidual); dgamma: the weights' gradient"""
+    if dy is None or gamma is None:
+        _missing(dy=dy, gamma=gamma)
+    d = ops.device
+    m = _mat(d, dy, "dy")
+    rc = _lib.tensile_rms_norm_backward(ops._ptr or ops.ptr, m, _ck(d, xhat), _vec(d, rstd, _F32, m.rows, "rstd"), _vec(d, gamma, gamma.dtype, m.cols, "gamma"),
+                                        _TYPES.get(gamma.dtype, -1), _mat(d, dresidual, "dresidual"), _mat(d, dx, "dx"), _vec(d, dgamma, gamma.dtype, m.cols, "dgamma"),
+                                        _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
+
+
+def _activation(act: str) -> int:
+    code = _ACTIVATIONS.get(act)
+    if code is None:
+        raise TensileError(TENSILE_E_INVAL, f"act: {act!r} is not one of {', '.join(_ACTIVATIONS)}")
+    return code
+
+
+def tensile_gated_linear(ops: OpsHandle, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, h: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
+                         b_up: Optional[torch.Tensor] = None, act: str = "silu", gate: Optional[Checkpoint] = None, up: Optional[Checkpoint] = None,
+                         stream=None) -> None:
+    """h = act(x w_gate^T + b_gate) * (x w_up^T + b_up); act: "silu", "gelu" or "gelu_tanh"; gate, up: both projections in 8 bits"""
+    if w_gate is None:
+        _missing(w_gate=w_gate)
+    d = ops.device
+    w = _mat(d, w_gate, "w_gate")
+    param = None if b_gate is None else b_gate.dtype
+    rc = _lib.tensile_gated_linear(ops._ptr or ops.ptr, _mat(d, x, "x"), w, _mat(d, w_up, "w_up"), _vec(d, b_gate, param, w.rows, "b_gate"),
+                                   _vec(d, b_up, param, w.rows, "b_up"), _TYPES.get(param, 0 if param is None else -1), _activation(act), _mat(d, h, "h"),
+                                   _ck(d, gate), _ck(d, up), _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
+    if rc:
+        _check(rc)
+
+
+def tensile_gated_linear_backward(ops: OpsHandle, dh: torch.Tensor, gate: Checkpoint, up: Checkpoint, dgate: torch.Tensor, dup: torch.Tensor,
+                                  w_gate: Optional[torch.Tensor] = None, w_up: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                                  act: str = "silu", h_ckpt: Optional[Checkpoint] = None, stream=None) -> None:
+    """dgate, dup = gradients of the two projections at what gate and up hold; dx = dgate w_gate + dup w_up; h_ckpt: act(gate)*up in
+    8 bits, for the next layer's weight gradient"""
+    d = ops.device
+    rc = _lib.tensile_gated_linear_backward(ops._ptr or ops.ptr, _mat(d, dh, "dh"), _ck(d, gate), _ck(d, up), _activation(act), _mat(d, dgate, "dgate"),
+                                            _mat(d, dup, "dup"), _ck(d, h_ckpt), _mat(d, w_gate, "w_gate"), _mat(d, w_up, "w_up"), _mat(d, dx, "dx"),
+                                            _raw_stream(d) if stream is None else _stream_ptr(stream, ops))
     if rc:
         _check(rc)

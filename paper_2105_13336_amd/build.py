@@ -12,7 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libtensile.so")
 SOURCES = ["tas.hip", "eval.hip", "score.hip", "greedy.hip", "link.hip", "workspace.hip", "step.hip",
-           "ops.hip", "ckpt.hip", "norm.hip", "linear_grad.hip"]
+           "ops.hip", "ckpt.hip", "norm.hip", "rms.hip", "gated.hip", "gated_backward.hip", "linear_grad.hip"]
 
 
 def build_library(verbose: bool = False, extra_flags=()) -> str:

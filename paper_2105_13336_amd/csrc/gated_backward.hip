@@ -1,0 +1,84 @@
+// The gated layer, backward: the gradients of gate and up from the checkpoints, elementwise, and that of the layer's input, a product
+// over both (see gated_body.h).
+#include "each_device.h"
+#include "gated_body.h"
+
+namespace tensile {
+
+namespace {
+
+// dgate = dh*u*act'(g), dup = dh*act(g), and act(g)*u in 8 bits.
+template <typename T, bool kDense, typename A>
+__global__ __launch_bounds__(kEachThreads) void gated_grad_kernel(Walk w, Matrix dh, Ckpt gate, Ckpt up, Matrix dgate, Matrix dup, Ckpt h, uint32_t cap) {
+    using S = Slot<kDense>;
+    struct All {
+        Raw8<T> dh;
+        Held g, u;
+    };
+    walk<kDense>(
+        w, [&](const S &s) { return All{read_raw<T>(dh, s), read_ckpt(gate, s), read_ckpt(up, s)}; },
+        [&](const S &s, const All &raw) {
+            float d[8], g[8], u[8], v[8];
+            widen(raw.dh, d);
+            unpack8(raw.g.q, scale_of(raw.g.code), g);
+            unpack8(raw.u.q, scale_of(raw.u.code), u);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float value;
+                const float slope = A::template slope<kRoundsTo32<T>>(g[j], value);
+                v[j] = value * u[j];
+                g[j] = d[j] * u[j] * slope;
+                u[j] = d[j] * value;
+            }
+            write8<T>(dgate, s, g);
+            write8<T>(dup, s, u);
+            if (h.q) {
+                blank(v, s);           // (a NaN group's missing columns)
+                write_ckpt(h, s, v, cap);
+            }
+        });
+}
+
+template <typename T>
+int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
+    const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.q[1], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
+    const char *const what = "gated_linear_backward: partial sums";
+    const int64_t large = ((a.M + Large::kTok - 1) / Large::kTok) * ((a.R + Large::kP - 1) / Large::kP);
+    if (large >= ops->num_cus) return run_tiles<T, Large, false>(ops, s, a, far, 1, what);
+    const int64_t small = ((a.M + Small::kTok - 1) / Small::kTok) * ((a.R + Small::kP - 1) / Small::kP);
+    int64_t split = 2 * static_cast<int64_t>(ops->num_cus) / small;
+    const int64_t most = 2 * a.C * static_cast<int64_t>(sizeof(T)) / 1024;
+    if (split > most) split = most;
+    return run_tiles<T, Small, false>(ops, s, a, far, split, what);
+}
+
+}  // namespace
+
+int launch_gated_backward(const ::tensile_ops *ops, hipStream_t s, const GatedArgs &g, int type) {
+    bool dense, dense2;
+    uint32_t blocks;
+    const Walk w = make_walk({g.M, g.F, g.h, g.dgate, g.gate, g.up, 0}, &dense, &blocks);
+    make_walk({g.M, g.F, g.dup, {}, g.h_c, {}, 0}, &dense2, &blocks);
+    const int rc = by_type(type, dense && dense2, [&](auto t, auto d) {
+        using T = decltype(t);
+        constexpr bool kD = decltype(d)::value;
+        auto kernel = g.act == TENSILE_SILU ? gated_grad_kernel<T, kD, Silu> : g.act == TENSILE_GELU ? gated_grad_kernel<T, kD, Gelu<false>>
+                                                                                                      : gated_grad_kernel<T, kD, Gelu<true>>;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kEachThreads), 0, s, w, g.h, g.gate, g.up, g.dgate, g.dup, g.h_c, static_cast<uint32_t>(g.cap));
+    });
+    if (rc != TENSILE_OK || !g.x.p) return rc;
+    ProductArgs a{};
+    a.M = g.M;
+    a.C = g.F;
+    a.R = g.K;
+    a.q[0] = g.dgate;
+    a.q[1] = g.dup;
+    a.p[0] = g.w_gate;
+    a.p[1] = g.w_up;
+    a.out = g.x;
+    if (type == TENSILE_F32) return choose<float>(ops, s, a);
+    if (type == TENSILE_BF16) return choose<bf16_t>(ops, s, a);
+    return choose<f16_t>(ops, s, a);
+}
+
+}  // namespace tensile

@@ -1,0 +1,548 @@
+// The matrix products of the gated layer, forward (gated.hip) and backward (gated_backward.hip):
+//   g[m,f] = sum_k x[m,k]*Wg[f,k],  u[m,f] = sum_k x[m,k]*Wu[f,k]          (and from both act(g)*u, in the registers that hold them)
+//   dx[m,k] = sum_f dgate[m,f]*Wg[f,k] + sum_f dup[m,f]*Wu[f,k]
+//
+// On the matrix instructions with 32-bit sums: bf16 and f16 as they are, f32 on those for 32 bits (products and sums as in ordinary arithmetic).
+// A block of the result is 32 x 32; its rows are weights (f, or k backward) and its columns tokens, so that a lane holds 16 of the 32
+// features of one token: the group of 32 that shares a checkpoint's scale is a lane and the one 32 further, and gate and up of the
+// same f and m lie in the same register of two blocks.
+#pragma once
+
+#include "act_device.h"
+
+#include <type_traits>
+
+namespace tensile {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// (the LDS-direct loads below take their target from m0, which the compiler counts as its own and says so)
+#pragma clang diagnostic ignored "-Winline-asm"
+
+typedef const __attribute__((address_space(1))) char *global_bytes;
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr uint32_t kXcds = 8;
+
+template <typename T>
+constexpr int kPer16 = 16 / static_cast<int>(sizeof(T));   // elements of 16 bytes
+
+// c += the product of what 16 bytes of each lane hold: lane l has row (or column) l % 32 and of the summed index the values
+// (l / 32) * kPer16 onwards.
+__device__ __forceinline__ f32x16 multiply_add(bf16_t, u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 multiply_add(f16_t, u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 multiply_add(float, u32x4 a, u32x4 b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(as_f32(a[j]), as_f32(b[j]), c, 0, 0, 0);
+    return c;
+}
+
+// Up to 16 bytes of a row, `left` elements of which exist (0 or fewer: none); zeros behind them.
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const T *p, int64_t left) {
+    constexpr int kPer = kPer16<T>;
+    u32x4 r = {0, 0, 0, 0};
+    if (left >= kPer) {
+        __builtin_memcpy(&r, p, 16);
+    } else if (left > 0) {
+        T e[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            T z{};
+            if (j < left) z = p[j];
+            e[j] = z;
+        }
+        __builtin_memcpy(&r, e, 16);
+    }
+    return r;
+}
+
+// The row of a block that a lane's register r is.
+__device__ __forceinline__ int block_row(int lane, int r) { return 8 * (r / 4) + 4 * (lane >> 5) + r % 4; }
+
+// A lane's 16 of 32 consecutive rows become two runs of eight consecutive ones, v[0] from 8 * (lane / 32), v[1] 16 further: lanes
+// 32 apart exchange fours.
+__device__ __forceinline__ void by_eights(const f32x16 &acc, float (&v)[2][8]) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const auto s = __builtin_amdgcn_permlane32_swap(as_u32(acc[8 * q + j]), as_u32(acc[8 * q + 4 + j]), false, false);
+            v[q][j] = as_f32(s[0]);
+            v[q][4 + j] = as_f32(s[1]);
+        }
+}
+
+// ------------------------------------------------------------------ what the kernels are given
+
+struct ProductArgs {
+    int64_t M;                        // tokens
+    int32_t C;                        // length of a sum (backward: of each of the two)
+    int32_t R;                        // features of the result
+    Matrix q[2];                      // tokens x C: x, or dgate and dup
+    Matrix p[2];                      // Wg, Wu: R x C forward, C x R backward
+    // forward
+    const void *bias[2];
+    int32_t param_type, act, cap;
+    Matrix out;                       // h, or dx
+    Ckpt kept[2];
+    // how the work is cut: tiles of tokens and features, and the steps of a sum among `split` workgroups a tile
+    uint32_t tiles_m, tiles_r, split;
+    float *part;                      // split > 1: [tile][split][wavefront][block][register][lane]
+};
+
+template <typename T>
+__device__ __forceinline__ float param_at(int type, const void *p, int64_t at) {
+    return type == TENSILE_F32 ? static_cast<const float *>(p)[at] : to_f32(static_cast<const T *>(p)[at]);
+}
+
+// One token's 32 features from f0 on, gate and up: biases, checkpoints, activation, product.  The lanes l and l + 32 hold them and call this
+// together.  (Rows that do not exist hold copies of the last one: they change no group's largest magnitude.)
+template <typename T>
+__device__ __forceinline__ void finish_pair(const ProductArgs &a, const f32x16 &gate, const f32x16 &up, int64_t token, int f0) {
+    const int lane = threadIdx.x & 63;
+    float g[2][8], u[2][8];
+    by_eights(gate, g);
+    by_eights(up, u);
+    const int first = f0 + 8 * (lane >> 5);
+    if (a.bias[0]) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int f = first + 16 * q + j, at = f < a.R ? f : a.R - 1;
+                g[q][j] += param_at<T>(a.param_type, a.bias[0], at);
+                u[q][j] += param_at<T>(a.param_type, a.bias[1], at);
+            }
+    }
+    const bool there = token < a.M;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (!a.kept[k].q) continue;
+        const float(&v)[2][8] = k ? u : g;
+        uint32_t most = largest(v[0]);
+        const uint32_t other = largest(v[1]);
+        most = most > other ? most : other;
+        const auto s = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+        most = s[0] > s[1] ? s[0] : s[1];
+        uint32_t code = 0;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int f = first + 16 * q;
+            const u32x2 w = pack8_of(v[q], most, static_cast<uint32_t>(a.cap), code);
+            if (there && f < a.R) store_q(a.kept[k].q + token * a.kept[k].ld_q + f, w, a.R - f);
+        }
+        if (there && f0 < a.R && lane < 32) a.kept[k].scale[token * a.kept[k].ld_scale + f0 / kGroup] = static_cast<uint8_t>(code);
+    }
+    auto apply = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[q][j] = decltype(act)::template value<kRoundsTo32<T>>(g[q][j]) * u[q][j];
+    };
+    if (a.act == TENSILE_SILU) apply(Silu{});
+    else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
+    else apply(Gelu<true>{});
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int f = first + 16 * q;
+        if (there && f < a.R) store8(static_cast<T *>(a.out.p) + token * a.out.ld + f, g[q], a.R - f);
+    }
+}
+
+// One token's 32 features of dx.
+template <typename T>
+__device__ __forceinline__ void finish_block(const ProductArgs &a, const f32x16 &acc, int64_t token, int r0) {
+    const int lane = threadIdx.x & 63;
+    float v[2][8];
+    by_eights(acc, v);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int r = r0 + 8 * (lane >> 5) + 16 * q;
+        if (token < a.M && r < a.R) store8(static_cast<T *>(a.out.p) + token * a.out.ld + r, v[q], a.R - r);
+    }
+}
+
+// ------------------------------------------------------------------ tiles
+
+// A workgroup's tile: kWP x kWT wavefronts of 32 kPB rows of the weights x 32 kTB tokens each.  Forward the weights' rows are gate and up by turns, 32 each: the
+// tile is half as many features wide.
+template <int kPB_, int kTB_, int kWP_, int kWT_, int kPerCu_>
+struct Tile {
+    static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_;
+    static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
+    static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
+};
+
+constexpr int kRow = 64;              // bytes of a row that a step takes
+constexpr int kSlots = 4;             // steps in the LDS
+
+// Staged rows of 64 bytes: their four 16-byte chunks are stored in an order that depends on the row, so that 16 rows' chunks of the same number lie in
+// different banks.
+__device__ __forceinline__ int row_chunk(int row, int chunk) { return row * kRow + ((chunk ^ (row >> 2)) & 3) * 16; }
+
+// Where a workgroup works.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets a run of consecutive tiles, and consecutive
+// tiles lie in bands kBand tiles high, so that those under way on an XCD share rows of both operands.
+constexpr uint32_t kBand = 8;
+struct Place {
+    uint32_t tile, split;
+    int r0;
+    int64_t m0;
+};
+template <typename G, bool kForward>
+__device__ __forceinline__ Place place_of(const ProductArgs &a, uint32_t tile) {
+    const uint32_t per_band = kBand * a.tiles_r, band = tile / per_band, in_band = tile - band * per_band;
+    const uint32_t rest = a.tiles_m - band * kBand, high = rest < kBand ? rest : kBand, r = in_band / high;
+    Place w;
+    w.tile = tile;
+    w.split = 0;
+    w.m0 = static_cast<int64_t>(band * kBand + (in_band - r * high)) * G::kTok;
+    w.r0 = static_cast<int>(r) * (kForward ? G::kP / 2 : G::kP);
+    return w;
+}
+template <typename G, bool kForward>
+__device__ __forceinline__ Place place(const ProductArgs &a) {
+    const uint32_t total = gridDim.x, xcd = blockIdx.x % kXcds;
+    const uint32_t at = xcd * (total / kXcds) + (xcd < total % kXcds ? xcd : total % kXcds) + blockIdx.x / kXcds;
+    Place w = place_of<G, kForward>(a, at / a.split);
+    w.split = at - w.tile * a.split;
+    return w;
+}
+
+// Everything that becomes of a block's sums, or of a pair of them.
+template <typename T, typename G, bool kForward>
+__device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w, int wave, f32x16 (&acc)[G::kPB][G::kTB]) {
+    const int lane = threadIdx.x & 63;
+    const int wave_p = wave / G::kWT, wave_t = wave % G::kWT;
+#pragma unroll
+    for (int t = 0; t < G::kTB; ++t) {
+        const int64_t token = w.m0 + (wave_t * G::kTB + t) * 32 + (lane & 31);
+        if constexpr (kForward) {
+#pragma unroll
+            for (int b = 0; b < G::kPB; b += 2) finish_pair<T>(a, acc[b][t], acc[b + 1][t], token, w.r0 + (wave_p * G::kPB + b) / 2 * 32);
+        } else {
+#pragma unroll
+            for (int b = 0; b < G::kPB; ++b) finish_block<T>(a, acc[b][t], token, w.r0 + (wave_p * G::kPB + b) * 32);
+        }
+    }
+}
+
+// kFar: rows too far apart for 32-bit offsets; every step goes by way of registers.
+template <typename T, typename G, bool kForward, bool kFar>
+__global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void product_kernel(ProductArgs a) {
+    constexpr int kPB = G::kPB, kTB = G::kTB, kPer = kPer16<T>, kStep = 4 * kPer;      // elements of a sum in a step
+    constexpr int kSlotP = G::kP * kRow, kSlot = kSlotP + G::kTok * kRow;
+    constexpr int kLoadsP = G::kP / 16 / G::kWaves, kLoadsQ = G::kTok / 16 / G::kWaves; // a wave's, of 1024 bytes each
+    static_assert(kLoadsP * G::kWaves * 16 == G::kP && kLoadsQ * G::kWaves * 16 == G::kTok, "");
+    constexpr int kLoads = kLoadsP + kLoadsQ;
+    constexpr int kRowP = G::kP * static_cast<int>(sizeof(T));                         // backward: bytes of a staged row of the weights
+    __shared__ __attribute__((aligned(1024))) char lds[kSlots * kSlot];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave_p = wave / G::kWT, wave_t = wave % G::kWT;
+    const Place w = place<G, kForward>(a);
+
+    // What a lane brings of a step, 16 bytes a load.  Tokens, and forward the weights: 16 rows x 4 chunks to a load.  Backward the weights lie with the summed
+    // index outermost: whole rows of the tile's columns, staged as they are (16 bits: their 32-byte blocks in an order that depends on the row, so
+    // that the 4 rows x 2 blocks that half a wavefront reads at a time lie in different banks).  What does not exist is replaced by something that does.
+    struct Piece {
+        int64_t row;                  // of the matrix (backward, weights: of the step)
+        int col;                      // element
+    };
+    auto row_of = [&](int i) __attribute__((always_inline)) { return (wave * kLoadsP + i) * 16 + lane / 4; };       // of the tile's weights, forward
+    auto piece_p = [&](int i) __attribute__((always_inline)) -> Piece {
+        if constexpr (kForward) {
+            const int row = row_of(i), f = w.r0 + row / 64 * 32 + row % 32;
+            return {f < a.R ? f : a.R - 1, ((lane & 3) ^ (row >> 2 & 3)) * kPer};
+        } else {
+            const int at = ((wave * kLoadsP + i) * 64 + lane) * 16, row = at / kRowP, in = at % kRowP;
+            int col = sizeof(T) == 2 ? ((in / 32) ^ (2 * (row & 3))) * 16 + in % 32 / 2 : in / 4;
+            col += w.r0;
+            return {row, col};
+        }
+    };
+    auto piece_q = [&](int i) __attribute__((always_inline)) -> Piece {
+        const int row = (wave * kLoadsQ + i) * 16 + lane / 4;
+        const int64_t m = w.m0 + row;
+        return {m < a.M ? m : a.M - 1, ((lane & 3) ^ (row >> 2 & 3)) * kPer};
+    };
+    auto matrix_of = [&](int i) __attribute__((always_inline)) { return kForward ? ((wave * kLoadsP + i) >> 1) & 1 : 0; };
+
+    f32x16 acc[kPB][kTB] = {};
+    u32x4 fp[2][kPB], fq[2][kTB];
+    auto read = [&](int e, int slot) __attribute__((always_inline)) {
+        const char *const from = lds + slot * kSlot;
+#pragma unroll
+        for (int b = 0; b < kPB; ++b) {
+            if constexpr (kForward) {
+                fp[e][b] = *reinterpret_cast<const u32x4 *>(from + row_chunk((wave_p * kPB + b) * 32 + (lane & 31), 2 * e + (lane >> 5)));
+            } else if constexpr (sizeof(T) == 2) {
+                // 16 lanes read four rows of 16 columns and each gets the four values of its column
+                const int group = lane >> 4, row = 16 * e + (group >> 1) * 8 + (lane & 15) / 4, block = (wave_p * kPB + b) * 2 + (group & 1);
+                const int at = slot * kSlot + row * kRowP + ((block ^ (2 * (row & 3))) * 32) + (lane & 3) * 8;
+                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lds + at));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lds + at + 4 * kRowP));
+                fp[e][b] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    fp[e][b][j] = *reinterpret_cast<const uint32_t *>(from + (8 * e + 4 * (lane >> 5) + j) * kRowP + ((wave_p * kPB + b) * 32 + (lane & 31)) * 4);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < kTB; ++t)
+            fq[e][t] = *reinterpret_cast<const u32x4 *>(from + kSlotP + row_chunk((wave_t * kTB + t) * 32 + (lane & 31), 2 * e + (lane >> 5)));
+    };
+    auto multiply = [&](int e) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < kPB; ++b)
+#pragma unroll
+            for (int t = 0; t < kTB; ++t) acc[b][t] = multiply_add(T{}, fp[e][b], fq[e][t], acc[b][t]);
+    };
+
+    // Whole steps.  Backward a load of columns reads what lies behind the row's last one, up to the end of the row's last chunk: not where that is behind
+    // the matrix.  Of those steps, 2 * n_whole backward (gate, then up), the split takes a part; the rest, by way of registers, its last one.
+    constexpr int kSums = kForward ? 1 : 2;
+    int n_whole = 0;
+    if constexpr (!kFar) {
+        if constexpr (kForward) {
+            n_whole = a.C / kStep;
+        } else {
+            const int64_t least = a.p[0].ld < a.p[1].ld ? a.p[0].ld : a.p[1].ld;
+            const int64_t behind = a.R % kPer == 0 ? 0 : (kPer - 1 + least - 1) / least;   // rows at the end that are not read whole
+            n_whole = a.C > behind ? static_cast<int>((a.C - behind) / kStep) : 0;
+        }
+    }
+    const int64_t n_steps = static_cast<int64_t>(kSums) * n_whole;
+    const int begin = static_cast<int>(n_steps * w.split / a.split), end = static_cast<int>(n_steps * (w.split + 1) / a.split);
+
+    if constexpr (!kFar) {
+        const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)lds));
+        // From memory to the LDS without a register in between, 16 bytes of each lane in the order of the lanes.  (By hand: of the builtin the compiler waits
+        // for every one under way before the next LDS read, whatever it reads.  They write no register; the waits are at the barriers below.)
+        auto bring_16 = [&](uint32_t to, global_bytes from, uint32_t off) __attribute__((always_inline)) {
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
+        };
+        uint32_t off_p[kLoadsP], off_q[kSums][kLoadsQ];
+        const char *base_p[2], *base_q[kSums];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            base_p[k] = static_cast<const char *>(a.p[k].p) + (kForward ? w.r0 * a.p[k].ld : static_cast<int64_t>(w.r0)) * static_cast<int64_t>(sizeof(T));
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) base_q[k] = static_cast<const char *>(a.q[k].p) + w.m0 * a.q[k].ld * static_cast<int64_t>(sizeof(T));
+#pragma unroll
+        for (int i = 0; i < kLoadsP; ++i) {
+            const Piece c = piece_p(i);
+            if constexpr (kForward) off_p[i] = static_cast<uint32_t>(((c.row - w.r0) * a.p[matrix_of(i)].ld + c.col) * static_cast<int64_t>(sizeof(T)));
+            else off_p[i] = static_cast<uint32_t>((c.col < a.R ? c.col - w.r0 : 0) * static_cast<int64_t>(sizeof(T)));
+        }
+#pragma unroll
+        for (int k = 0; k < kSums; ++k)
+#pragma unroll
+            for (int i = 0; i < kLoadsQ; ++i) {
+                const Piece c = piece_q(i);
+                off_q[k][i] = static_cast<uint32_t>(((c.row - w.m0) * a.q[k].ld + c.col) * static_cast<int64_t>(sizeof(T)));
+            }
+        auto bring = [&](int s, int slot) __attribute__((always_inline)) {
+            const bool second = !kForward && s >= n_whole;
+            const int64_t at = static_cast<int64_t>(second ? s - n_whole : s) * kStep;
+            const uint32_t to = lds_at + slot * kSlot;
+            if constexpr (kForward) {
+#pragma unroll
+                for (int i = 0; i < kLoadsP; ++i)
+                    bring_16(to + (wave * kLoadsP + i) * 1024, (global_bytes)(base_p[matrix_of(i)] + at * static_cast<int64_t>(sizeof(T))), off_p[i]);
+            } else {
+                const int64_t pitch = (second ? a.p[1].ld : a.p[0].ld) * static_cast<int64_t>(sizeof(T));
+                const char *const from = second ? base_p[1] : base_p[0];
+#pragma unroll
+                for (int i = 0; i < kLoadsP; ++i) {
+                    const uint32_t row = static_cast<uint32_t>(((wave * kLoadsP + i) * 64 + lane) * 16 / kRowP);
+                    bring_16(to + (wave * kLoadsP + i) * 1024, (global_bytes)(from + at * pitch), row * static_cast<uint32_t>(pitch) + off_p[i]);
+                }
+            }
+            const char *const from = (kForward || !second ? base_q[0] : base_q[kSums - 1]) + at * static_cast<int64_t>(sizeof(T));
+#pragma unroll
+            for (int i = 0; i < kLoadsQ; ++i)
+                bring_16(to + kSlotP + (wave * kLoadsQ + i) * 1024, (global_bytes)from, kForward || !second ? off_q[0][i] : off_q[kSums - 1][i]);
+        };
+        // Step s multiplies while steps s+1 to s+3 are on their way or there.  Behind its barrier every wave has the last fragments of step s in registers and
+        // its share of step s+1 in the LDS: step s+4 is sent for in its place.  At the barrier the newest two steps' loads may be under way.
+        auto step = [&](int s, int slot, auto steady) __attribute__((always_inline)) {
+            read(1, slot);
+            multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            read(0, (slot + 1) % kSlots);
+            if (decltype(steady)::value || s + kSlots < end) bring(s + kSlots, slot);
+            multiply(1);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (begin < end) {
+#pragma unroll
+            for (int s = 0; s < kSlots; ++s)
+                if (begin + s < end) bring(begin + s, s);
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            read(0, 0);
+            int s = begin;
+            for (; s + 2 * kSlots <= end; s += kSlots) {
+                step(s, 0, std::true_type{});
+                step(s + 1, 1, std::true_type{});
+                step(s + 2, 2, std::true_type{});
+                step(s + 3, 3, std::true_type{});
+            }
+            for (; s < end; s += kSlots) {
+                step(s, 0, std::false_type{});
+                if (s + 1 < end) step(s + 1, 1, std::false_type{});
+                if (s + 2 < end) step(s + 2, 2, std::false_type{});
+                if (s + 3 < end) step(s + 3, 3, std::false_type{});
+            }
+        }
+    }
+    // What is left of the sums, less than a step or the matrices' last rows (kFar: all of them, split by steps), by way of registers.
+    auto rest = [&](int k, int64_t c0) __attribute__((always_inline)) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kLoadsP; ++i) {
+            const Piece c = piece_p(i);
+            u32x4 v;
+            if constexpr (kForward) {
+                const Matrix &m = a.p[matrix_of(i)];
+                v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
+            } else {
+                const Matrix &m = a.p[k];
+                const int64_t row = c0 + c.row;
+                v = load_chunk(static_cast<const T *>(m.p) + row * m.ld + c.col, row < a.C ? a.R - c.col : 0);
+            }
+            *reinterpret_cast<u32x4 *>(lds + (wave * kLoadsP + i) * 1024 + lane * 16) = v;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoadsQ; ++i) {
+            const Piece c = piece_q(i);
+            const Matrix &m = a.q[k];
+            const u32x4 v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
+            *reinterpret_cast<u32x4 *>(lds + kSlotP + (wave * kLoadsQ + i) * 1024 + lane * 16) = v;
+        }
+        __syncthreads();
+        read(0, 0);
+        read(1, 0);
+        multiply(0);
+        multiply(1);
+    };
+    if constexpr (kFar) {
+        const int64_t per = (a.C + kStep - 1) / kStep, n = per * kSums;
+        for (int64_t s = n * w.split / a.split; s < n * (w.split + 1) / a.split; ++s) rest(s >= per, (s >= per ? s - per : s) * kStep);
+    } else if (w.split == a.split - 1) {
+        for (int k = 0; k < kSums; ++k)
+            for (int64_t c0 = static_cast<int64_t>(n_whole) * kStep; c0 < a.C; c0 += kStep) rest(k, c0);
+    }
+    if (a.split > 1) {
+        float *const out = a.part + ((static_cast<int64_t>(w.tile) * a.split + w.split) * G::kWaves + wave) * (kPB * kTB * 1024) + lane;
+#pragma unroll
+        for (int b = 0; b < kPB; ++b)
+#pragma unroll
+            for (int t = 0; t < kTB; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) out[((b * kTB + t) * 16 + r) * 64] = acc[b][t][r];
+        return;
+    }
+    finish_tile<T, G, kForward>(a, w, wave, acc);
+}
+
+// split > 1: the parts of a sum added up in a fixed order, then as above.  A wavefront takes a block of 32 x 32, forward a pair of them.
+template <typename T, typename G, bool kForward>
+__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a) {
+    constexpr int kOwn = kForward ? 2 : 1, kUnits = G::kPB / kOwn * G::kTB * G::kWaves;       // of a tile
+    const int lane = threadIdx.x & 63;
+    const uint32_t at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = at / kUnits;
+    if (tile >= a.tiles_m * a.tiles_r) return;
+    const int unit = static_cast<int>(at - tile * kUnits), wave = unit / (kUnits / G::kWaves), in = unit % (kUnits / G::kWaves);
+    const int b = in / G::kTB * kOwn, t = in % G::kTB;
+    const Place w = place_of<G, kForward>(a, tile);
+    const int64_t token = w.m0 + (wave % G::kWT * G::kTB + t) * 32 + (lane & 31);
+    f32x16 acc[kOwn] = {};
+    const float *from = a.part + (static_cast<int64_t>(tile) * a.split * G::kWaves + wave) * (G::kPB * G::kTB * 1024) + lane;
+    for (uint32_t s = 0; s < a.split; ++s, from += G::kWaves * G::kPB * G::kTB * 1024)
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[k][r] += from[(((b + k) * G::kTB + t) * 16 + r) * 64];
+    if constexpr (kForward) finish_pair<T>(a, acc[0], acc[1], token, w.r0 + (wave / G::kWT * G::kPB + b) / 2 * 32);
+    else finish_block<T>(a, acc[0], token, w.r0 + (wave / G::kWT * G::kPB + b) * 32);
+}
+
+// Launches a tile's kernels.  A launch takes kMost tiles each way at most (it has room for 2^32 threads, and wraps silently beyond).
+constexpr int64_t kMost = 1 << 11;
+template <typename T, typename G, bool kForward>
+int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split, const char *what) {
+    constexpr int64_t kWide = kForward ? G::kP / 2 : G::kP, kSize = sizeof(T);
+    const int64_t tiles_m = (whole.M + G::kTok - 1) / G::kTok, tiles_r = (whole.R + kWide - 1) / kWide;
+    const int64_t steps = (kForward ? 1 : 2) * ((static_cast<int64_t>(whole.C) + 4 * kPer16<T> - 1) / (4 * kPer16<T>));
+    if (split > steps) split = steps;
+    if (split < 1) split = 1;
+    std::unique_lock<std::mutex> lock;
+    float *part = nullptr;
+    if (split > 1) {                                                     // (where there are few tiles: one launch)
+        OpsScratch &scratch = ops_scratch(ops, s);
+        lock = std::unique_lock<std::mutex>(scratch.mu);
+        const int rc = scratch.provide(static_cast<size_t>(tiles_m * tiles_r * split) * G::kP * G::kTok, what);
+        if (rc != TENSILE_OK) return rc;
+        part = scratch.buf.p;
+    }
+    auto moved = [](Matrix m, int64_t rows, int64_t cols) {
+        return Matrix{m.p ? static_cast<char *>(m.p) + (rows * m.ld + cols) * kSize : nullptr, m.ld};
+    };
+    for (int64_t r = 0; r < tiles_r; r += kMost)
+        for (int64_t m = 0; m < tiles_m; m += kMost) {
+            ProductArgs a = whole;
+            const int64_t r0 = r * kWide, m0 = m * G::kTok;
+            a.tiles_r = static_cast<uint32_t>(tiles_r - r < kMost ? tiles_r - r : kMost);
+            a.tiles_m = static_cast<uint32_t>(tiles_m - m < kMost ? tiles_m - m : kMost);
+            a.split = static_cast<uint32_t>(split);
+            a.part = part;
+            a.M -= m0;
+            a.R -= static_cast<int32_t>(r0);
+            a.out = moved(a.out, m0, r0);
+            for (int k = 0; k < 2; ++k) {
+                a.q[k] = moved(a.q[k], m0, 0);
+                a.p[k] = kForward ? moved(a.p[k], r0, 0) : moved(a.p[k], 0, r0);
+                if (a.bias[k]) a.bias[k] = static_cast<const char *>(a.bias[k]) + r0 * (a.param_type == TENSILE_F32 ? 4 : 2);
+                if (a.kept[k].q) {
+                    a.kept[k].q += m0 * a.kept[k].ld_q + r0;
+                    a.kept[k].scale += m0 * a.kept[k].ld_scale + r0 / kGroup;
+                }
+            }
+            const dim3 grid(a.tiles_m * a.tiles_r * a.split), block(G::kThreads);
+            if (far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, true>), grid, block, 0, s, a);
+            else hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
+            TS_HIP(hipGetLastError());
+            if (split > 1) {
+                const uint32_t units = a.tiles_m * a.tiles_r * (G::kPB / (kForward ? 2 : 1) * G::kTB * G::kWaves);
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3((units + 3) / 4), dim3(256), 0, s, a);
+                TS_HIP(hipGetLastError());
+            }
+        }
+    return TENSILE_OK;
+}
+
+// Rows further apart than this are reached by 64-bit addresses only (256 of them, or 32 of a step, from a scalar one).
+constexpr int64_t kFarBytes = 1 << 23;
+inline bool is_far(const Matrix &m, int64_t size) { return m.ld * size >= kFarBytes; }
+
+using Large = Tile<4, 2, 2, 4, 1>;    // 256 x 256
+using Small = Tile<2, 2, 2, 2, 2>;    // 128 x 128
+
+}  // namespace
+
+}  // namespace tensile

@@ -1,5 +1,6 @@
 // Declarations shared by the operators on 8-bit checkpoints of activations (ops.hip: handle and entry points,
-// ckpt.hip: pack, unpack and GELU, norm.hip: layer norm, linear_grad.hip: the weight gradient).
+// ckpt.hip: pack, unpack and GELU, norm.hip: layer norm, rms.hip: root-mean-square norm, gated.hip and gated_backward.hip: the gated layer,
+// linear_grad.hip: the weight gradient).
 #pragma once
 
 #include "common.h"
@@ -61,7 +62,19 @@ struct NormArgs {
     const void *gamma, *beta;
     float eps;
     int32_t cap;
-    float *part;                      // backward: [workgroup][2][cols]
+    float *part;                      // backward: [workgroup][2][cols], of the root-mean-square norm [workgroup][cols]
+};
+
+// The gated layer; backward h is dh and x is dx (null: not wanted).
+struct GatedArgs {
+    int64_t M;
+    int32_t K, F;
+    Matrix x, w_gate, w_up, h;
+    const void *b_gate, *b_up;
+    int32_t param_type, act, cap;
+    Ckpt gate, up;
+    Matrix dgate, dup;
+    Ckpt h_c;
 };
 
 struct LinearArgs {
@@ -83,6 +96,10 @@ int launch_gelu(const tensile_ops *ops, hipStream_t s, const EachArgs &a, int ty
 int launch_gelu_backward(const tensile_ops *ops, hipStream_t s, const EachArgs &a, int type, bool tanh_form);
 int launch_norm(const tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type);
 int launch_norm_backward(const tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type, void *dgamma, void *dbeta);
+int launch_rms_norm(const tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type);
+int launch_rms_norm_backward(const tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type, void *dgamma);
+int launch_gated(const tensile_ops *ops, hipStream_t s, const GatedArgs &g, int type);
+int launch_gated_backward(const tensile_ops *ops, hipStream_t s, const GatedArgs &g, int type);
 int launch_linear_grad(const tensile_ops *ops, hipStream_t s, const LinearArgs &a, int type);
 
 }  // namespace tensile

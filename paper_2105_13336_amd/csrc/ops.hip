@@ -151,6 +151,19 @@ int check_param(const void *p, int param_type, int type, const char *who, const 
     return TENSILE_OK;
 }
 
+int check_eps(double eps, const char *who) {
+    return eps >= 0.0 && eps <= FLT_MAX ? TENSILE_OK : refuse(who, "eps", "is negative or not a finite 32-bit number");
+}
+float held_eps(double eps) {
+    const float e = static_cast<float>(eps);
+    return eps > 0.0 && e == 0.0f ? FLT_TRUE_MIN : e;                     // (a row of zeros, or a constant one, has no NaN then)
+}
+
+int check_activation(int32_t activation, const char *who) {
+    const bool known = activation == TENSILE_SILU || activation == TENSILE_GELU || activation == TENSILE_GELU_TANH;
+    return known ? TENSILE_OK : refuse(who, "activation", "is not one of TENSILE_SILU, TENSILE_GELU, TENSILE_GELU_TANH");
+}
+
 Matrix view(const tensile_matrix *m) { return m ? Matrix{m->data, m->ld} : Matrix{nullptr, 0}; }
 Ckpt view(const tensile_ckpt *c) { return c ? Ckpt{c->q, c->scale, c->ld_q, c->ld_scale} : Ckpt{nullptr, nullptr, 0, 0}; }
 
@@ -241,7 +254,7 @@ int tensile_layer_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_
         if (xhat) TS_TRY(check_ckpt(xhat, x->rows, x->cols, who, "xhat"));
         TS_TRY(check_param(gamma, param_type, x->type, who, "gamma"));
         TS_TRY(check_param(beta, param_type, x->type, who, "beta"));
-        if (!(eps >= 0.0 && eps <= FLT_MAX)) return refuse(who, "eps", "is negative or not a finite 32-bit number");
+        TS_TRY(check_eps(eps, who));
         if (x->rows == 0) return TENSILE_OK;
         NormArgs a{};
         a.rows = x->rows;
@@ -250,8 +263,7 @@ int tensile_layer_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_
         a.c = view(xhat);
         a.rstd = rstd;
         a.gamma = gamma; a.beta = beta;
-        a.eps = static_cast<float>(eps);
-        if (eps > 0.0 && a.eps == 0.0f) a.eps = FLT_TRUE_MIN;             // (a constant row has no NaN then)
+        a.eps = held_eps(eps);
         a.cap = largest_code(x->type);
         return launch_norm(ops, static_cast<hipStream_t>(hip_stream), a, x->type, param_type);
     });
@@ -283,6 +295,135 @@ int tensile_layer_norm_backward(tensile_ops *ops, const tensile_matrix *dy, cons
         a.rstd = const_cast<float *>(rstd);
         a.gamma = gamma;
         return launch_norm_backward(ops, static_cast<hipStream_t>(hip_stream), a, dy->type, param_type, dgamma, dbeta);
+    });
+}
+
+int tensile_rms_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *residual, const void *gamma,
+                     int32_t param_type, double eps, const tensile_matrix *y, const tensile_matrix *total,
+                     const tensile_ckpt *xhat, float *rstd, void *hip_stream) {
+    return guarded("rms_norm", [&]() -> int {
+        const char *who = "rms_norm";
+        TS_TRY(check_ops(ops, who));
+        TS_TRY(check_matrix(x, who, "x"));
+        if (residual) TS_TRY(check_like(residual, x, who, "residual"));
+        TS_TRY(check_like(y, x, who, "y"));
+        if (total) TS_TRY(check_like(total, x, who, "total"));
+        if (total && x->rows > 0 && total->data == y->data) return refuse(who, "total", "is y");
+        if (xhat) TS_TRY(check_ckpt(xhat, x->rows, x->cols, who, "xhat"));
+        TS_TRY(check_param(gamma, param_type, x->type, who, "gamma"));
+        TS_TRY(check_eps(eps, who));
+        if (x->rows == 0) return TENSILE_OK;
+        NormArgs a{};
+        a.rows = x->rows;
+        a.cols = static_cast<int32_t>(x->cols);
+        a.x = view(x); a.r = view(residual); a.y = view(y); a.t = view(total);
+        a.c = view(xhat);
+        a.rstd = rstd;
+        a.gamma = gamma;
+        a.eps = held_eps(eps);
+        a.cap = largest_code(x->type);
+        return launch_rms_norm(ops, static_cast<hipStream_t>(hip_stream), a, x->type, param_type);
+    });
+}
+
+int tensile_rms_norm_backward(tensile_ops *ops, const tensile_matrix *dy, const tensile_ckpt *xhat, const float *rstd,
+                              const void *gamma, int32_t param_type, const tensile_matrix *dresidual,
+                              const tensile_matrix *dx, void *dgamma, void *hip_stream) {
+    return guarded("rms_norm_backward", [&]() -> int {
+        const char *who = "rms_norm_backward";
+        TS_TRY(check_ops(ops, who));
+        TS_TRY(check_matrix(dy, who, "dy"));
+        TS_TRY(check_ckpt(xhat, dy->rows, dy->cols, who, "xhat"));
+        if (dy->rows > 0 && !rstd) return refuse(who, "rstd", "is NULL");
+        if (dresidual) TS_TRY(check_like(dresidual, dy, who, "dresidual"));
+        TS_TRY(check_like(dx, dy, who, "dx"));
+        TS_TRY(check_param(gamma, param_type, dy->type, who, "gamma"));
+        if (dgamma) TS_TRY(check_param(dgamma, param_type, dy->type, who, "dgamma"));
+        if (dy->rows == 0 && !dgamma) return TENSILE_OK;
+        NormArgs a{};
+        a.rows = dy->rows;
+        a.cols = static_cast<int32_t>(dy->cols);
+        a.x = view(dy); a.r = view(dresidual); a.y = view(dx);
+        a.c = view(xhat);
+        a.rstd = const_cast<float *>(rstd);
+        a.gamma = gamma;
+        return launch_rms_norm_backward(ops, static_cast<hipStream_t>(hip_stream), a, dy->type, param_type, dgamma);
+    });
+}
+
+int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *w_gate, const tensile_matrix *w_up,
+                         const void *b_gate, const void *b_up, int32_t param_type, int32_t activation,
+                         const tensile_matrix *h, const tensile_ckpt *gate, const tensile_ckpt *up, void *hip_stream) {
+    return guarded("gated_linear", [&]() -> int {
+        const char *who = "gated_linear";
+        TS_TRY(check_ops(ops, who));
+        TS_TRY(check_matrix(x, who, "x"));
+        TS_TRY(check_matrix(w_gate, who, "w_gate"));
+        TS_TRY(check_like(w_up, w_gate, who, "w_up"));
+        if (w_gate->type != x->type) return refuse(who, "w_gate", "is not of x's type");
+        if (w_gate->cols != x->cols) return refuse(who, "w_gate", "has not the columns of x");
+        if (w_gate->rows < 1) return refuse(who, "w_gate", "has no rows");
+        if (w_gate->rows > kMostCols) { set_error("gated_linear: w_gate has more than 2^30 rows"); return TENSILE_E_RANGE; }
+        TS_TRY(check_matrix(h, who, "h"));
+        if (h->rows != x->rows || h->cols != w_gate->rows || h->type != x->type) return refuse(who, "h", "is not (rows of x) x (rows of w_gate), or not of x's type");
+        if (!b_gate != !b_up) return refuse(who, "b_gate, b_up", "are given one without the other");
+        if (b_gate) {
+            TS_TRY(check_param(b_gate, param_type, x->type, who, "b_gate"));
+            TS_TRY(check_param(b_up, param_type, x->type, who, "b_up"));
+        }
+        TS_TRY(check_activation(activation, who));
+        if (gate) TS_TRY(check_ckpt(gate, h->rows, h->cols, who, "gate"));
+        if (up) TS_TRY(check_ckpt(up, h->rows, h->cols, who, "up"));
+        if (x->rows == 0) return TENSILE_OK;
+        GatedArgs a{};
+        a.M = x->rows;
+        a.K = static_cast<int32_t>(x->cols);
+        a.F = static_cast<int32_t>(w_gate->rows);
+        a.x = view(x); a.w_gate = view(w_gate); a.w_up = view(w_up); a.h = view(h);
+        a.b_gate = b_gate; a.b_up = b_up;
+        a.param_type = param_type;
+        a.act = activation;
+        a.cap = largest_code(x->type);
+        a.gate = view(gate); a.up = view(up);
+        return launch_gated(ops, static_cast<hipStream_t>(hip_stream), a, x->type);
+    });
+}
+
+int tensile_gated_linear_backward(tensile_ops *ops, const tensile_matrix *dh, const tensile_ckpt *gate, const tensile_ckpt *up,
+                                  int32_t activation, const tensile_matrix *dgate, const tensile_matrix *dup,
+                                  const tensile_ckpt *h_c, const tensile_matrix *w_gate, const tensile_matrix *w_up,
+                                  const tensile_matrix *dx, void *hip_stream) {
+    return guarded("gated_linear_backward", [&]() -> int {
+        const char *who = "gated_linear_backward";
+        TS_TRY(check_ops(ops, who));
+        TS_TRY(check_matrix(dh, who, "dh"));
+        TS_TRY(check_ckpt(gate, dh->rows, dh->cols, who, "gate"));
+        TS_TRY(check_ckpt(up, dh->rows, dh->cols, who, "up"));
+        TS_TRY(check_activation(activation, who));
+        TS_TRY(check_like(dgate, dh, who, "dgate"));
+        TS_TRY(check_like(dup, dh, who, "dup"));
+        if (dh->rows > 0 && dgate->data == dup->data) return refuse(who, "dup", "is dgate");
+        if (h_c) TS_TRY(check_ckpt(h_c, dh->rows, dh->cols, who, "h_c"));
+        if (!w_gate != !dx || !w_up != !dx) return refuse(who, "w_gate, w_up, dx", "are given one without the others");
+        if (dx) {
+            TS_TRY(check_matrix(w_gate, who, "w_gate"));
+            TS_TRY(check_like(w_up, w_gate, who, "w_up"));
+            if (w_gate->rows != dh->cols || w_gate->type != dh->type) return refuse(who, "w_gate", "has not a row for each column of dh, or is not of dh's type");
+            TS_TRY(check_matrix(dx, who, "dx"));
+            if (dx->rows != dh->rows || dx->cols != w_gate->cols || dx->type != dh->type) return refuse(who, "dx", "is not (rows of dh) x (columns of w_gate), or not of dh's type");
+        }
+        if (dh->rows == 0) return TENSILE_OK;
+        GatedArgs a{};
+        a.M = dh->rows;
+        a.F = static_cast<int32_t>(dh->cols);
+        a.h = view(dh); a.gate = view(gate); a.up = view(up); a.dgate = view(dgate); a.dup = view(dup); a.h_c = view(h_c);
+        a.act = activation;
+        a.cap = largest_code(dh->type);
+        if (dx) {
+            a.K = static_cast<int32_t>(dx->cols);
+            a.w_gate = view(w_gate); a.w_up = view(w_up); a.x = view(dx);
+        }
+        return launch_gated_backward(ops, static_cast<hipStream_t>(hip_stream), a, dh->type);
     });
 }
 

@@ -181,11 +181,8 @@ __device__ __forceinline__ uint32_t largest(const float (&f)[8]) {
     return a;
 }
 
-// The four lanes 4k .. 4k+3 hold a group's 32 values (zero where there are none) and all of them call this.
-__device__ __forceinline__ u32x2 pack8(const float (&f)[8], uint32_t cap, uint32_t &code) {
-    uint32_t a = largest(f);
-    a = quad_max<0xB1>(a);             // quad_perm [1,0,3,2]
-    a = quad_max<0x4E>(a);             // quad_perm [2,3,0,1]
+// Eight of a group's values; a: the largest magnitude of all 32.
+__device__ __forceinline__ u32x2 pack8_of(const float (&f)[8], uint32_t a, uint32_t cap, uint32_t &code) {
     // a = m * 2^E, 1 <= m < 2: the scale is 2^(E-6), or 2^(E-5) where m >= 127.5/64 (the quotient would round to 128)
     const uint32_t up = (a + 0x10000u) >> 23;
     uint32_t c = up > 7 ? up - 6 : 1;
@@ -214,6 +211,14 @@ __device__ __forceinline__ u32x2 pack8(const float (&f)[8], uint32_t cap, uint32
     }
     code = c;
     return w;
+}
+
+// The four lanes 4k .. 4k+3 hold a group's 32 values (zero where there are none) and all of them call this.
+__device__ __forceinline__ u32x2 pack8(const float (&f)[8], uint32_t cap, uint32_t &code) {
+    uint32_t a = largest(f);
+    a = quad_max<0xB1>(a);             // quad_perm [1,0,3,2]
+    a = quad_max<0x4E>(a);             // quad_perm [2,3,0,1]
+    return pack8_of(f, a, cap, code);
 }
 
 // ------------------------------------------------------------------ sums over lanes

@@ -4,8 +4,7 @@
 //
 // On the matrix instructions with 32-bit sums: bf16 and f16 as they are, f32 on those for 32 bits (products and sums as in ordinary arithmetic).
 // A block of the result is 32 x 32; its rows are weights (f, or k backward) and its columns tokens, so that a lane holds 16 of the 32
-// features of one token: the group of 32 that shares a checkpoint's scale is a lane and the one 32 further, and gate and up of the
-// same f and m lie in the same register of two blocks.
+// features of one token, and gate and up of the same f and m lie in the same register of two blocks.
 #pragma once
 
 #include "act_device.h"
@@ -67,22 +66,6 @@ __device__ __forceinline__ u32x4 load_chunk(const T *p, int64_t left) {
     return r;
 }
 
-// The row of a block that a lane's register r is.
-__device__ __forceinline__ int block_row(int lane, int r) { return 8 * (r / 4) + 4 * (lane >> 5) + r % 4; }
-
-// A lane's 16 of 32 consecutive rows become two runs of eight consecutive ones, v[0] from 8 * (lane / 32), v[1] 16 further: lanes
-// 32 apart exchange fours.
-__device__ __forceinline__ void by_eights(const f32x16 &acc, float (&v)[2][8]) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const auto s = __builtin_amdgcn_permlane32_swap(as_u32(acc[8 * q + j]), as_u32(acc[8 * q + 4 + j]), false, false);
-            v[q][j] = as_f32(s[0]);
-            v[q][4 + j] = as_f32(s[1]);
-        }
-}
-
 // ------------------------------------------------------------------ what the kernels are given
 
 struct ProductArgs {
@@ -106,70 +89,96 @@ __device__ __forceinline__ float param_at(int type, const void *p, int64_t at) {
     return type == TENSILE_F32 ? static_cast<const float *>(p)[at] : to_f32(static_cast<const T *>(p)[at]);
 }
 
-// One token's 32 features from f0 on, gate and up: biases, checkpoints, activation, product.  The lanes l and l + 32 hold them and call this
-// together.  (Rows that do not exist hold copies of the last one: they change no group's largest magnitude.)
-template <typename T>
-__device__ __forceinline__ void finish_pair(const ProductArgs &a, const f32x16 &gate, const f32x16 &up, int64_t token, int f0) {
-    const int lane = threadIdx.x & 63;
-    float g[2][8], u[2][8];
-    by_eights(gate, g);
-    by_eights(up, u);
-    const int first = f0 + 8 * (lane >> 5);
-    if (a.bias[0]) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int f = first + 16 * q + j, at = f < a.R ? f : a.R - 1;
-                g[q][j] += param_at<T>(a.param_type, a.bias[0], at);
-                u[q][j] += param_at<T>(a.param_type, a.bias[1], at);
-            }
-    }
-    const bool there = token < a.M;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        if (!a.kept[k].q) continue;
-        const float(&v)[2][8] = k ? u : g;
-        uint32_t most = largest(v[0]);
-        const uint32_t other = largest(v[1]);
-        most = most > other ? most : other;
-        const auto s = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-        most = s[0] > s[1] ? s[0] : s[1];
-        uint32_t code = 0;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int f = first + 16 * q;
-            const u32x2 w = pack8_of(v[q], most, static_cast<uint32_t>(a.cap), code);
-            if (there && f < a.R) store_q(a.kept[k].q + token * a.kept[k].ld_q + f, w, a.R - f);
-        }
-        if (there && f0 < a.R && lane < 32) a.kept[k].scale[token * a.kept[k].ld_scale + f0 / kGroup] = static_cast<uint8_t>(code);
-    }
-    auto apply = [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[q][j] = decltype(act)::template value<kRoundsTo32<T>>(g[q][j]) * u[q][j];
-    };
-    if (a.act == TENSILE_SILU) apply(Silu{});
-    else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
-    else apply(Gelu<true>{});
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        const int f = first + 16 * q;
-        if (there && f < a.R) store8(static_cast<T *>(a.out.p) + token * a.out.ld + f, g[q], a.R - f);
-    }
-}
+// What becomes of the sums of a wavefront's kPB blocks (32 rows each) of 32 tokens.  They go through the LDS, so that a lane has eight features of a token and a
+// store whole lines of memory, in a loop: in registers it takes a copy of all of this for every block, which the instruction cache does not hold
+// (8192 x 4096 x 10944 with checkpoints 1356 us, so LATER).
+template <int kPB_, bool kForward>
+struct Exchange {
+    static constexpr int kPB = kPB_, kWide = kForward ? kPB * 16 : kPB * 32;           // features
+    static constexpr int kPitch = kWide + 4;                                           // floats from a token to the next: 16 lanes' 16 bytes lie in different banks
+    static constexpr int kBytes = 32 * kPitch * 4 * (kForward ? 2 : 1);                // of a wavefront
+    static constexpr int kLanes = kWide / 8, kAtOnce = 64 / kLanes;                    // a token's lanes, tokens at once
 
-// One token's 32 features of dx.
-template <typename T>
-__device__ __forceinline__ void finish_block(const ProductArgs &a, const f32x16 &acc, int64_t token, int r0) {
-    const int lane = threadIdx.x & 63;
-    float v[2][8];
-    by_eights(acc, v);
+    // Block b of the blocks, as the matrix instructions leave it: a lane has rows 8q + 4 (lane / 32) .. + 3 of token lane % 32.
+    static __device__ __forceinline__ void put(float *region, int b, const f32x16 &acc) {
+        const int lane = threadIdx.x & 63, plane = kForward ? b & 1 : 0, at = (kForward ? b / 2 : b) * 32;
+        float *const to = region + plane * 32 * kPitch + (lane & 31) * kPitch + at + 4 * (lane >> 5);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        const int r = r0 + 8 * (lane >> 5) + 16 * q;
-        if (token < a.M && r < a.R) store8(static_cast<T *>(a.out.p) + token * a.out.ld + r, v[q], a.R - r);
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4 *>(to + 8 * q) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    }
+    static __device__ __forceinline__ void get(const float *region, int plane, int token, float (&v)[8]) {
+        const int lane = threadIdx.x & 63;
+        const float *const from = region + plane * 32 * kPitch + token * kPitch + lane % kLanes * 8;
+        const f32x4 lo = *reinterpret_cast<const f32x4 *>(from), hi = *reinterpret_cast<const f32x4 *>(from + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = lo[j];
+            v[4 + j] = hi[j];
+        }
+    }
+    // (a wavefront's LDS accesses are in order; this keeps the compiler from changing it)
+    static __device__ __forceinline__ void order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+};
+
+// Tokens first_token .. +31 and the wavefront's features from r0 on, times() of them: write(t) puts what belongs to the t-th 32 tokens into the region.
+template <typename T, int kPB, bool kForward, typename Write>
+__device__ __forceinline__ void finish(const ProductArgs &a, float *region, int64_t first_token, int r0, int times, Write write) {
+    using E = Exchange<kPB, kForward>;
+    const int lane = threadIdx.x & 63;
+    const int r = r0 + lane % E::kLanes * 8, left = a.R - r;
+    float bias[2][8] = {};
+    if constexpr (kForward) {
+        if (a.bias[0]) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < left) bias[k][j] = param_at<T>(a.param_type, a.bias[k], r + j);
+        }
+    }
+#pragma unroll 1
+    for (int t = 0; t < times; ++t) {
+        E::order();
+        write(t);
+        E::order();
+#pragma unroll 1
+        for (int in = lane / E::kLanes; in < 32; in += E::kAtOnce) {
+            const int64_t token = first_token + 32 * t + in;
+            const bool there = token < a.M && left > 0;
+            float v[8];
+            E::get(region, 0, in, v);
+            if constexpr (kForward) {
+                float u[8];
+                E::get(region, 1, in, u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] += bias[0][j];
+                    u[j] += bias[1][j];
+                }
+                // (Rows that do not exist hold copies of the last one, without its bias: they take no part.)
+                if (left < 8) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j >= left) v[j] = u[j] = 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (!a.kept[k].q) continue;
+                    uint32_t code;
+                    const u32x2 w = pack8(k ? u : v, static_cast<uint32_t>(a.cap), code);
+                    if (there) store_q(a.kept[k].q + token * a.kept[k].ld_q + r, w, left);
+                    if (there && (lane & 3) == 0) a.kept[k].scale[token * a.kept[k].ld_scale + r / kGroup] = static_cast<uint8_t>(code);
+                }
+                auto apply = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = decltype(act)::template value<kRoundsTo32<T>>(v[j]) * u[j];
+                };
+                if (a.act == TENSILE_SILU) apply(Silu{});
+                else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
+                else apply(Gelu<true>{});
+            }
+            if (there) store8(static_cast<T *>(a.out.p) + token * a.out.ld + r, v, left);
+        }
     }
 }
 
@@ -177,15 +186,14 @@ __device__ __forceinline__ void finish_block(const ProductArgs &a, const f32x16 
 
 // A workgroup's tile: kWP x kWT wavefronts of 32 kPB rows of the weights x 32 kTB tokens each.  Forward the weights' rows are gate and up by turns, 32 each: the
 // tile is half as many features wide.
-template <int kPB_, int kTB_, int kWP_, int kWT_, int kPerCu_>
+template <int kPB_, int kTB_, int kWP_, int kWT_, int kPerCu_, int kSlots_>
 struct Tile {
-    static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_;
+    static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_, kSlots = kSlots_;
     static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
     static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
 };
 
 constexpr int kRow = 64;              // bytes of a row that a step takes
-constexpr int kSlots = 4;             // steps in the LDS
 
 // Staged rows of 64 bytes: their four 16-byte chunks are stored in an order that depends on the row, so that 16 rows' chunks of the same number lie in
 // different banks.
@@ -219,34 +227,17 @@ __device__ __forceinline__ Place place(const ProductArgs &a) {
     return w;
 }
 
-// Everything that becomes of a block's sums, or of a pair of them.
-template <typename T, typename G, bool kForward>
-__device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w, int wave, f32x16 (&acc)[G::kPB][G::kTB]) {
-    const int lane = threadIdx.x & 63;
-    const int wave_p = wave / G::kWT, wave_t = wave % G::kWT;
-#pragma unroll
-    for (int t = 0; t < G::kTB; ++t) {
-        const int64_t token = w.m0 + (wave_t * G::kTB + t) * 32 + (lane & 31);
-        if constexpr (kForward) {
-#pragma unroll
-            for (int b = 0; b < G::kPB; b += 2) finish_pair<T>(a, acc[b][t], acc[b + 1][t], token, w.r0 + (wave_p * G::kPB + b) / 2 * 32);
-        } else {
-#pragma unroll
-            for (int b = 0; b < G::kPB; ++b) finish_block<T>(a, acc[b][t], token, w.r0 + (wave_p * G::kPB + b) * 32);
-        }
-    }
-}
-
 // kFar: rows too far apart for 32-bit offsets; every step goes by way of registers.
 template <typename T, typename G, bool kForward, bool kFar>
 __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void product_kernel(ProductArgs a) {
-    constexpr int kPB = G::kPB, kTB = G::kTB, kPer = kPer16<T>, kStep = 4 * kPer;      // elements of a sum in a step
+    constexpr int kPB = G::kPB, kTB = G::kTB, kPer = kPer16<T>, kStep = 4 * kPer, kSlots = G::kSlots;      // elements of a sum in a step; steps in the LDS
     constexpr int kSlotP = G::kP * kRow, kSlot = kSlotP + G::kTok * kRow;
     constexpr int kLoadsP = G::kP / 16 / G::kWaves, kLoadsQ = G::kTok / 16 / G::kWaves; // a wave's, of 1024 bytes each
     static_assert(kLoadsP * G::kWaves * 16 == G::kP && kLoadsQ * G::kWaves * 16 == G::kTok, "");
     constexpr int kLoads = kLoadsP + kLoadsQ;
     constexpr int kRowP = G::kP * static_cast<int>(sizeof(T));                         // backward: bytes of a staged row of the weights
-    __shared__ __attribute__((aligned(1024))) char lds[kSlots * kSlot];
+    constexpr int kExchange = Exchange<kPB, kForward>::kBytes * G::kWaves;
+    __shared__ __attribute__((aligned(1024))) char lds[kSlots * kSlot > kExchange ? kSlots * kSlot : kExchange];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wave_p = wave / G::kWT, wave_t = wave % G::kWT;
@@ -280,29 +271,50 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
 
     f32x16 acc[kPB][kTB] = {};
     u32x4 fp[2][kPB], fq[2][kTB];
+    // Where a lane's fragments lie: a few places of its own, all else is constant.  (A fragment's second half of a step is 2 chunks further, which the order of the
+    // chunks makes an exclusive or.  An LDS instruction reaches 64 KB from its register: there are places for the first slots and for the others.)
+    const int half = lane >> 5, in_row = row_chunk(lane & 31, half);
+    constexpr int kFirst = 65536 / kSlot < kSlots ? 65536 / kSlot : kSlots;
+    auto base_of = [&](int slot) { return slot < kFirst ? 0 : kFirst * kSlot; };
+    // backward, 16 bits: 16 lanes read four rows of 16 columns and each gets the four values of its column
+    const int t_row = (lane >> 5) * 8 + (lane & 15) / 4;
+    int p_at[2][2][kForward ? 1 : kPB], q_at[2][2];
+#pragma unroll
+    for (int far_slot = 0; far_slot < 2; ++far_slot)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int from = far_slot * kFirst * kSlot;
+            q_at[far_slot][e] = from + wave_t * kTB * 2048 + (in_row ^ (32 * e));
+            if constexpr (kForward) {
+                p_at[far_slot][e][0] = from + wave_p * kPB * 2048 + (in_row ^ (32 * e));
+            } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int b = 0; b < kPB; ++b)
+                    p_at[far_slot][e][b] = from + (t_row + 16 * e) * kRowP + ((((wave_p * kPB + b) * 2 + (lane >> 4 & 1)) ^ (2 * (t_row & 3))) * 32) + (lane & 3) * 8;
+            } else {
+#pragma unroll
+                for (int b = 0; b < kPB; ++b) p_at[far_slot][e][b] = from + (8 * e + 4 * half) * kRowP + ((wave_p * kPB + b) * 32 + (lane & 31)) * 4;
+            }
+        }
     auto read = [&](int e, int slot) __attribute__((always_inline)) {
-        const char *const from = lds + slot * kSlot;
+        const int far_slot = slot >= kFirst, rest = slot * kSlot - base_of(slot);
 #pragma unroll
         for (int b = 0; b < kPB; ++b) {
             if constexpr (kForward) {
-                fp[e][b] = *reinterpret_cast<const u32x4 *>(from + row_chunk((wave_p * kPB + b) * 32 + (lane & 31), 2 * e + (lane >> 5)));
+                fp[e][b] = *reinterpret_cast<const u32x4 *>(lds + p_at[far_slot][e][0] + (rest + b * 2048));
             } else if constexpr (sizeof(T) == 2) {
-                // 16 lanes read four rows of 16 columns and each gets the four values of its column
-                const int group = lane >> 4, row = 16 * e + (group >> 1) * 8 + (lane & 15) / 4, block = (wave_p * kPB + b) * 2 + (group & 1);
-                const int at = slot * kSlot + row * kRowP + ((block ^ (2 * (row & 3))) * 32) + (lane & 3) * 8;
                 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lds + at));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((lds_char *)lds + at + 4 * kRowP));
+                lds_char *const from = (lds_char *)lds + p_at[far_slot][e][b] + rest;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * kRowP));
                 fp[e][b] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    fp[e][b][j] = *reinterpret_cast<const uint32_t *>(from + (8 * e + 4 * (lane >> 5) + j) * kRowP + ((wave_p * kPB + b) * 32 + (lane & 31)) * 4);
+                for (int j = 0; j < 4; ++j) fp[e][b][j] = *reinterpret_cast<const uint32_t *>(lds + p_at[far_slot][e][b] + (rest + j * kRowP));
             }
         }
 #pragma unroll
-        for (int t = 0; t < kTB; ++t)
-            fq[e][t] = *reinterpret_cast<const u32x4 *>(from + kSlotP + row_chunk((wave_t * kTB + t) * 32 + (lane & 31), 2 * e + (lane >> 5)));
+        for (int t = 0; t < kTB; ++t) fq[e][t] = *reinterpret_cast<const u32x4 *>(lds + q_at[far_slot][e] + (rest + kSlotP + t * 2048));
     };
     auto multiply = [&](int e) __attribute__((always_inline)) {
 #pragma unroll
@@ -376,13 +388,13 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             for (int i = 0; i < kLoadsQ; ++i)
                 bring_16(to + kSlotP + (wave * kLoadsQ + i) * 1024, (global_bytes)from, kForward || !second ? off_q[0][i] : off_q[kSums - 1][i]);
         };
-        // Step s multiplies while steps s+1 to s+3 are on their way or there.  Behind its barrier every wave has the last fragments of step s in registers and
-        // its share of step s+1 in the LDS: step s+4 is sent for in its place.  At the barrier the newest two steps' loads may be under way.
+        // Step s multiplies while the kSlots - 1 steps behind it are on their way or there.  Behind its barrier every wave has the last fragments of step s in
+        // registers and its share of step s+1 in the LDS: step s + kSlots is sent for in its place.  At the barrier all but step s+1 may be under way.
         auto step = [&](int s, int slot, auto steady) __attribute__((always_inline)) {
             read(1, slot);
             multiply(0);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+            if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kSlots - 2) * kLoads) : "memory");
             else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             read(0, (slot + 1) % kSlots);
             if (decltype(steady)::value || s + kSlots < end) bring(s + kSlots, slot);
@@ -397,16 +409,13 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             read(0, 0);
             int s = begin;
             for (; s + 2 * kSlots <= end; s += kSlots) {
-                step(s, 0, std::true_type{});
-                step(s + 1, 1, std::true_type{});
-                step(s + 2, 2, std::true_type{});
-                step(s + 3, 3, std::true_type{});
+#pragma unroll
+                for (int k = 0; k < kSlots; ++k) step(s + k, k, std::true_type{});
             }
             for (; s < end; s += kSlots) {
-                step(s, 0, std::false_type{});
-                if (s + 1 < end) step(s + 1, 1, std::false_type{});
-                if (s + 2 < end) step(s + 2, 2, std::false_type{});
-                if (s + 3 < end) step(s + 3, 3, std::false_type{});
+#pragma unroll
+                for (int k = 0; k < kSlots; ++k)
+                    if (s + k < end) step(s + k, k, std::false_type{});
             }
         }
     }
@@ -457,29 +466,42 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
                 for (int r = 0; r < 16; ++r) out[((b * kTB + t) * 16 + r) * 64] = acc[b][t][r];
         return;
     }
-    finish_tile<T, G, kForward>(a, w, wave, acc);
+    __syncthreads();
+    using E = Exchange<kPB, kForward>;
+    float *const region = reinterpret_cast<float *>(lds + wave * E::kBytes);
+    finish<T, kPB, kForward>(a, region, w.m0 + wave_t * kTB * 32, w.r0 + wave_p * E::kWide, kTB, [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int tt = 0; tt < kTB; ++tt)
+            if (t == tt) {
+#pragma unroll
+                for (int b = 0; b < kPB; ++b) E::put(region, b, acc[b][tt]);
+            }
+    });
 }
 
-// split > 1: the parts of a sum added up in a fixed order, then as above.  A wavefront takes a block of 32 x 32, forward a pair of them.
+// split > 1: the parts of a sum added up in a fixed order, then as above.  A wavefront takes what one of the tile's had of 32 tokens.
 template <typename T, typename G, bool kForward>
 __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a) {
-    constexpr int kOwn = kForward ? 2 : 1, kUnits = G::kPB / kOwn * G::kTB * G::kWaves;       // of a tile
-    const int lane = threadIdx.x & 63;
-    const uint32_t at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = at / kUnits;
+    using E = Exchange<G::kPB, kForward>;
+    constexpr int kUnits = G::kTB * G::kWaves;                           // of a tile
+    __shared__ __attribute__((aligned(16))) char lds[4 * E::kBytes];
+    const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t at = blockIdx.x * 4 + own, tile = at / kUnits;
     if (tile >= a.tiles_m * a.tiles_r) return;
-    const int unit = static_cast<int>(at - tile * kUnits), wave = unit / (kUnits / G::kWaves), in = unit % (kUnits / G::kWaves);
-    const int b = in / G::kTB * kOwn, t = in % G::kTB;
+    const int unit = static_cast<int>(at - tile * kUnits), wave = unit / G::kTB, t = unit % G::kTB;
     const Place w = place_of<G, kForward>(a, tile);
-    const int64_t token = w.m0 + (wave % G::kWT * G::kTB + t) * 32 + (lane & 31);
-    f32x16 acc[kOwn] = {};
+    float *const region = reinterpret_cast<float *>(lds + own * E::kBytes);
+    f32x16 acc[G::kPB] = {};
     const float *from = a.part + (static_cast<int64_t>(tile) * a.split * G::kWaves + wave) * (G::kPB * G::kTB * 1024) + lane;
     for (uint32_t s = 0; s < a.split; ++s, from += G::kWaves * G::kPB * G::kTB * 1024)
 #pragma unroll
-        for (int k = 0; k < kOwn; ++k)
+        for (int b = 0; b < G::kPB; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[k][r] += from[(((b + k) * G::kTB + t) * 16 + r) * 64];
-    if constexpr (kForward) finish_pair<T>(a, acc[0], acc[1], token, w.r0 + (wave / G::kWT * G::kPB + b) / 2 * 32);
-    else finish_block<T>(a, acc[0], token, w.r0 + (wave / G::kWT * G::kPB + b) * 32);
+            for (int r = 0; r < 16; ++r) acc[b][r] += from[((b * G::kTB + t) * 16 + r) * 64];
+    finish<T, G::kPB, kForward>(a, region, w.m0 + (wave % G::kWT * G::kTB + t) * 32, w.r0 + wave / G::kWT * E::kWide, 1, [&](int) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < G::kPB; ++b) E::put(region, b, acc[b]);
+    });
 }
 
 // Launches a tile's kernels.  A launch takes kMost tiles each way at most (it has room for 2^32 threads, and wraps silently beyond).
@@ -528,7 +550,7 @@ int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole,
             else hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
             TS_HIP(hipGetLastError());
             if (split > 1) {
-                const uint32_t units = a.tiles_m * a.tiles_r * (G::kPB / (kForward ? 2 : 1) * G::kTB * G::kWaves);
+                const uint32_t units = a.tiles_m * a.tiles_r * (G::kTB * G::kWaves);
                 hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3((units + 3) / 4), dim3(256), 0, s, a);
                 TS_HIP(hipGetLastError());
             }
@@ -540,8 +562,8 @@ int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole,
 constexpr int64_t kFarBytes = 1 << 23;
 inline bool is_far(const Matrix &m, int64_t size) { return m.ld * size >= kFarBytes; }
 
-using Large = Tile<4, 2, 2, 4, 1>;    // 256 x 256
-using Small = Tile<2, 2, 2, 2, 2>;    // 128 x 128
+using Large = Tile<4, 2, 2, 2, 2, 3>;    // 256 x 128
+using Small = Tile<2, 2, 2, 2, 2, 4>;    // 128 x 128
 
 }  // namespace
 

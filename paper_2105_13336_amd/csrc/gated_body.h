@@ -186,18 +186,19 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
 
 // A workgroup's tile: kWP x kWT wavefronts of 32 kPB rows of the weights x 32 kTB tokens each.  Forward the weights' rows are gate and up by turns, 32 each: the
 // tile is half as many features wide.
-template <int kPB_, int kTB_, int kWP_, int kWT_, int kPerCu_, int kSlots_>
+template <int kPB_, int kTB_, int kWP_, int kWT_, int kPerCu_>
 struct Tile {
-    static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_, kSlots = kSlots_;
+    static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_;
     static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
     static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
 };
 
-constexpr int kRow = 64;              // bytes of a row that a step takes
+// A step takes kRow bytes of a row, a line of the caches (with half a line to a step the L2 is asked twice as often: it answers a line or half of one in the same
+// time); two steps are in the LDS, kParts fragments long each.
+constexpr int kRow = 128, kSlots = 2, kParts = kRow / 32;
 
-// Staged rows of 64 bytes: their four 16-byte chunks are stored in an order that depends on the row, so that 16 rows' chunks of the same number lie in
-// different banks.
-__device__ __forceinline__ int row_chunk(int row, int chunk) { return row * kRow + ((chunk ^ (row >> 2)) & 3) * 16; }
+// Of staged rows the 16-byte chunks are stored in an order that depends on the row, so that 16 rows' chunks of the same number lie in different banks.
+__device__ __forceinline__ int stored_chunk(int row, int chunk) { return chunk ^ (row >> 1 & 7); }
 
 // Where a workgroup works.  Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD gets a run of consecutive tiles, and consecutive
 // tiles lie in bands kBand tiles high, so that those under way on an XCD share rows of both operands.
@@ -230,11 +231,10 @@ __device__ __forceinline__ Place place(const ProductArgs &a) {
 // kFar: rows too far apart for 32-bit offsets; every step goes by way of registers.
 template <typename T, typename G, bool kForward, bool kFar>
 __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void product_kernel(ProductArgs a) {
-    constexpr int kPB = G::kPB, kTB = G::kTB, kPer = kPer16<T>, kStep = 4 * kPer, kSlots = G::kSlots;      // elements of a sum in a step; steps in the LDS
+    constexpr int kPB = G::kPB, kTB = G::kTB, kPer = kPer16<T>, kStep = kRow / static_cast<int>(sizeof(T));      // elements of a sum in a step
     constexpr int kSlotP = G::kP * kRow, kSlot = kSlotP + G::kTok * kRow;
-    constexpr int kLoadsP = G::kP / 16 / G::kWaves, kLoadsQ = G::kTok / 16 / G::kWaves; // a wave's, of 1024 bytes each
-    static_assert(kLoadsP * G::kWaves * 16 == G::kP && kLoadsQ * G::kWaves * 16 == G::kTok, "");
-    constexpr int kLoads = kLoadsP + kLoadsQ;
+    constexpr int kLoadsP = G::kP / 8 / G::kWaves, kLoadsQ = G::kTok / 8 / G::kWaves;   // a wave's, of 1024 bytes each
+    static_assert(kLoadsP * G::kWaves * 8 == G::kP && kLoadsQ * G::kWaves * 8 == G::kTok, "");
     constexpr int kRowP = G::kP * static_cast<int>(sizeof(T));                         // backward: bytes of a staged row of the weights
     constexpr int kExchange = Exchange<kPB, kForward>::kBytes * G::kWaves;
     __shared__ __attribute__((aligned(1024))) char lds[kSlots * kSlot > kExchange ? kSlots * kSlot : kExchange];
@@ -243,18 +243,18 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
     const int wave_p = wave / G::kWT, wave_t = wave % G::kWT;
     const Place w = place<G, kForward>(a);
 
-    // What a lane brings of a step, 16 bytes a load.  Tokens, and forward the weights: 16 rows x 4 chunks to a load.  Backward the weights lie with the summed
+    // What a lane brings of a step, 16 bytes a load.  Tokens, and forward the weights: 8 rows x 8 chunks to a load.  Backward the weights lie with the summed
     // index outermost: whole rows of the tile's columns, staged as they are (16 bits: their 32-byte blocks in an order that depends on the row, so
     // that the 4 rows x 2 blocks that half a wavefront reads at a time lie in different banks).  What does not exist is replaced by something that does.
     struct Piece {
         int64_t row;                  // of the matrix (backward, weights: of the step)
         int col;                      // element
     };
-    auto row_of = [&](int i) __attribute__((always_inline)) { return (wave * kLoadsP + i) * 16 + lane / 4; };       // of the tile's weights, forward
+    auto row_of = [&](int i) __attribute__((always_inline)) { return (wave * kLoadsP + i) * 8 + lane / 8; };       // of the tile's weights, forward
     auto piece_p = [&](int i) __attribute__((always_inline)) -> Piece {
         if constexpr (kForward) {
             const int row = row_of(i), f = w.r0 + row / 64 * 32 + row % 32;
-            return {f < a.R ? f : a.R - 1, ((lane & 3) ^ (row >> 2 & 3)) * kPer};
+            return {f < a.R ? f : a.R - 1, stored_chunk(row, lane & 7) * kPer};
         } else {
             const int at = ((wave * kLoadsP + i) * 64 + lane) * 16, row = at / kRowP, in = at % kRowP;
             int col = sizeof(T) == 2 ? ((in / 32) ^ (2 * (row & 3))) * 16 + in % 32 / 2 : in / 4;
@@ -263,64 +263,55 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
         }
     };
     auto piece_q = [&](int i) __attribute__((always_inline)) -> Piece {
-        const int row = (wave * kLoadsQ + i) * 16 + lane / 4;
+        const int row = (wave * kLoadsQ + i) * 8 + lane / 8;
         const int64_t m = w.m0 + row;
-        return {m < a.M ? m : a.M - 1, ((lane & 3) ^ (row >> 2 & 3)) * kPer};
+        return {m < a.M ? m : a.M - 1, stored_chunk(row, lane & 7) * kPer};
     };
-    auto matrix_of = [&](int i) __attribute__((always_inline)) { return kForward ? ((wave * kLoadsP + i) >> 1) & 1 : 0; };
+    auto matrix_of = [&](int i) __attribute__((always_inline)) { return kForward ? ((wave * kLoadsP + i) >> 2) & 1 : 0; };
 
     f32x16 acc[kPB][kTB] = {};
     u32x4 fp[2][kPB], fq[2][kTB];
-    // Where a lane's fragments lie: a few places of its own, all else is constant.  (A fragment's second half of a step is 2 chunks further, which the order of the
-    // chunks makes an exclusive or.  An LDS instruction reaches 64 KB from its register: there are places for the first slots and for the others.)
-    const int half = lane >> 5, in_row = row_chunk(lane & 31, half);
-    constexpr int kFirst = 65536 / kSlot < kSlots ? 65536 / kSlot : kSlots;
-    auto base_of = [&](int slot) { return slot < kFirst ? 0 : kFirst * kSlot; };
+    // Where a lane's fragments lie, part e of the step in the first slot.  (Two chunks on are an exclusive or, in the order of the chunks.)
+    const int half = lane >> 5, in_row = (lane & 31) * kRow + stored_chunk(lane & 31, half) * 16;
     // backward, 16 bits: 16 lanes read four rows of 16 columns and each gets the four values of its column
-    const int t_row = (lane >> 5) * 8 + (lane & 15) / 4;
-    int p_at[2][2][kForward ? 1 : kPB], q_at[2][2];
+    const int t_row = half * 8 + (lane & 15) / 4;
+    int p_at[kForward ? 1 : kPB];
+    if constexpr (kForward) {
+        p_at[0] = wave_p * kPB * 32 * kRow + in_row;
+    } else {
 #pragma unroll
-    for (int far_slot = 0; far_slot < 2; ++far_slot)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int from = far_slot * kFirst * kSlot;
-            q_at[far_slot][e] = from + wave_t * kTB * 2048 + (in_row ^ (32 * e));
-            if constexpr (kForward) {
-                p_at[far_slot][e][0] = from + wave_p * kPB * 2048 + (in_row ^ (32 * e));
-            } else if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                for (int b = 0; b < kPB; ++b)
-                    p_at[far_slot][e][b] = from + (t_row + 16 * e) * kRowP + ((((wave_p * kPB + b) * 2 + (lane >> 4 & 1)) ^ (2 * (t_row & 3))) * 32) + (lane & 3) * 8;
-            } else {
-#pragma unroll
-                for (int b = 0; b < kPB; ++b) p_at[far_slot][e][b] = from + (8 * e + 4 * half) * kRowP + ((wave_p * kPB + b) * 32 + (lane & 31)) * 4;
-            }
+        for (int b = 0; b < kPB; ++b) {
+            if constexpr (sizeof(T) == 2)
+                p_at[b] = t_row * kRowP + ((((wave_p * kPB + b) * 2 + (lane >> 4 & 1)) ^ (2 * (t_row & 3))) * 32) + (lane & 3) * 8;
+            else p_at[b] = 4 * half * kRowP + ((wave_p * kPB + b) * 32 + (lane & 31)) * 4;
         }
+    }
+    const int q_at = kSlotP + wave_t * kTB * 32 * kRow + in_row;
     auto read = [&](int e, int slot) __attribute__((always_inline)) {
-        const int far_slot = slot >= kFirst, rest = slot * kSlot - base_of(slot);
+        const int to = e & 1;
 #pragma unroll
         for (int b = 0; b < kPB; ++b) {
             if constexpr (kForward) {
-                fp[e][b] = *reinterpret_cast<const u32x4 *>(lds + p_at[far_slot][e][0] + (rest + b * 2048));
+                fp[to][b] = *reinterpret_cast<const u32x4 *>(lds + ((p_at[0] ^ (32 * e)) + slot * kSlot) + b * 32 * kRow);
             } else if constexpr (sizeof(T) == 2) {
                 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                lds_char *const from = (lds_char *)lds + p_at[far_slot][e][b] + rest;
+                lds_char *const from = (lds_char *)lds + (p_at[b] + slot * kSlot) + 16 * e * kRowP;
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from);
                 const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * kRowP));
-                fp[e][b] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                fp[to][b] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) fp[e][b][j] = *reinterpret_cast<const uint32_t *>(lds + p_at[far_slot][e][b] + (rest + j * kRowP));
+                for (int j = 0; j < 4; ++j) fp[to][b][j] = *reinterpret_cast<const uint32_t *>(lds + (p_at[b] + slot * kSlot) + (8 * e + j) * kRowP);
             }
         }
 #pragma unroll
-        for (int t = 0; t < kTB; ++t) fq[e][t] = *reinterpret_cast<const u32x4 *>(lds + q_at[far_slot][e] + (rest + kSlotP + t * 2048));
+        for (int t = 0; t < kTB; ++t) fq[to][t] = *reinterpret_cast<const u32x4 *>(lds + ((q_at ^ (32 * e)) + slot * kSlot) + t * 32 * kRow);
     };
     auto multiply = [&](int e) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < kPB; ++b)
 #pragma unroll
-            for (int t = 0; t < kTB; ++t) acc[b][t] = multiply_add(T{}, fp[e][b], fq[e][t], acc[b][t]);
+            for (int t = 0; t < kTB; ++t) acc[b][t] = multiply_add(T{}, fp[e & 1][b], fq[e & 1][t], acc[b][t]);
     };
 
     // Whole steps.  Backward a load of columns reads what lies behind the row's last one, up to the end of the row's last chunk: not where that is behind
@@ -388,17 +379,19 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             for (int i = 0; i < kLoadsQ; ++i)
                 bring_16(to + kSlotP + (wave * kLoadsQ + i) * 1024, (global_bytes)from, kForward || !second ? off_q[0][i] : off_q[kSums - 1][i]);
         };
-        // Step s multiplies while the kSlots - 1 steps behind it are on their way or there.  Behind its barrier every wave has the last fragments of step s in
-        // registers and its share of step s+1 in the LDS: step s + kSlots is sent for in its place.  At the barrier all but step s+1 may be under way.
+        // Step s multiplies while step s+1 is on its way.  Behind its barrier every wave has the last fragments of step s in registers and its share of step s+1
+        // in the LDS: step s+2 is sent for in the place of step s.
         auto step = [&](int s, int slot, auto steady) __attribute__((always_inline)) {
-            read(1, slot);
-            multiply(0);
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kSlots - 2) * kLoads) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            read(0, (slot + 1) % kSlots);
+#pragma unroll
+            for (int e = 0; e < kParts - 1; ++e) {
+                read(e + 1, slot);
+                multiply(e);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            read(0, slot ^ 1);
             if (decltype(steady)::value || s + kSlots < end) bring(s + kSlots, slot);
-            multiply(1);
+            multiply(kParts - 1);
             __builtin_amdgcn_sched_barrier(0);
         };
         if (begin < end) {
@@ -444,10 +437,11 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             *reinterpret_cast<u32x4 *>(lds + kSlotP + (wave * kLoadsQ + i) * 1024 + lane * 16) = v;
         }
         __syncthreads();
-        read(0, 0);
-        read(1, 0);
-        multiply(0);
-        multiply(1);
+#pragma unroll
+        for (int e = 0; e < kParts; ++e) {
+            read(e, 0);
+            multiply(e);
+        }
     };
     if constexpr (kFar) {
         const int64_t per = (a.C + kStep - 1) / kStep, n = per * kSums;
@@ -510,7 +504,7 @@ template <typename T, typename G, bool kForward>
 int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split, const char *what) {
     constexpr int64_t kWide = kForward ? G::kP / 2 : G::kP, kSize = sizeof(T);
     const int64_t tiles_m = (whole.M + G::kTok - 1) / G::kTok, tiles_r = (whole.R + kWide - 1) / kWide;
-    const int64_t steps = (kForward ? 1 : 2) * ((static_cast<int64_t>(whole.C) + 4 * kPer16<T> - 1) / (4 * kPer16<T>));
+    const int64_t steps = (kForward ? 1 : 2) * ((static_cast<int64_t>(whole.C) * kSize + kRow - 1) / kRow);
     if (split > steps) split = steps;
     if (split < 1) split = 1;
     std::unique_lock<std::mutex> lock;
@@ -562,8 +556,8 @@ int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole,
 constexpr int64_t kFarBytes = 1 << 23;
 inline bool is_far(const Matrix &m, int64_t size) { return m.ld * size >= kFarBytes; }
 
-using Large = Tile<4, 2, 2, 2, 2, 3>;    // 256 x 128
-using Small = Tile<2, 2, 2, 2, 2, 4>;    // 128 x 128
+using Large = Tile<4, 2, 2, 4, 1>;    // 256 x 256
+using Small = Tile<2, 2, 2, 2, 2>;    // 128 x 128
 
 }  // namespace
 

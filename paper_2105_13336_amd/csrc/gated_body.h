@@ -120,13 +120,13 @@ struct Exchange {
     static __device__ __forceinline__ void order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 };
 
-// Tokens first_token .. +31 and the wavefront's features from r0 on, times() of them: write(t) puts what belongs to the t-th 32 tokens into the region.
+// Tokens from first_token on, 32 at a time, `times` times, and the wavefront's features from r0 on: write(t) puts what belongs to the t-th 32 tokens into the region.
 template <typename T, int kPB, bool kForward, typename Write>
 __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int64_t first_token, int r0, int times, Write write) {
     using E = Exchange<kPB, kForward>;
     const int lane = threadIdx.x & 63;
     const int r = r0 + lane % E::kLanes * 8, left = a.R - r;
-    float bias[2][8] = {};
+    float bias[kForward ? 2 : 1][8] = {};
     if constexpr (kForward) {
         if (a.bias[0]) {
 #pragma unroll
@@ -136,50 +136,76 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
                     if (j < left) bias[k][j] = param_at<T>(a.param_type, a.bias[k], r + j);
         }
     }
-#pragma unroll 1
-    for (int t = 0; t < times; ++t) {
-        E::order();
-        write(t);
-        E::order();
-#pragma unroll 1
-        for (int in = lane / E::kLanes; in < 32; in += E::kAtOnce) {
-            const int64_t token = first_token + 32 * t + in;
-            const bool there = token < a.M && left > 0;
-            float v[8];
-            E::get(region, 0, in, v);
-            if constexpr (kForward) {
-                float u[8];
-                E::get(region, 1, in, u);
+    // (Addresses go on by additions: a product of 64 bits for each store is a quarter of all of this.)
+    int64_t token = first_token + lane / E::kLanes;
+    T *out = static_cast<T *>(a.out.p) + token * a.out.ld + r;
+    int8_t *q[2] = {};
+    uint8_t *scale[2] = {};
+    if constexpr (kForward) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[j] += bias[0][j];
-                    u[j] += bias[1][j];
-                }
-                // (Rows that do not exist hold copies of the last one, without its bias: they take no part.)
-                if (left < 8) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j >= left) v[j] = u[j] = 0.0f;
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    if (!a.kept[k].q) continue;
-                    uint32_t code;
-                    const u32x2 w = pack8(k ? u : v, static_cast<uint32_t>(a.cap), code);
-                    if (there) store_q(a.kept[k].q + token * a.kept[k].ld_q + r, w, left);
-                    if (there && (lane & 3) == 0) a.kept[k].scale[token * a.kept[k].ld_scale + r / kGroup] = static_cast<uint8_t>(code);
-                }
-                auto apply = [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = decltype(act)::template value<kRoundsTo32<T>>(v[j]) * u[j];
-                };
-                if (a.act == TENSILE_SILU) apply(Silu{});
-                else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
-                else apply(Gelu<true>{});
+        for (int k = 0; k < 2; ++k)
+            if (a.kept[k].q) {
+                q[k] = a.kept[k].q + token * a.kept[k].ld_q + r;
+                scale[k] = a.kept[k].scale + token * a.kept[k].ld_scale + r / kGroup;
             }
-            if (there) store8(static_cast<T *>(a.out.p) + token * a.out.ld + r, v, left);
-        }
     }
+    auto all = [&](auto whole) __attribute__((always_inline)) {
+        constexpr bool kWhole = decltype(whole)::value;
+#pragma unroll 1
+        for (int t = 0; t < times; ++t) {
+            E::order();
+            write(t);
+            E::order();
+#pragma unroll 2
+            for (int pass = 0; pass < 32 / E::kAtOnce; ++pass) {
+                const int in = pass * E::kAtOnce + lane / E::kLanes, n = kWhole ? kChunk : left;
+                const bool there = kWhole || (token < a.M && left > 0);
+                float v[8];
+                E::get(region, 0, in, v);
+                if constexpr (kForward) {
+                    float u[8];
+                    E::get(region, 1, in, u);
+                    if (a.bias[0]) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            v[j] += bias[0][j];
+                            u[j] += bias[1][j];
+                        }
+                    }
+                    // (Rows that do not exist hold copies of the last one, without its bias: they take no part.)
+                    if (!kWhole && left < 8) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j >= left) v[j] = u[j] = 0.0f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        if (!a.kept[k].q) continue;
+                        uint32_t code;
+                        const u32x2 w = pack8(k ? u : v, static_cast<uint32_t>(a.cap), code);
+                        if (there) store_q(q[k], w, n);
+                        if (there && (lane & 3) == 0) *scale[k] = static_cast<uint8_t>(code);
+                        q[k] += E::kAtOnce * a.kept[k].ld_q;
+                        scale[k] += E::kAtOnce * a.kept[k].ld_scale;
+                    }
+                    auto apply = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] = decltype(act)::template value<kRoundsTo32<T>>(v[j]) * u[j];
+                    };
+                    if (a.act == TENSILE_SILU) apply(Silu{});
+                    else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
+                    else apply(Gelu<true>{});
+                }
+                if (there) store8(out, v, n);
+                out += E::kAtOnce * a.out.ld;
+                token += E::kAtOnce;
+            }
+        }
+    };
+    // (The same for all lanes of the wavefront, and asked once: else a tenth of this is questions.)
+    const bool whole = r0 + E::kWide <= a.R && first_token + 32 * times <= a.M;
+    if (whole) all(std::true_type{});
+    else all(std::false_type{});
 }
 
 // ------------------------------------------------------------------ tiles
@@ -327,8 +353,12 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             n_whole = a.C > behind ? static_cast<int>((a.C - behind) / kStep) : 0;
         }
     }
-    const int64_t n_steps = static_cast<int64_t>(kSums) * n_whole;
-    const int begin = static_cast<int>(n_steps * w.split / a.split), end = static_cast<int>(n_steps * (w.split + 1) / a.split);
+    int begin = 0, end = kSums * n_whole;                                // (at most 2^25: a step is 32 elements at least)
+    if (a.split > 1) {                                                   // (a division of 64 bits is some hundred instructions)
+        const int64_t n = end;
+        begin = static_cast<int>(n * w.split / a.split);
+        end = static_cast<int>(n * (w.split + 1) / a.split);
+    }
 
     if constexpr (!kFar) {
         const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)lds));
@@ -398,7 +428,8 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
 #pragma unroll
             for (int s = 0; s < kSlots; ++s)
                 if (begin + s < end) bring(begin + s, s);
-            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (begin + 1 < end) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoadsP + kLoadsQ) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
             read(0, 0);
             int s = begin;
             for (; s + 2 * kSlots <= end; s += kSlots) {

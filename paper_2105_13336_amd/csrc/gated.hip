@@ -8,14 +8,14 @@ namespace {
 template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
     const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
-    const char *const what = "gated_linear: partial sums";
+    if (a.M <= 32) return run_rows<T, true>(ops, s, a, far, 1, (a.R + 31) / 32 <= ops->num_cus);
     const int64_t large = ((a.M + Large::kTok - 1) / Large::kTok) * ((a.R + Large::kP / 2 - 1) / (Large::kP / 2));
-    if (large >= ops->num_cus) return run_tiles<T, Large, true>(ops, s, a, far, 1, what);
+    if (large >= ops->num_cus) return run_tiles<T, Large, true>(ops, s, a, far, 1);
     const int64_t small = ((a.M + Small::kTok - 1) / Small::kTok) * ((a.R + Small::kP / 2 - 1) / (Small::kP / 2));
     int64_t split = 2 * static_cast<int64_t>(ops->num_cus) / small;
     const int64_t most = a.C * static_cast<int64_t>(sizeof(T)) / 1024;
     if (split > most) split = most;
-    return run_tiles<T, Small, true>(ops, s, a, far, split, what);
+    return run_tiles<T, Small, true>(ops, s, a, far, split);
 }
 
 }  // namespace

@@ -42,14 +42,19 @@ __global__ __launch_bounds__(kEachThreads) void gated_grad_kernel(Walk w, Matrix
 template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
     const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.q[1], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
-    const char *const what = "gated_linear_backward: partial sums";
+    if (a.M <= 32) {
+        const int64_t tiles = (a.R + 63) / 64, steps = 2 * static_cast<int64_t>(a.C) * static_cast<int64_t>(sizeof(T)) / kRow;
+        int64_t split = 2 * static_cast<int64_t>(ops->num_cus) / tiles;
+        if (split > steps / 4) split = steps / 4;
+        return run_rows<T, false>(ops, s, a, far, split, tiles * split <= ops->num_cus);
+    }
     const int64_t large = ((a.M + Large::kTok - 1) / Large::kTok) * ((a.R + Large::kP - 1) / Large::kP);
-    if (large >= ops->num_cus) return run_tiles<T, Large, false>(ops, s, a, far, 1, what);
+    if (large >= ops->num_cus) return run_tiles<T, Large, false>(ops, s, a, far, 1);
     const int64_t small = ((a.M + Small::kTok - 1) / Small::kTok) * ((a.R + Small::kP - 1) / Small::kP);
     int64_t split = 2 * static_cast<int64_t>(ops->num_cus) / small;
     const int64_t most = 2 * a.C * static_cast<int64_t>(sizeof(T)) / 1024;
     if (split > most) split = most;
-    return run_tiles<T, Small, false>(ops, s, a, far, split, what);
+    return run_tiles<T, Small, false>(ops, s, a, far, split);
 }
 
 }  // namespace

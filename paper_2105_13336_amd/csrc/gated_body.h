@@ -106,10 +106,18 @@ struct Exchange {
 #pragma unroll
         for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4 *>(to + 8 * q) = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
     }
+    // Eight features of a token, kRegions wavefronts' sums added up.
+    template <int kRegions>
     static __device__ __forceinline__ void get(const float *region, int plane, int token, float (&v)[8]) {
         const int lane = threadIdx.x & 63;
-        const float *const from = region + plane * 32 * kPitch + token * kPitch + lane % kLanes * 8;
-        const f32x4 lo = *reinterpret_cast<const f32x4 *>(from), hi = *reinterpret_cast<const f32x4 *>(from + 4);
+        const float *from = region + plane * 32 * kPitch + token * kPitch + lane % kLanes * 8;
+        f32x4 lo = *reinterpret_cast<const f32x4 *>(from), hi = *reinterpret_cast<const f32x4 *>(from + 4);
+#pragma unroll
+        for (int k = 1; k < kRegions; ++k) {
+            from += kBytes / 4;
+            lo += *reinterpret_cast<const f32x4 *>(from);
+            hi += *reinterpret_cast<const f32x4 *>(from + 4);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             v[j] = lo[j];
@@ -120,9 +128,10 @@ struct Exchange {
     static __device__ __forceinline__ void order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 };
 
-// Tokens from first_token on, 32 at a time, `times` times, and the wavefront's features from r0 on: write(t) puts what belongs to the t-th 32 tokens into the region.
-template <typename T, int kPB, bool kForward, typename Write>
-__device__ __forceinline__ void finish(const ProductArgs &a, float *region, int64_t first_token, int r0, int times, Write write) {
+// Tokens from first_token on, 32 at a time, `times` times, and features from r0 on: write(t) puts what belongs to the t-th 32 tokens into the region (kRegions of
+// them: each wavefront's part of the sums).  A wavefront goes through them from pass `start` on, every `stride`-th one.
+template <typename T, int kPB, bool kForward, int kRegions, typename Write>
+__device__ __forceinline__ void finish(const ProductArgs &a, float *region, int64_t first_token, int r0, int times, int start, int stride, Write write) {
     using E = Exchange<kPB, kForward>;
     const int lane = threadIdx.x & 63;
     const int r = r0 + lane % E::kLanes * 8, left = a.R - r;
@@ -137,7 +146,7 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
         }
     }
     // (Addresses go on by additions: a product of 64 bits for each store is a quarter of all of this.)
-    int64_t token = first_token + lane / E::kLanes;
+    int64_t token = first_token + start * E::kAtOnce + lane / E::kLanes;
     T *out = static_cast<T *>(a.out.p) + token * a.out.ld + r;
     int8_t *q[2] = {};
     uint8_t *scale[2] = {};
@@ -157,14 +166,14 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
             write(t);
             E::order();
 #pragma unroll 2
-            for (int pass = 0; pass < 32 / E::kAtOnce; ++pass) {
+            for (int pass = start; pass < 32 / E::kAtOnce; pass += stride) {
                 const int in = pass * E::kAtOnce + lane / E::kLanes, n = kWhole ? kChunk : left;
                 const bool there = kWhole || (token < a.M && left > 0);
                 float v[8];
-                E::get(region, 0, in, v);
+                E::template get<kRegions>(region, 0, in, v);
                 if constexpr (kForward) {
                     float u[8];
-                    E::get(region, 1, in, u);
+                    E::template get<kRegions>(region, 1, in, u);
                     if (a.bias[0]) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -185,8 +194,8 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
                         const u32x2 w = pack8(k ? u : v, static_cast<uint32_t>(a.cap), code);
                         if (there) store_q(q[k], w, n);
                         if (there && (lane & 3) == 0) *scale[k] = static_cast<uint8_t>(code);
-                        q[k] += E::kAtOnce * a.kept[k].ld_q;
-                        scale[k] += E::kAtOnce * a.kept[k].ld_scale;
+                        q[k] += stride * E::kAtOnce * a.kept[k].ld_q;
+                        scale[k] += stride * E::kAtOnce * a.kept[k].ld_scale;
                     }
                     auto apply = [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
@@ -197,8 +206,8 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
                     else apply(Gelu<true>{});
                 }
                 if (there) store8(out, v, n);
-                out += E::kAtOnce * a.out.ld;
-                token += E::kAtOnce;
+                out += stride * E::kAtOnce * a.out.ld;
+                token += stride * E::kAtOnce;
             }
         }
     };
@@ -254,20 +263,51 @@ __device__ __forceinline__ Place place(const ProductArgs &a) {
     return w;
 }
 
+// From memory to the LDS without a register in between, 16 bytes of each lane in the order of the lanes.  (By hand: of the builtin the compiler waits for every
+// one under way before the next LDS read, whatever it reads.  They write no register; the kernels wait.)
+__device__ __forceinline__ void bring_16(uint32_t to, global_bytes from, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
+}
+
+// A tile's steps: what is brought to the LDS, read from there and multiplied.  kWaves wavefronts, of which this is number `wave`, share slots at `lds`;
 // kFar: rows too far apart for 32-bit offsets; every step goes by way of registers.
 template <typename T, typename G, bool kForward, bool kFar>
-__global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void product_kernel(ProductArgs a) {
-    constexpr int kPB = G::kPB, kTB = G::kTB, kPer = kPer16<T>, kStep = kRow / static_cast<int>(sizeof(T));      // elements of a sum in a step
-    constexpr int kSlotP = G::kP * kRow, kSlot = kSlotP + G::kTok * kRow;
-    constexpr int kLoadsP = G::kP / 8 / G::kWaves, kLoadsQ = G::kTok / 8 / G::kWaves;   // a wave's, of 1024 bytes each
+struct Steps {
+    static constexpr int kPB = G::kPB, kTB = G::kTB, kPer = kPer16<T>, kStep = kRow / static_cast<int>(sizeof(T));   // elements of a sum in a step
+    static constexpr int kSums = kForward ? 1 : 2;
+    static constexpr int kSlotP = G::kP * kRow, kSlot = kSlotP + G::kTok * kRow;
+    static constexpr int kLoadsP = G::kP / 8 / G::kWaves, kLoadsQ = G::kTok / 8 / G::kWaves;                         // a wave's, of 1024 bytes each
     static_assert(kLoadsP * G::kWaves * 8 == G::kP && kLoadsQ * G::kWaves * 8 == G::kTok, "");
-    constexpr int kRowP = G::kP * static_cast<int>(sizeof(T));                         // backward: bytes of a staged row of the weights
-    constexpr int kExchange = Exchange<kPB, kForward>::kBytes * G::kWaves;
-    __shared__ __attribute__((aligned(1024))) char lds[kSlots * kSlot > kExchange ? kSlots * kSlot : kExchange];
+    static constexpr int kRowP = G::kP * static_cast<int>(sizeof(T));                                                // backward: bytes of a staged row of the weights
+    static constexpr int64_t kSize = sizeof(T);
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wave_p = wave / G::kWT, wave_t = wave % G::kWT;
-    const Place w = place<G, kForward>(a);
+    const ProductArgs &a;
+    char *const lds;
+    const int64_t m0;
+    const int r0, lane, wave, wave_p, wave_t;
+    int n_whole = 0;                  // whole steps (backward: of each sum)
+
+    // What a lane multiplies of a part of a step, and the sums.  (Not members: the compiler would keep them in memory.)
+    struct Fragments {
+        u32x4 p[kPB], q[kTB];
+    };
+    using Sums = f32x16[kPB][kTB];
+
+    __device__ __forceinline__ Steps(const ProductArgs &args, const Place &w, char *slots, int number)
+        : a(args), lds(slots), m0(w.m0), r0(w.r0), lane(threadIdx.x & 63), wave(number), wave_p(number / G::kWT), wave_t(number % G::kWT) {
+        if constexpr (!kFar) {
+            if constexpr (kForward) {
+                n_whole = a.C / kStep;
+            } else {
+                // A load of columns reads what lies behind the row's last one, up to the end of the row's last chunk: not where that is behind the matrix.
+                const int64_t least = a.p[0].ld < a.p[1].ld ? a.p[0].ld : a.p[1].ld;
+                const int64_t behind = a.R % kPer == 0 ? 0 : (kPer - 1 + least - 1) / least;   // rows at the end that are not read whole
+                n_whole = a.C > behind ? static_cast<int>((a.C - behind) / kStep) : 0;
+            }
+        }
+        places();
+        if constexpr (!kFar) offsets();
+    }
 
     // What a lane brings of a step, 16 bytes a load.  Tokens, and forward the weights: 8 rows x 8 chunks to a load.  Backward the weights lie with the summed
     // index outermost: whole rows of the tile's columns, staged as they are (16 bits: their 32-byte blocks in an order that depends on the row, so
@@ -276,161 +316,190 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
         int64_t row;                  // of the matrix (backward, weights: of the step)
         int col;                      // element
     };
-    auto row_of = [&](int i) __attribute__((always_inline)) { return (wave * kLoadsP + i) * 8 + lane / 8; };       // of the tile's weights, forward
-    auto piece_p = [&](int i) __attribute__((always_inline)) -> Piece {
+    static __device__ __forceinline__ int turned(int row) { return kRowP >= 256 ? 2 * (row & 3) : 2 * (row >> 1 & 1); }
+    __device__ __forceinline__ Piece piece_p(int i) const {
         if constexpr (kForward) {
-            const int row = row_of(i), f = w.r0 + row / 64 * 32 + row % 32;
+            const int row = (wave * kLoadsP + i) * 8 + lane / 8, f = r0 + row / 64 * 32 + row % 32;
             return {f < a.R ? f : a.R - 1, stored_chunk(row, lane & 7) * kPer};
         } else {
             const int at = ((wave * kLoadsP + i) * 64 + lane) * 16, row = at / kRowP, in = at % kRowP;
-            int col = sizeof(T) == 2 ? ((in / 32) ^ (2 * (row & 3))) * 16 + in % 32 / 2 : in / 4;
-            col += w.r0;
-            return {row, col};
-        }
-    };
-    auto piece_q = [&](int i) __attribute__((always_inline)) -> Piece {
-        const int row = (wave * kLoadsQ + i) * 8 + lane / 8;
-        const int64_t m = w.m0 + row;
-        return {m < a.M ? m : a.M - 1, stored_chunk(row, lane & 7) * kPer};
-    };
-    auto matrix_of = [&](int i) __attribute__((always_inline)) { return kForward ? ((wave * kLoadsP + i) >> 2) & 1 : 0; };
-
-    f32x16 acc[kPB][kTB] = {};
-    u32x4 fp[2][kPB], fq[2][kTB];
-    // Where a lane's fragments lie, part e of the step in the first slot.  (Two chunks on are an exclusive or, in the order of the chunks.)
-    const int half = lane >> 5, in_row = (lane & 31) * kRow + stored_chunk(lane & 31, half) * 16;
-    // backward, 16 bits: 16 lanes read four rows of 16 columns and each gets the four values of its column
-    const int t_row = half * 8 + (lane & 15) / 4;
-    int p_at[kForward ? 1 : kPB];
-    if constexpr (kForward) {
-        p_at[0] = wave_p * kPB * 32 * kRow + in_row;
-    } else {
-#pragma unroll
-        for (int b = 0; b < kPB; ++b) {
-            if constexpr (sizeof(T) == 2)
-                p_at[b] = t_row * kRowP + ((((wave_p * kPB + b) * 2 + (lane >> 4 & 1)) ^ (2 * (t_row & 3))) * 32) + (lane & 3) * 8;
-            else p_at[b] = 4 * half * kRowP + ((wave_p * kPB + b) * 32 + (lane & 31)) * 4;
+            const int col = sizeof(T) == 2 ? ((in / 32) ^ turned(row)) * 16 + in % 32 / 2 : in / 4;
+            return {row, r0 + col};
         }
     }
-    const int q_at = kSlotP + wave_t * kTB * 32 * kRow + in_row;
-    auto read = [&](int e, int slot) __attribute__((always_inline)) {
-        const int to = e & 1;
+    __device__ __forceinline__ Piece piece_q(int i) const {
+        const int row = (wave * kLoadsQ + i) * 8 + lane / 8;
+        const int64_t m = m0 + row;
+        return {m < a.M ? m : a.M - 1, stored_chunk(row, lane & 7) * kPer};
+    }
+    __device__ __forceinline__ int matrix_of(int i) const { return kForward ? ((wave * kLoadsP + i) >> 2) & 1 : 0; }
+
+    uint32_t off_p[kLoadsP], off_q[kSums][kLoadsQ];
+    const char *base_p[2], *base_q[kSums];
+    __device__ __forceinline__ void offsets() {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) base_p[k] = static_cast<const char *>(a.p[k].p) + (kForward ? r0 * a.p[k].ld : static_cast<int64_t>(r0)) * kSize;
+#pragma unroll
+        for (int i = 0; i < kLoadsP; ++i) {
+            const Piece c = piece_p(i);
+            if constexpr (kForward) off_p[i] = static_cast<uint32_t>(((c.row - r0) * (matrix_of(i) ? a.p[1].ld : a.p[0].ld) + c.col) * kSize);
+            else off_p[i] = static_cast<uint32_t>((c.col < a.R ? c.col - r0 : 0) * kSize);
+        }
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) {
+            base_q[k] = static_cast<const char *>(a.q[k].p) + m0 * a.q[k].ld * kSize;
+#pragma unroll
+            for (int i = 0; i < kLoadsQ; ++i) {
+                const Piece c = piece_q(i);
+                off_q[k][i] = static_cast<uint32_t>(((c.row - m0) * a.q[k].ld + c.col) * kSize);
+            }
+        }
+    }
+    // Step s, of 2 * n_whole backward (gate, then up); kQ: of the tokens' loads the first ones only
+    template <int kQ = kLoadsQ>
+    __device__ __forceinline__ void bring(int s, int slot) const {
+        const bool second = !kForward && s >= n_whole;
+        const int64_t at = static_cast<int64_t>(second ? s - n_whole : s) * kStep;
+        const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)lds)) + slot * kSlot;
+        if constexpr (kForward) {
+#pragma unroll
+            for (int i = 0; i < kLoadsP; ++i) bring_16(to + (wave * kLoadsP + i) * 1024, (global_bytes)((matrix_of(i) ? base_p[1] : base_p[0]) + at * kSize), off_p[i]);
+        } else {
+            const int64_t pitch = (second ? a.p[1].ld : a.p[0].ld) * kSize;
+            const char *const from = second ? base_p[1] : base_p[0];
+#pragma unroll
+            for (int i = 0; i < kLoadsP; ++i) {
+                const uint32_t row = static_cast<uint32_t>(((wave * kLoadsP + i) * 64 + lane) * 16 / kRowP);
+                bring_16(to + (wave * kLoadsP + i) * 1024, (global_bytes)(from + at * pitch), row * static_cast<uint32_t>(pitch) + off_p[i]);
+            }
+        }
+        const char *const from = (kForward || !second ? base_q[0] : base_q[kSums - 1]) + at * kSize;
+#pragma unroll
+        for (int i = 0; i < kQ; ++i)
+            bring_16(to + kSlotP + (wave * kLoadsQ + i) * 1024, (global_bytes)from, kForward || !second ? off_q[0][i] : off_q[kSums - 1][i]);
+    }
+
+    // Where a lane's fragments lie, part e of the step in the first slot.  (Two chunks on are an exclusive or, in the order of the chunks.)
+    int p_at[kForward ? 1 : kPB], q_at;
+    __device__ __forceinline__ void places() {
+        const int half = lane >> 5, in_row = (lane & 31) * kRow + stored_chunk(lane & 31, half) * 16;
+        q_at = kSlotP + wave_t * kTB * 32 * kRow + in_row;
+        if constexpr (kForward) {
+            p_at[0] = wave_p * kPB * 32 * kRow + in_row;
+        } else {
+            // 16 bits: 16 lanes read four rows of 16 columns and each gets the four values of its column
+            const int t_row = half * 8 + (lane & 15) / 4;
+#pragma unroll
+            for (int b = 0; b < kPB; ++b) {
+                if constexpr (sizeof(T) == 2)
+                    p_at[b] = t_row * kRowP + ((((wave_p * kPB + b) * 2 + (lane >> 4 & 1)) ^ turned(t_row)) * 32) + (lane & 3) * 8;
+                else p_at[b] = 4 * half * kRowP + ((wave_p * kPB + b) * 32 + (lane & 31)) * 4;
+            }
+        }
+    }
+    __device__ __forceinline__ void read(Fragments &f, int e, int slot) const {
 #pragma unroll
         for (int b = 0; b < kPB; ++b) {
             if constexpr (kForward) {
-                fp[to][b] = *reinterpret_cast<const u32x4 *>(lds + ((p_at[0] ^ (32 * e)) + slot * kSlot) + b * 32 * kRow);
+                f.p[b] = *reinterpret_cast<const u32x4 *>(lds + ((p_at[0] ^ (32 * e)) + slot * kSlot) + b * 32 * kRow);
             } else if constexpr (sizeof(T) == 2) {
                 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
                 lds_char *const from = (lds_char *)lds + (p_at[b] + slot * kSlot) + 16 * e * kRowP;
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from);
                 const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * kRowP));
-                fp[to][b] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                f.p[b] = __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) fp[to][b][j] = *reinterpret_cast<const uint32_t *>(lds + (p_at[b] + slot * kSlot) + (8 * e + j) * kRowP);
+                for (int j = 0; j < 4; ++j) f.p[b][j] = *reinterpret_cast<const uint32_t *>(lds + (p_at[b] + slot * kSlot) + (8 * e + j) * kRowP);
             }
         }
 #pragma unroll
-        for (int t = 0; t < kTB; ++t) fq[to][t] = *reinterpret_cast<const u32x4 *>(lds + ((q_at ^ (32 * e)) + slot * kSlot) + t * 32 * kRow);
-    };
-    auto multiply = [&](int e) __attribute__((always_inline)) {
+        for (int t = 0; t < kTB; ++t) f.q[t] = *reinterpret_cast<const u32x4 *>(lds + ((q_at ^ (32 * e)) + slot * kSlot) + t * 32 * kRow);
+    }
+    static __device__ __forceinline__ void multiply(const Fragments &f, Sums &acc) {
 #pragma unroll
         for (int b = 0; b < kPB; ++b)
 #pragma unroll
-            for (int t = 0; t < kTB; ++t) acc[b][t] = multiply_add(T{}, fp[e & 1][b], fq[e & 1][t], acc[b][t]);
-    };
+            for (int t = 0; t < kTB; ++t) acc[b][t] = multiply_add(T{}, f.p[b], f.q[t], acc[b][t]);
+    }
 
-    // Whole steps.  Backward a load of columns reads what lies behind the row's last one, up to the end of the row's last chunk: not where that is behind
-    // the matrix.  Of those steps, 2 * n_whole backward (gate, then up), the split takes a part; the rest, by way of registers, its last one.
-    constexpr int kSums = kForward ? 1 : 2;
-    int n_whole = 0;
-    if constexpr (!kFar) {
-        if constexpr (kForward) {
-            n_whole = a.C / kStep;
-        } else {
-            const int64_t least = a.p[0].ld < a.p[1].ld ? a.p[0].ld : a.p[1].ld;
-            const int64_t behind = a.R % kPer == 0 ? 0 : (kPer - 1 + least - 1) / least;   // rows at the end that are not read whole
-            n_whole = a.C > behind ? static_cast<int>((a.C - behind) / kStep) : 0;
+    // Elements from c0 on of sum k, less than a step or the matrices' last rows, by way of registers, to the first slot.  `meet`: what the wavefronts that share
+    // the slots do before and behind.
+    template <typename Meet>
+    __device__ __forceinline__ void rest(int k, int64_t c0, Sums &acc, Meet meet) const {
+        meet();
+#pragma unroll
+        for (int i = 0; i < kLoadsP; ++i) {
+            const Piece c = piece_p(i);
+            u32x4 v;
+            if constexpr (kForward) {
+                const Matrix m = matrix_of(i) ? a.p[1] : a.p[0];
+                v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
+            } else {
+                const Matrix m = k ? a.p[1] : a.p[0];
+                const int64_t row = c0 + c.row;
+                v = load_chunk(static_cast<const T *>(m.p) + row * m.ld + c.col, row < a.C ? a.R - c.col : 0);
+            }
+            *reinterpret_cast<u32x4 *>(lds + (wave * kLoadsP + i) * 1024 + lane * 16) = v;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoadsQ; ++i) {
+            const Piece c = piece_q(i);
+            const Matrix m = k ? a.q[1] : a.q[0];
+            const u32x4 v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
+            *reinterpret_cast<u32x4 *>(lds + kSlotP + (wave * kLoadsQ + i) * 1024 + lane * 16) = v;
+        }
+        meet();
+#pragma unroll
+        for (int e = 0; e < kParts; ++e) {
+            Fragments f;
+            read(f, e, 0);
+            multiply(f, acc);
         }
     }
-    int begin = 0, end = kSums * n_whole;                                // (at most 2^25: a step is 32 elements at least)
+};
+
+// The whole steps are the splits' by equal parts, the rest is the last one's.
+template <typename T, typename G, bool kForward, bool kFar>
+__global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void product_kernel(ProductArgs a) {
+    using S = Steps<T, G, kForward, kFar>;
+    using E = Exchange<G::kPB, kForward>;
+    constexpr int kExchange = E::kBytes * G::kWaves;
+    __shared__ __attribute__((aligned(1024))) char lds[kSlots * S::kSlot > kExchange ? kSlots * S::kSlot : kExchange];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place w = place<G, kForward>(a);
+    const S st(a, w, lds, wave);
+    typename S::Sums acc = {};
+    typename S::Fragments f[2];
+    int begin = 0, end = S::kSums * st.n_whole;                          // (at most 2^25: a step is 32 elements at least)
     if (a.split > 1) {                                                   // (a division of 64 bits is some hundred instructions)
         const int64_t n = end;
         begin = static_cast<int>(n * w.split / a.split);
         end = static_cast<int>(n * (w.split + 1) / a.split);
     }
-
     if constexpr (!kFar) {
-        const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)lds));
-        // From memory to the LDS without a register in between, 16 bytes of each lane in the order of the lanes.  (By hand: of the builtin the compiler waits
-        // for every one under way before the next LDS read, whatever it reads.  They write no register; the waits are at the barriers below.)
-        auto bring_16 = [&](uint32_t to, global_bytes from, uint32_t off) __attribute__((always_inline)) {
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
-        };
-        uint32_t off_p[kLoadsP], off_q[kSums][kLoadsQ];
-        const char *base_p[2], *base_q[kSums];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            base_p[k] = static_cast<const char *>(a.p[k].p) + (kForward ? w.r0 * a.p[k].ld : static_cast<int64_t>(w.r0)) * static_cast<int64_t>(sizeof(T));
-#pragma unroll
-        for (int k = 0; k < kSums; ++k) base_q[k] = static_cast<const char *>(a.q[k].p) + w.m0 * a.q[k].ld * static_cast<int64_t>(sizeof(T));
-#pragma unroll
-        for (int i = 0; i < kLoadsP; ++i) {
-            const Piece c = piece_p(i);
-            if constexpr (kForward) off_p[i] = static_cast<uint32_t>(((c.row - w.r0) * a.p[matrix_of(i)].ld + c.col) * static_cast<int64_t>(sizeof(T)));
-            else off_p[i] = static_cast<uint32_t>((c.col < a.R ? c.col - w.r0 : 0) * static_cast<int64_t>(sizeof(T)));
-        }
-#pragma unroll
-        for (int k = 0; k < kSums; ++k)
-#pragma unroll
-            for (int i = 0; i < kLoadsQ; ++i) {
-                const Piece c = piece_q(i);
-                off_q[k][i] = static_cast<uint32_t>(((c.row - w.m0) * a.q[k].ld + c.col) * static_cast<int64_t>(sizeof(T)));
-            }
-        auto bring = [&](int s, int slot) __attribute__((always_inline)) {
-            const bool second = !kForward && s >= n_whole;
-            const int64_t at = static_cast<int64_t>(second ? s - n_whole : s) * kStep;
-            const uint32_t to = lds_at + slot * kSlot;
-            if constexpr (kForward) {
-#pragma unroll
-                for (int i = 0; i < kLoadsP; ++i)
-                    bring_16(to + (wave * kLoadsP + i) * 1024, (global_bytes)(base_p[matrix_of(i)] + at * static_cast<int64_t>(sizeof(T))), off_p[i]);
-            } else {
-                const int64_t pitch = (second ? a.p[1].ld : a.p[0].ld) * static_cast<int64_t>(sizeof(T));
-                const char *const from = second ? base_p[1] : base_p[0];
-#pragma unroll
-                for (int i = 0; i < kLoadsP; ++i) {
-                    const uint32_t row = static_cast<uint32_t>(((wave * kLoadsP + i) * 64 + lane) * 16 / kRowP);
-                    bring_16(to + (wave * kLoadsP + i) * 1024, (global_bytes)(from + at * pitch), row * static_cast<uint32_t>(pitch) + off_p[i]);
-                }
-            }
-            const char *const from = (kForward || !second ? base_q[0] : base_q[kSums - 1]) + at * static_cast<int64_t>(sizeof(T));
-#pragma unroll
-            for (int i = 0; i < kLoadsQ; ++i)
-                bring_16(to + kSlotP + (wave * kLoadsQ + i) * 1024, (global_bytes)from, kForward || !second ? off_q[0][i] : off_q[kSums - 1][i]);
-        };
         // Step s multiplies while step s+1 is on its way.  Behind its barrier every wave has the last fragments of step s in registers and its share of step s+1
         // in the LDS: step s+2 is sent for in the place of step s.
         auto step = [&](int s, int slot, auto steady) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < kParts - 1; ++e) {
-                read(e + 1, slot);
-                multiply(e);
+                st.read(f[(e + 1) & 1], e + 1, slot);
+                S::multiply(f[e & 1], acc);
                 __builtin_amdgcn_sched_barrier(0);
             }
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            read(0, slot ^ 1);
-            if (decltype(steady)::value || s + kSlots < end) bring(s + kSlots, slot);
-            multiply(kParts - 1);
+            st.read(f[0], 0, slot ^ 1);
+            if (decltype(steady)::value || s + kSlots < end) st.bring(s + kSlots, slot);
+            S::multiply(f[(kParts - 1) & 1], acc);
             __builtin_amdgcn_sched_barrier(0);
         };
         if (begin < end) {
 #pragma unroll
             for (int s = 0; s < kSlots; ++s)
-                if (begin + s < end) bring(begin + s, s);
-            if (begin + 1 < end) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kLoadsP + kLoadsQ) : "memory");
+                if (begin + s < end) st.bring(begin + s, s);
+            if (begin + 1 < end) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(S::kLoadsP + S::kLoadsQ) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-            read(0, 0);
+            st.read(f[0], 0, 0);
             int s = begin;
             for (; s + 2 * kSlots <= end; s += kSlots) {
 #pragma unroll
@@ -443,65 +512,129 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             }
         }
     }
-    // What is left of the sums, less than a step or the matrices' last rows (kFar: all of them, split by steps), by way of registers.
-    auto rest = [&](int k, int64_t c0) __attribute__((always_inline)) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kLoadsP; ++i) {
-            const Piece c = piece_p(i);
-            u32x4 v;
-            if constexpr (kForward) {
-                const Matrix &m = a.p[matrix_of(i)];
-                v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
-            } else {
-                const Matrix &m = a.p[k];
-                const int64_t row = c0 + c.row;
-                v = load_chunk(static_cast<const T *>(m.p) + row * m.ld + c.col, row < a.C ? a.R - c.col : 0);
-            }
-            *reinterpret_cast<u32x4 *>(lds + (wave * kLoadsP + i) * 1024 + lane * 16) = v;
-        }
-#pragma unroll
-        for (int i = 0; i < kLoadsQ; ++i) {
-            const Piece c = piece_q(i);
-            const Matrix &m = a.q[k];
-            const u32x4 v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
-            *reinterpret_cast<u32x4 *>(lds + kSlotP + (wave * kLoadsQ + i) * 1024 + lane * 16) = v;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kParts; ++e) {
-            read(e, 0);
-            multiply(e);
-        }
-    };
+    auto meet = [] { __syncthreads(); };
     if constexpr (kFar) {
-        const int64_t per = (a.C + kStep - 1) / kStep, n = per * kSums;
-        for (int64_t s = n * w.split / a.split; s < n * (w.split + 1) / a.split; ++s) rest(s >= per, (s >= per ? s - per : s) * kStep);
+        const int64_t per = (a.C + S::kStep - 1) / S::kStep, n = per * S::kSums;
+        for (int64_t s = n * w.split / a.split; s < n * (w.split + 1) / a.split; ++s) st.rest(s >= per, (s >= per ? s - per : s) * S::kStep, acc, meet);
     } else if (w.split == a.split - 1) {
-        for (int k = 0; k < kSums; ++k)
-            for (int64_t c0 = static_cast<int64_t>(n_whole) * kStep; c0 < a.C; c0 += kStep) rest(k, c0);
+        for (int k = 0; k < S::kSums; ++k)
+            for (int64_t c0 = static_cast<int64_t>(st.n_whole) * S::kStep; c0 < a.C; c0 += S::kStep) st.rest(k, c0, acc, meet);
     }
     if (a.split > 1) {
-        float *const out = a.part + ((static_cast<int64_t>(w.tile) * a.split + w.split) * G::kWaves + wave) * (kPB * kTB * 1024) + lane;
+        float *const out = a.part + ((static_cast<int64_t>(w.tile) * a.split + w.split) * G::kWaves + wave) * (G::kPB * G::kTB * 1024) + lane;
 #pragma unroll
-        for (int b = 0; b < kPB; ++b)
+        for (int b = 0; b < G::kPB; ++b)
 #pragma unroll
-            for (int t = 0; t < kTB; ++t)
+            for (int t = 0; t < G::kTB; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) out[((b * kTB + t) * 16 + r) * 64] = acc[b][t][r];
+                for (int r = 0; r < 16; ++r) out[((b * G::kTB + t) * 16 + r) * 64] = acc[b][t][r];
         return;
     }
     __syncthreads();
-    using E = Exchange<kPB, kForward>;
     float *const region = reinterpret_cast<float *>(lds + wave * E::kBytes);
-    finish<T, kPB, kForward>(a, region, w.m0 + wave_t * kTB * 32, w.r0 + wave_p * E::kWide, kTB, [&](int t) __attribute__((always_inline)) {
+    finish<T, G::kPB, kForward, 1>(a, region, w.m0 + st.wave_t * G::kTB * 32, w.r0 + st.wave_p * E::kWide, G::kTB, 0, 1, [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-        for (int tt = 0; tt < kTB; ++tt)
+        for (int tt = 0; tt < G::kTB; ++tt)
             if (t == tt) {
 #pragma unroll
-                for (int b = 0; b < kPB; ++b) E::put(region, b, acc[b][tt]);
+                for (int b = 0; b < G::kPB; ++b) E::put(region, b, acc[b][tt]);
             }
     });
+}
+
+// Up to 32 tokens: the weights are read once and that is what it costs.  A workgroup has 32 features (backward 64), of whose sums each wavefront takes every
+// kWaves-th step, by itself: it brings its own steps, kRing of them, and waits for nobody.  The wavefronts' sums are added up where they go through
+// the LDS.  kQ: loads of eight tokens (more rows of the staged 32 than that are left as they are; their columns of the result are not used).
+constexpr int kRing = 3;
+using Rows = Tile<2, 1, 1, 1, 1>;
+template <typename T, bool kForward, bool kFar, int kWaves, int kQ>
+__global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a) {
+    using S = Steps<T, Rows, kForward, kFar>;
+    using E = Exchange<Rows::kPB, kForward>;
+    static_assert(kWaves * E::kBytes <= kWaves * kRing * S::kSlot, "");
+    __shared__ __attribute__((aligned(1024))) char lds[kWaves * kRing * S::kSlot];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Place w = place<Rows, kForward>(a);
+    const S st(a, w, lds + wave * kRing * S::kSlot, 0);
+    typename S::Sums acc = {};
+    if constexpr (!kFar) {
+        // the wavefront's steps: first, first + stride, ... : n of them
+        const int stride = kWaves * static_cast<int>(a.split), first = static_cast<int>(w.split) * kWaves + wave, total = S::kSums * st.n_whole;
+        const int n = total > first ? (total - first + stride - 1) / stride : 0;
+        auto step = [&](int i, int slot, auto steady) __attribute__((always_inline)) {
+            if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRing - 1) * (S::kLoadsP + kQ)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            typename S::Fragments f[2];
+            st.read(f[0], 0, slot);
+#pragma unroll
+            for (int e = 0; e < kParts; ++e) {
+                if (e + 1 < kParts) st.read(f[(e + 1) & 1], e + 1, slot);
+                S::multiply(f[e & 1], acc);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (decltype(steady)::value || i + kRing < n) st.template bring<kQ>(first + (i + kRing) * stride, slot);
+        };
+#pragma unroll
+        for (int k = 0; k < kRing; ++k)
+            if (k < n) st.template bring<kQ>(first + k * stride, k);
+        int i = 0;
+        for (; i + 2 * kRing <= n; i += kRing) {
+#pragma unroll
+            for (int k = 0; k < kRing; ++k) step(i + k, k, std::true_type{});
+        }
+        for (; i < n; i += kRing) {
+#pragma unroll
+            for (int k = 0; k < kRing; ++k)
+                if (i + k < n) step(i + k, k, std::false_type{});
+        }
+    }
+    // (the rest goes on in turn behind the whole steps: kFar all of it)
+    {
+        const int64_t c0 = static_cast<int64_t>(st.n_whole) * S::kStep, per = (a.C - c0 + S::kStep - 1) / S::kStep, n = per * S::kSums;
+        const int64_t stride = static_cast<int64_t>(kWaves) * a.split;
+        for (int64_t s = (static_cast<int64_t>(w.split) * kWaves + wave + stride - S::kSums * static_cast<int64_t>(st.n_whole) % stride) % stride; s < n; s += stride)
+            st.rest(s >= per, c0 + (s >= per ? s - per : s) * S::kStep, acc, [] { E::order(); });
+    }
+    __syncthreads();
+    float *const region = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int b = 0; b < Rows::kPB; ++b) E::put(reinterpret_cast<float *>(lds + wave * E::kBytes), b, acc[b][0]);
+    __syncthreads();
+    if (a.split > 1) {                                                   // (backward: 32 x 64 sums, token by token)
+        if constexpr (!kForward) {
+            float *const out = a.part + (static_cast<int64_t>(w.tile) * a.split + w.split) * (32 * E::kWide);
+            for (int pass = wave; pass < 32 / E::kAtOnce; pass += kWaves) {
+                const int in = pass * E::kAtOnce + lane / E::kLanes;
+                float v[8];
+                E::template get<kWaves>(region, 0, in, v);
+                if (w.m0 + in < a.M) store8(out + in * E::kWide + lane % E::kLanes * 8, v, kChunk);
+            }
+        }
+        return;
+    }
+    finish<T, Rows::kPB, kForward, kWaves>(a, region, w.m0, w.r0, 1, wave, kWaves, [](int) {});
+}
+
+// Backward with split > 1: the parts added up in a fixed order.  Eight columns of a token to a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void rows_join_kernel(ProductArgs a) {
+    constexpr int kWide = Exchange<Rows::kPB, false>::kWide, kUnits = 32 * kWide / 8;
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, tile = at / kUnits, unit = at % kUnits;
+    if (tile >= a.tiles_m * a.tiles_r) return;
+    const Place w = place_of<Rows, false>(a, tile);
+    const int64_t token = w.m0 + unit / (kWide / 8);
+    const int r = w.r0 + unit % (kWide / 8) * 8;
+    if (token >= a.M || r >= a.R) return;
+    const float *from = a.part + static_cast<int64_t>(tile) * a.split * (32 * kWide) + unit * 8;
+    float sum[8] = {};
+#pragma unroll 4
+    for (uint32_t s = 0; s < a.split; ++s, from += 32 * kWide) {
+        float v[8];
+        load8(from, kChunk, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += v[j];
+    }
+    store8(static_cast<T *>(a.out.p) + token * a.out.ld + r, sum, a.R - r);
 }
 
 // split > 1: the parts of a sum added up in a fixed order, then as above.  A wavefront takes what one of the tile's had of 32 tokens.
@@ -523,16 +656,16 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a) {
         for (int b = 0; b < G::kPB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[b][r] += from[((b * G::kTB + t) * 16 + r) * 64];
-    finish<T, G::kPB, kForward>(a, region, w.m0 + (wave % G::kWT * G::kTB + t) * 32, w.r0 + wave / G::kWT * E::kWide, 1, [&](int) __attribute__((always_inline)) {
+    finish<T, G::kPB, kForward, 1>(a, region, w.m0 + (wave % G::kWT * G::kTB + t) * 32, w.r0 + wave / G::kWT * E::kWide, 1, 0, 1, [&](int) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < G::kPB; ++b) E::put(region, b, acc[b]);
     });
 }
 
-// Launches a tile's kernels.  A launch takes kMost tiles each way at most (it has room for 2^32 threads, and wraps silently beyond).
+// Cuts the result into tiles of G and launches for them.  A launch takes kMost tiles each way at most (it has room for 2^32 threads, and wraps silently beyond).
 constexpr int64_t kMost = 1 << 11;
-template <typename T, typename G, bool kForward>
-int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split, const char *what) {
+template <typename T, typename G, bool kForward, typename Launch>
+int run(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, int64_t split, Launch launch) {
     constexpr int64_t kWide = kForward ? G::kP / 2 : G::kP, kSize = sizeof(T);
     const int64_t tiles_m = (whole.M + G::kTok - 1) / G::kTok, tiles_r = (whole.R + kWide - 1) / kWide;
     const int64_t steps = (kForward ? 1 : 2) * ((static_cast<int64_t>(whole.C) * kSize + kRow - 1) / kRow);
@@ -543,7 +676,8 @@ int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole,
     if (split > 1) {                                                     // (where there are few tiles: one launch)
         OpsScratch &scratch = ops_scratch(ops, s);
         lock = std::unique_lock<std::mutex>(scratch.mu);
-        const int rc = scratch.provide(static_cast<size_t>(tiles_m * tiles_r * split) * G::kP * G::kTok, what);
+        const int rc = scratch.provide(static_cast<size_t>(tiles_m * tiles_r * split) * G::kP * G::kTok,
+                                       kForward ? "gated_linear: partial sums" : "gated_linear_backward: partial sums");
         if (rc != TENSILE_OK) return rc;
         part = scratch.buf.p;
     }
@@ -570,17 +704,41 @@ int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole,
                     a.kept[k].scale += m0 * a.kept[k].ld_scale + r0 / kGroup;
                 }
             }
-            const dim3 grid(a.tiles_m * a.tiles_r * a.split), block(G::kThreads);
-            if (far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, true>), grid, block, 0, s, a);
-            else hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
+            launch(a, dim3(a.tiles_m * a.tiles_r * a.split), a.tiles_m * a.tiles_r);
             TS_HIP(hipGetLastError());
-            if (split > 1) {
-                const uint32_t units = a.tiles_m * a.tiles_r * (G::kTB * G::kWaves);
-                hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3((units + 3) / 4), dim3(256), 0, s, a);
-                TS_HIP(hipGetLastError());
-            }
         }
     return TENSILE_OK;
+}
+
+template <typename T, typename G, bool kForward>
+int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split) {
+    return run<T, G, kForward>(ops, s, whole, split, [&](const ProductArgs &a, dim3 grid, uint32_t tiles) {
+        const dim3 block(G::kThreads);
+        if (far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
+        if (a.split > 1)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3((tiles * (G::kTB * G::kWaves) + 3) / 4), dim3(256), 0, s, a);
+    });
+}
+template <typename T, bool kForward>
+int run_rows(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split, bool four) {
+    return run<T, Rows, kForward>(ops, s, whole, split, [&](const ProductArgs &a, dim3 grid, uint32_t tiles) {
+        auto with = [&](auto waves, auto q) {
+            constexpr int kWaves = decltype(waves)::value, kQ = decltype(q)::value;
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(product_rows_kernel<T, kForward, false, kWaves, kQ>), grid, dim3(64 * kWaves), 0, s, a);
+        };
+        using Two = std::integral_constant<int, 2>;
+        using Four = std::integral_constant<int, 4>;
+        using One = std::integral_constant<int, 1>;
+        if (far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_rows_kernel<T, kForward, true, 4, 4>), grid, dim3(256), 0, s, a);
+        else if (four && a.M <= 8) with(Four{}, One{});
+        else if (four) with(Four{}, Four{});
+        else if (a.M <= 8) with(Two{}, One{});
+        else with(Two{}, Four{});
+        if constexpr (!kForward) {
+            if (a.split > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(rows_join_kernel<T>), dim3(tiles), dim3(256), 0, s, a);
+        }
+    });
 }
 
 // Rows further apart than this are reached by 64-bit addresses only (256 of them, or 32 of a step, from a scalar one).

@@ -46,7 +46,20 @@ __device__ __forceinline__ f32x16 multiply_add(float, u32x4 a, u32x4 b, f32x16 c
     return c;
 }
 
-// Up to 16 bytes of a row, `left` elements of which exist (0 or fewer: none); zeros behind them.
+// 16 bytes of a row of `n` elements (kPer16 at least) from element c on, zeros behind the last one: the load takes what exists, and as many before, which are
+// shifted out.
+template <typename T>
+__device__ __forceinline__ u32x4 load_end(const T *row, int64_t c, int64_t n, bool keep) {
+    constexpr int kPer = kPer16<T>;
+    const int64_t left = n - c;
+    const int over = left < kPer && left > 0 ? kPer - static_cast<int>(left) : 0;
+    u32x4 r;
+    __builtin_memcpy(&r, row + (left > 0 ? c - over : 0), 16);
+    r = shift_out(r, over * static_cast<int>(sizeof(T)));
+    const u32x4 none = {0, 0, 0, 0};
+    return keep && left > 0 ? r : none;
+}
+// The same of any row, element by element.
 template <typename T>
 __device__ __forceinline__ u32x4 load_chunk(const T *p, int64_t left) {
     constexpr int kPer = kPer16<T>;
@@ -428,27 +441,29 @@ struct Steps {
     template <typename Meet>
     __device__ __forceinline__ void rest(int k, int64_t c0, Sums &acc, Meet meet) const {
         meet();
+        auto bring_all = [&](auto load) __attribute__((always_inline)) {
+            u32x4 v[kLoadsP + kLoadsQ];
 #pragma unroll
-        for (int i = 0; i < kLoadsP; ++i) {
-            const Piece c = piece_p(i);
-            u32x4 v;
-            if constexpr (kForward) {
-                const Matrix m = matrix_of(i) ? a.p[1] : a.p[0];
-                v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
-            } else {
-                const Matrix m = k ? a.p[1] : a.p[0];
-                const int64_t row = c0 + c.row;
-                v = load_chunk(static_cast<const T *>(m.p) + row * m.ld + c.col, row < a.C ? a.R - c.col : 0);
+            for (int i = 0; i < kLoadsP; ++i) {
+                const Piece c = piece_p(i);
+                const Matrix m = (kForward ? matrix_of(i) : k) ? a.p[1] : a.p[0];
+                if constexpr (kForward) v[i] = load(static_cast<const T *>(m.p) + c.row * m.ld, c0 + c.col, a.C, true);
+                else v[i] = load(static_cast<const T *>(m.p) + (c0 + c.row < a.C ? c0 + c.row : a.C - 1) * m.ld, c.col, a.R, c0 + c.row < a.C);
             }
-            *reinterpret_cast<u32x4 *>(lds + (wave * kLoadsP + i) * 1024 + lane * 16) = v;
-        }
 #pragma unroll
-        for (int i = 0; i < kLoadsQ; ++i) {
-            const Piece c = piece_q(i);
-            const Matrix m = k ? a.q[1] : a.q[0];
-            const u32x4 v = load_chunk(static_cast<const T *>(m.p) + c.row * m.ld + c0 + c.col, a.C - c0 - c.col);
-            *reinterpret_cast<u32x4 *>(lds + kSlotP + (wave * kLoadsQ + i) * 1024 + lane * 16) = v;
-        }
+            for (int i = 0; i < kLoadsQ; ++i) {
+                const Piece c = piece_q(i);
+                const Matrix m = k ? a.q[1] : a.q[0];
+                v[kLoadsP + i] = load(static_cast<const T *>(m.p) + c.row * m.ld, c0 + c.col, a.C, true);
+            }
+#pragma unroll
+            for (int i = 0; i < kLoadsP; ++i) *reinterpret_cast<u32x4 *>(lds + (wave * kLoadsP + i) * 1024 + lane * 16) = v[i];
+#pragma unroll
+            for (int i = 0; i < kLoadsQ; ++i) *reinterpret_cast<u32x4 *>(lds + kSlotP + (wave * kLoadsQ + i) * 1024 + lane * 16) = v[kLoadsP + i];
+        };
+        // (one load after the other, each behind a question, takes 1 us a load)
+        if (a.C >= kPer && (kForward || a.R >= kPer)) bring_all([](const T *row, int64_t c, int64_t n, bool keep) __attribute__((always_inline)) { return load_end(row, c, n, keep); });
+        else bring_all([](const T *row, int64_t c, int64_t n, bool keep) __attribute__((always_inline)) { return load_chunk(row + c, keep ? n - c : 0); });
         meet();
 #pragma unroll
         for (int e = 0; e < kParts; ++e) {
@@ -459,7 +474,7 @@ struct Steps {
     }
 };
 
-// The whole steps are the splits' by equal parts, the rest is the last one's.
+// The steps, whole ones and behind them the rest, are the splits' by equal parts.
 template <typename T, typename G, bool kForward, bool kFar>
 __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void product_kernel(ProductArgs a) {
     using S = Steps<T, G, kForward, kFar>;
@@ -471,12 +486,14 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
     const S st(a, w, lds, wave);
     typename S::Sums acc = {};
     typename S::Fragments f[2];
-    int begin = 0, end = S::kSums * st.n_whole;                          // (at most 2^25: a step is 32 elements at least)
+    const int whole = S::kSums * st.n_whole, rest_from = st.n_whole * S::kStep, rests = (a.C - rest_from + S::kStep - 1) / S::kStep;
+    int from = 0, to = whole + S::kSums * rests;                         // (at most 2^26: a step is 32 elements at least)
     if (a.split > 1) {                                                   // (a division of 64 bits is some hundred instructions)
-        const int64_t n = end;
-        begin = static_cast<int>(n * w.split / a.split);
-        end = static_cast<int>(n * (w.split + 1) / a.split);
+        const int64_t n = to;
+        from = static_cast<int>(n * w.split / a.split);
+        to = static_cast<int>(n * (w.split + 1) / a.split);
     }
+    const int begin = from, end = to < whole ? to : whole;
     if constexpr (!kFar) {
         // Step s multiplies while step s+1 is on its way.  Behind its barrier every wave has the last fragments of step s in registers and its share of step s+1
         // in the LDS: step s+2 is sent for in the place of step s.
@@ -512,13 +529,9 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             }
         }
     }
-    auto meet = [] { __syncthreads(); };
-    if constexpr (kFar) {
-        const int64_t per = (a.C + S::kStep - 1) / S::kStep, n = per * S::kSums;
-        for (int64_t s = n * w.split / a.split; s < n * (w.split + 1) / a.split; ++s) st.rest(s >= per, (s >= per ? s - per : s) * S::kStep, acc, meet);
-    } else if (w.split == a.split - 1) {
-        for (int k = 0; k < S::kSums; ++k)
-            for (int64_t c0 = static_cast<int64_t>(st.n_whole) * S::kStep; c0 < a.C; c0 += S::kStep) st.rest(k, c0, acc, meet);
+    for (int s = from < whole ? whole : from; s < to; ++s) {
+        const int k = s - whole >= rests;
+        st.rest(k, rest_from + static_cast<int64_t>(s - whole - (k ? rests : 0)) * S::kStep, acc, [] { __syncthreads(); });
     }
     if (a.split > 1) {
         float *const out = a.part + ((static_cast<int64_t>(w.tile) * a.split + w.split) * G::kWaves + wave) * (G::kPB * G::kTB * 1024) + lane;

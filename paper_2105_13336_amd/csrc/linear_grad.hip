@@ -66,14 +66,6 @@ __device__ __forceinline__ void split_bf16(float x, uint32_t (&p)[kPieces]) {
     }
 }
 
-// The 16 bytes moved down by `bytes` (0 .. 15), zeros behind them.
-__device__ __forceinline__ u32x4 shift_out(u32x4 w, int bytes) {
-    const u32x4 two = bytes & 8 ? u32x4{w[2], w[3], 0, 0} : w;
-    const u32x4 one = bytes & 4 ? u32x4{two[1], two[2], two[3], 0} : two;
-    const uint32_t b = bytes & 3;
-    return u32x4{__builtin_amdgcn_alignbyte(one[1], one[0], b), __builtin_amdgcn_alignbyte(one[2], one[1], b),
-                 __builtin_amdgcn_alignbyte(one[3], one[2], b), __builtin_amdgcn_alignbyte(0, one[3], b)};
-}
 // Eight elements without their first n (0 .. 7), zeros behind them; all zero unless `keep`.
 template <typename T>
 __device__ __forceinline__ void drop_front(Raw8<T> &r, int n, bool keep) {

@@ -130,6 +130,15 @@ __device__ __forceinline__ void from_f32(float f, float &x) { x = f; }
 __device__ __forceinline__ void from_f32(float f, bf16_t &x) { x.bits = __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
 __device__ __forceinline__ void from_f32(float f, f16_t &x) { x.bits = __builtin_bit_cast(uint16_t, static_cast<_Float16>(f)); }
 
+// The 16 bytes moved down by `bytes` (0 .. 15), zeros behind them.
+__device__ __forceinline__ u32x4 shift_out(u32x4 w, int bytes) {
+    const u32x4 two = bytes & 8 ? u32x4{w[2], w[3], 0, 0} : w;
+    const u32x4 one = bytes & 4 ? u32x4{two[1], two[2], two[3], 0} : two;
+    const uint32_t b = bytes & 3;
+    return u32x4{__builtin_amdgcn_alignbyte(one[1], one[0], b), __builtin_amdgcn_alignbyte(one[2], one[1], b),
+                 __builtin_amdgcn_alignbyte(one[3], one[2], b), __builtin_amdgcn_alignbyte(0, one[3], b)};
+}
+
 // ------------------------------------------------------------------ checkpoints
 
 __device__ __forceinline__ u32x2 load_q(const int8_t *p, int left) {

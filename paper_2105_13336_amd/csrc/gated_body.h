@@ -94,7 +94,7 @@ struct ProductArgs {
     Ckpt kept[2];
     // how the work is cut: tiles of tokens and features, and the steps of a sum among `split` workgroups a tile
     uint32_t tiles_m, tiles_r, split;
-    float *part;                      // split > 1: [tile][split][wavefront][block][register][lane]
+    float *part;                      // split > 1: [tile][split][gate, up][token][feature]
 };
 
 template <typename T>
@@ -111,6 +111,8 @@ struct Exchange {
     static constexpr int kPitch = kWide + 4;                                           // floats from a token to the next: 16 lanes' 16 bytes lie in different banks
     static constexpr int kBytes = 32 * kPitch * 4 * (kForward ? 2 : 1);                // of a wavefront
     static constexpr int kLanes = kWide / 8, kAtOnce = 64 / kLanes;                    // a token's lanes, tokens at once
+    static constexpr int kPasses = (32 + kAtOnce - 1) / kAtOnce;
+    static constexpr bool kEven = kLanes * kAtOnce == 64 && 32 % kAtOnce == 0;         // every lane has a token in every pass
 
     // Block b of the blocks, as the matrix instructions leave it: a lane has rows 8q + 4 (lane / 32) .. + 3 of token lane % 32.
     static __device__ __forceinline__ void put(float *region, int b, const f32x16 &acc) {
@@ -141,36 +143,90 @@ struct Exchange {
     static __device__ __forceinline__ void order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 };
 
+// Where a token's eight features go, h or dx and their places in the checkpoints.
+template <typename T, bool kForward>
+struct Target {
+    T *out;
+    int8_t *q[2] = {};
+    uint8_t *scale[2] = {};
+    __device__ __forceinline__ Target(const ProductArgs &a, int64_t token, int r) : out(static_cast<T *>(a.out.p) + token * a.out.ld + r) {
+        if constexpr (kForward) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (a.kept[k].q) {
+                    q[k] = a.kept[k].q + token * a.kept[k].ld_q + r;
+                    scale[k] = a.kept[k].scale + token * a.kept[k].ld_scale + r / kGroup;
+                }
+        }
+    }
+    __device__ __forceinline__ void go_on(const ProductArgs &a, int tokens) {
+        out += tokens * a.out.ld;
+        if constexpr (kForward) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (a.kept[k].q) {
+                    q[k] += tokens * a.kept[k].ld_q;
+                    scale[k] += tokens * a.kept[k].ld_scale;
+                }
+        }
+    }
+};
+template <typename T>
+__device__ __forceinline__ void load_bias(const ProductArgs &a, int r, int left, float (&bias)[2][8]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bias[k][j] = a.bias[0] && j < left ? param_at<T>(a.param_type, a.bias[k], r + j) : 0.0f;
+}
+// Gate and up, v and u, of a token's eight features, of which `left` exist (kWhole: all): biases, checkpoints, activation, product.  Four neighbouring lanes
+// hold a group and call this together, `there` or not.
+template <typename T, bool kWhole>
+__device__ __forceinline__ void finish_gated(const ProductArgs &a, float (&v)[8], float (&u)[8], const float (&bias)[2][8], const Target<T, true> &to, int left, bool there) {
+    const int n = kWhole ? kChunk : left;
+    if (a.bias[0]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] += bias[0][j];
+            u[j] += bias[1][j];
+        }
+    }
+    // (Features that do not exist hold copies of the last one, without its bias: they take no part.)
+    if (!kWhole && left < 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j >= left) v[j] = u[j] = 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (!a.kept[k].q) continue;
+        uint32_t code;
+        const u32x2 w = pack8(k ? u : v, static_cast<uint32_t>(a.cap), code);
+        if (there) store_q(to.q[k], w, n);
+        if (there && (threadIdx.x & 3) == 0) *to.scale[k] = static_cast<uint8_t>(code);
+    }
+    auto apply = [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = decltype(act)::template value<kRoundsTo32<T>>(v[j]) * u[j];
+    };
+    if (a.act == TENSILE_SILU) apply(Silu{});
+    else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
+    else apply(Gelu<true>{});
+    if (there) store8(to.out, v, n);
+}
+
 // Tokens from first_token on, 32 at a time, `times` times, and features from r0 on: write(t) puts what belongs to the t-th 32 tokens into the region (kRegions of
 // them: each wavefront's part of the sums).  A wavefront goes through them from pass `start` on, every `stride`-th one.
 template <typename T, int kPB, bool kForward, int kRegions, typename Write>
 __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int64_t first_token, int r0, int times, int start, int stride, Write write) {
     using E = Exchange<kPB, kForward>;
+    static_assert(!kForward || E::kEven, "");
     const int lane = threadIdx.x & 63;
     const int r = r0 + lane % E::kLanes * 8, left = a.R - r;
-    float bias[kForward ? 2 : 1][8] = {};
-    if constexpr (kForward) {
-        if (a.bias[0]) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < left) bias[k][j] = param_at<T>(a.param_type, a.bias[k], r + j);
-        }
-    }
+    float bias[2][8];
+    if constexpr (kForward) load_bias<T>(a, r, left, bias);
     // (Addresses go on by additions: a product of 64 bits for each store is a quarter of all of this.)
     int64_t token = first_token + start * E::kAtOnce + lane / E::kLanes;
-    T *out = static_cast<T *>(a.out.p) + token * a.out.ld + r;
-    int8_t *q[2] = {};
-    uint8_t *scale[2] = {};
-    if constexpr (kForward) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (a.kept[k].q) {
-                q[k] = a.kept[k].q + token * a.kept[k].ld_q + r;
-                scale[k] = a.kept[k].scale + token * a.kept[k].ld_scale + r / kGroup;
-            }
-    }
+    Target<T, kForward> to(a, token, r);
     auto all = [&](auto whole) __attribute__((always_inline)) {
         constexpr bool kWhole = decltype(whole)::value;
 #pragma unroll 1
@@ -179,48 +235,24 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
             write(t);
             E::order();
 #pragma unroll 2
-            for (int pass = start; pass < 32 / E::kAtOnce; pass += stride) {
-                const int in = pass * E::kAtOnce + lane / E::kLanes, n = kWhole ? kChunk : left;
-                const bool there = kWhole || (token < a.M && left > 0);
+            for (int pass = start; pass < E::kPasses; pass += stride) {
+                const int in = pass * E::kAtOnce + lane / E::kLanes;
+                const bool mine = E::kEven || (lane / E::kLanes < E::kAtOnce && in < 32), there = mine && (kWhole || (token < a.M && left > 0));
                 float v[8];
-                E::template get<kRegions>(region, 0, in, v);
+                E::template get<kRegions>(region, 0, mine ? in : 0, v);
                 if constexpr (kForward) {
                     float u[8];
                     E::template get<kRegions>(region, 1, in, u);
-                    if (a.bias[0]) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            v[j] += bias[0][j];
-                            u[j] += bias[1][j];
-                        }
-                    }
-                    // (Rows that do not exist hold copies of the last one, without its bias: they take no part.)
-                    if (!kWhole && left < 8) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j >= left) v[j] = u[j] = 0.0f;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        if (!a.kept[k].q) continue;
-                        uint32_t code;
-                        const u32x2 w = pack8(k ? u : v, static_cast<uint32_t>(a.cap), code);
-                        if (there) store_q(q[k], w, n);
-                        if (there && (lane & 3) == 0) *scale[k] = static_cast<uint8_t>(code);
-                        q[k] += stride * E::kAtOnce * a.kept[k].ld_q;
-                        scale[k] += stride * E::kAtOnce * a.kept[k].ld_scale;
-                    }
-                    auto apply = [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = decltype(act)::template value<kRoundsTo32<T>>(v[j]) * u[j];
-                    };
-                    if (a.act == TENSILE_SILU) apply(Silu{});
-                    else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
-                    else apply(Gelu<true>{});
+                    finish_gated<T, kWhole>(a, v, u, bias, to, left, there);
+                } else if (there) {
+                    store8(to.out, v, kWhole ? kChunk : left);
                 }
-                if (there) store8(out, v, n);
-                out += stride * E::kAtOnce * a.out.ld;
+                to.go_on(a, stride * E::kAtOnce);
                 token += stride * E::kAtOnce;
+            }
+            if constexpr (!E::kEven) {
+                to.go_on(a, 32 - E::kPasses * E::kAtOnce);
+                token += 32 - E::kPasses * E::kAtOnce;
             }
         }
     };
@@ -230,20 +262,44 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
     else all(std::false_type{});
 }
 
+// Where the sums are split: a part's sums as they are, [tile][split][gate, up][token][feature].  base: of the (tile, split)'s first, wide: the tile's features.
+template <int kPB, bool kForward, int kRegions, typename Write>
+__device__ __forceinline__ void leave_part(float *base, int tokens, int wide, int first_token, int r0, float *region, int times, int start, int stride, Write write) {
+    using E = Exchange<kPB, kForward>;
+    static_assert(E::kEven, "");
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (int t = 0; t < times; ++t) {
+        E::order();
+        write(t);
+        E::order();
+#pragma unroll
+        for (int k = 0; k < (kForward ? 2 : 1); ++k)
+#pragma unroll 1
+            for (int pass = start; pass < E::kPasses; pass += stride) {
+                const int in = pass * E::kAtOnce + lane / E::kLanes;
+                float v[8];
+                E::template get<kRegions>(region, k, in, v);
+                store8(base + (k * tokens + first_token + 32 * t + in) * wide + r0 + lane % E::kLanes * 8, v, kChunk);
+            }
+    }
+}
+
 // ------------------------------------------------------------------ tiles
 
 // A workgroup's tile: kWP x kWT wavefronts of 32 kPB rows of the weights x 32 kTB tokens each.  Forward the weights' rows are gate and up by turns, 32 each: the
 // tile is half as many features wide.
-template <int kPB_, int kTB_, int kWP_, int kWT_, int kPerCu_>
+template <int kPB_, int kTB_, int kWP_, int kWT_, int kPerCu_, int kSlots_>
 struct Tile {
-    static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_;
+    static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_, kSlots = kSlots_;   // kSlots: steps in the LDS
     static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
     static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
+    static constexpr bool kSplit = kSlots > 3;                           // sums are split where tiles of this kind are taken
 };
 
 // A step takes kRow bytes of a row, a line of the caches (with half a line to a step the L2 is asked twice as often: it answers a line or half of one in the same
-// time); two steps are in the LDS, kParts fragments long each.
-constexpr int kRow = 128, kSlots = 2, kParts = kRow / 32;
+// time): kParts fragments.
+constexpr int kRow = 128, kParts = kRow / 32;
 
 // Of staged rows the 16-byte chunks are stored in an order that depends on the row, so that 16 rows' chunks of the same number lie in different banks.
 __device__ __forceinline__ int stored_chunk(int row, int chunk) { return chunk ^ (row >> 1 & 7); }
@@ -329,7 +385,8 @@ struct Steps {
         int64_t row;                  // of the matrix (backward, weights: of the step)
         int col;                      // element
     };
-    static __device__ __forceinline__ int turned(int row) { return kRowP >= 256 ? 2 * (row & 3) : 2 * (row >> 1 & 1); }
+    // (rows of a multiple of 256 bytes begin at the same bank, others in the one or the other half of the banks by turns)
+    static __device__ __forceinline__ int turned(int row) { return kRowP % 256 == 0 ? 2 * (row & 3) : 2 * (row >> 1 & 1); }
     __device__ __forceinline__ Piece piece_p(int i) const {
         if constexpr (kForward) {
             const int row = (wave * kLoadsP + i) * 8 + lane / 8, f = r0 + row / 64 * 32 + row % 32;
@@ -479,9 +536,9 @@ template <typename T, typename G, bool kForward, bool kFar>
 __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void product_kernel(ProductArgs a) {
     using S = Steps<T, G, kForward, kFar>;
     using E = Exchange<G::kPB, kForward>;
-    constexpr int kExchange = E::kBytes * G::kWaves;
+    constexpr int kExchange = E::kBytes * G::kWaves, kSlots = G::kSlots, kLoads = S::kLoadsP + S::kLoadsQ;
     __shared__ __attribute__((aligned(1024))) char lds[kSlots * S::kSlot > kExchange ? kSlots * S::kSlot : kExchange];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place w = place<G, kForward>(a);
     const S st(a, w, lds, wave);
     typename S::Sums acc = {};
@@ -495,8 +552,8 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
     }
     const int begin = from, end = to < whole ? to : whole;
     if constexpr (!kFar) {
-        // Step s multiplies while step s+1 is on its way.  Behind its barrier every wave has the last fragments of step s in registers and its share of step s+1
-        // in the LDS: step s+2 is sent for in the place of step s.
+        // Step s multiplies while the kSlots - 1 steps behind it are on their way or there.  Behind its barrier every wave has the last fragments of step s in
+        // registers and its share of step s+1 in the LDS: step s + kSlots is sent for in its place.  At the barrier all but step s+1 may be under way.
         auto step = [&](int s, int slot, auto steady) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < kParts - 1; ++e) {
@@ -504,8 +561,9 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
                 S::multiply(f[e & 1], acc);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            st.read(f[0], 0, slot ^ 1);
+            if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kSlots - 2) * kLoads) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            st.read(f[0], 0, (slot + 1) % kSlots);
             if (decltype(steady)::value || s + kSlots < end) st.bring(s + kSlots, slot);
             S::multiply(f[(kParts - 1) & 1], acc);
             __builtin_amdgcn_sched_barrier(0);
@@ -514,7 +572,7 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
 #pragma unroll
             for (int s = 0; s < kSlots; ++s)
                 if (begin + s < end) st.bring(begin + s, s);
-            if (begin + 1 < end) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(S::kLoadsP + S::kLoadsQ) : "memory");
+            if (begin + kSlots <= end) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kSlots - 1) * kLoads) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
             st.read(f[0], 0, 0);
             int s = begin;
@@ -533,40 +591,38 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
         const int k = s - whole >= rests;
         st.rest(k, rest_from + static_cast<int64_t>(s - whole - (k ? rests : 0)) * S::kStep, acc, [] { __syncthreads(); });
     }
-    if (a.split > 1) {
-        float *const out = a.part + ((static_cast<int64_t>(w.tile) * a.split + w.split) * G::kWaves + wave) * (G::kPB * G::kTB * 1024) + lane;
-#pragma unroll
-        for (int b = 0; b < G::kPB; ++b)
-#pragma unroll
-            for (int t = 0; t < G::kTB; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) out[((b * G::kTB + t) * 16 + r) * 64] = acc[b][t][r];
-        return;
-    }
     __syncthreads();
     float *const region = reinterpret_cast<float *>(lds + wave * E::kBytes);
-    finish<T, G::kPB, kForward, 1>(a, region, w.m0 + st.wave_t * G::kTB * 32, w.r0 + st.wave_p * E::kWide, G::kTB, 0, 1, [&](int t) __attribute__((always_inline)) {
+    auto write = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int tt = 0; tt < G::kTB; ++tt)
             if (t == tt) {
 #pragma unroll
                 for (int b = 0; b < G::kPB; ++b) E::put(region, b, acc[b][tt]);
             }
-    });
+    };
+    if constexpr (G::kSplit) {
+        if (a.split > 1) {
+            leave_part<G::kPB, kForward, 1>(a.part + (static_cast<int64_t>(w.tile) * a.split + w.split) * (G::kP * G::kTok), G::kTok, kForward ? G::kP / 2 : G::kP,
+                                            st.wave_t * G::kTB * 32, st.wave_p * E::kWide, region, G::kTB, 0, 1, write);
+            return;
+        }
+    }
+    finish<T, G::kPB, kForward, 1>(a, region, w.m0 + st.wave_t * G::kTB * 32, w.r0 + st.wave_p * E::kWide, G::kTB, 0, 1, write);
 }
 
 // Up to 32 tokens: the weights are read once and that is what it costs.  A workgroup has 32 features (backward 64), of whose sums each wavefront takes every
 // kWaves-th step, by itself: it brings its own steps, kRing of them, and waits for nobody.  The wavefronts' sums are added up where they go through
 // the LDS.  kQ: loads of eight tokens (more rows of the staged 32 than that are left as they are; their columns of the result are not used).
 constexpr int kRing = 3;
-using Rows = Tile<2, 1, 1, 1, 1>;
+using Rows = Tile<2, 1, 1, 1, 1, kRing>;
 template <typename T, bool kForward, bool kFar, int kWaves, int kQ>
 __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a) {
     using S = Steps<T, Rows, kForward, kFar>;
     using E = Exchange<Rows::kPB, kForward>;
     static_assert(kWaves * E::kBytes <= kWaves * kRing * S::kSlot, "");
     __shared__ __attribute__((aligned(1024))) char lds[kWaves * kRing * S::kSlot];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place w = place<Rows, kForward>(a);
     const S st(a, w, lds + wave * kRing * S::kSlot, 0);
     typename S::Sums acc = {};
@@ -613,66 +669,44 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
 #pragma unroll
     for (int b = 0; b < Rows::kPB; ++b) E::put(reinterpret_cast<float *>(lds + wave * E::kBytes), b, acc[b][0]);
     __syncthreads();
-    if (a.split > 1) {                                                   // (backward: 32 x 64 sums, token by token)
-        if constexpr (!kForward) {
-            float *const out = a.part + (static_cast<int64_t>(w.tile) * a.split + w.split) * (32 * E::kWide);
-            for (int pass = wave; pass < 32 / E::kAtOnce; pass += kWaves) {
-                const int in = pass * E::kAtOnce + lane / E::kLanes;
-                float v[8];
-                E::template get<kWaves>(region, 0, in, v);
-                if (w.m0 + in < a.M) store8(out + in * E::kWide + lane % E::kLanes * 8, v, kChunk);
-            }
-        }
-        return;
-    }
-    finish<T, Rows::kPB, kForward, kWaves>(a, region, w.m0, w.r0, 1, wave, kWaves, [](int) {});
+    if (a.split > 1)
+        leave_part<Rows::kPB, kForward, kWaves>(a.part + (static_cast<int64_t>(w.tile) * a.split + w.split) * (Rows::kP * Rows::kTok), Rows::kTok, E::kWide, 0, 0, region,
+                                                1, wave, kWaves, [](int) {});
+    else finish<T, Rows::kPB, kForward, kWaves>(a, region, w.m0, w.r0, 1, wave, kWaves, [](int) {});
 }
 
-// Backward with split > 1: the parts added up in a fixed order.  Eight columns of a token to a thread.
-template <typename T>
-__global__ __launch_bounds__(256) void rows_join_kernel(ProductArgs a) {
-    constexpr int kWide = Exchange<Rows::kPB, false>::kWide, kUnits = 32 * kWide / 8;
-    const uint32_t at = blockIdx.x * 256 + threadIdx.x, tile = at / kUnits, unit = at % kUnits;
-    if (tile >= a.tiles_m * a.tiles_r) return;
-    const Place w = place_of<Rows, false>(a, tile);
-    const int64_t token = w.m0 + unit / (kWide / 8);
-    const int r = w.r0 + unit % (kWide / 8) * 8;
-    if (token >= a.M || r >= a.R) return;
-    const float *from = a.part + static_cast<int64_t>(tile) * a.split * (32 * kWide) + unit * 8;
-    float sum[8] = {};
-#pragma unroll 4
-    for (uint32_t s = 0; s < a.split; ++s, from += 32 * kWide) {
-        float v[8];
-        load8(from, kChunk, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += v[j];
-    }
-    store8(static_cast<T *>(a.out.p) + token * a.out.ld + r, sum, a.R - r);
-}
-
-// split > 1: the parts of a sum added up in a fixed order, then as above.  A wavefront takes what one of the tile's had of 32 tokens.
+// split > 1: the parts of a sum added up in a fixed order, then as above.  Eight features of a token to a thread.
 template <typename T, typename G, bool kForward>
 __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a) {
-    using E = Exchange<G::kPB, kForward>;
-    constexpr int kUnits = G::kTB * G::kWaves;                           // of a tile
-    __shared__ __attribute__((aligned(16))) char lds[4 * E::kBytes];
-    const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t at = blockIdx.x * 4 + own, tile = at / kUnits;
-    if (tile >= a.tiles_m * a.tiles_r) return;
-    const int unit = static_cast<int>(at - tile * kUnits), wave = unit / G::kTB, t = unit % G::kTB;
+    constexpr int kWide = kForward ? G::kP / 2 : G::kP, kPlane = G::kTok * kWide, kPart = G::kP * G::kTok, kUnits = kPlane / 8;
+    static_assert(kUnits % 256 == 0, "");
+    const uint32_t tile = blockIdx.x / (kUnits / 256);
+    const int unit = blockIdx.x % (kUnits / 256) * 256 + threadIdx.x;
     const Place w = place_of<G, kForward>(a, tile);
-    float *const region = reinterpret_cast<float *>(lds + own * E::kBytes);
-    f32x16 acc[G::kPB] = {};
-    const float *from = a.part + (static_cast<int64_t>(tile) * a.split * G::kWaves + wave) * (G::kPB * G::kTB * 1024) + lane;
-    for (uint32_t s = 0; s < a.split; ++s, from += G::kWaves * G::kPB * G::kTB * 1024)
+    const int64_t token = w.m0 + unit / (kWide / 8);
+    const int r = w.r0 + unit % (kWide / 8) * 8, left = a.R - r;
+    const bool there = token < a.M && left > 0;
+    float sum[2][8] = {};
+    if (there) {                                                         // (four parts' loads under way)
+        const float *from = a.part + static_cast<int64_t>(tile) * a.split * kPart + unit * 8;
+#pragma unroll 4
+        for (uint32_t s = 0; s < a.split; ++s, from += kPart)
 #pragma unroll
-        for (int b = 0; b < G::kPB; ++b)
+            for (int k = 0; k < (kForward ? 2 : 1); ++k) {
+                float v[8];
+                load8(from + k * kPlane, kChunk, v);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[b][r] += from[((b * G::kTB + t) * 16 + r) * 64];
-    finish<T, G::kPB, kForward, 1>(a, region, w.m0 + (wave % G::kWT * G::kTB + t) * 32, w.r0 + wave / G::kWT * E::kWide, 1, 0, 1, [&](int) __attribute__((always_inline)) {
-#pragma unroll
-        for (int b = 0; b < G::kPB; ++b) E::put(region, b, acc[b]);
-    });
+                for (int j = 0; j < 8; ++j) sum[k][j] += v[j];
+            }
+    }
+    const Target<T, kForward> to(a, token, r);
+    if constexpr (kForward) {
+        float bias[2][8];
+        load_bias<T>(a, r, left, bias);
+        finish_gated<T, false>(a, sum[0], sum[1], bias, to, left, there);
+    } else if (there) {
+        store8(to.out, sum[0], left);
+    }
 }
 
 // Cuts the result into tiles of G and launches for them.  A launch takes kMost tiles each way at most (it has room for 2^32 threads, and wraps silently beyond).
@@ -724,13 +758,15 @@ int run(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, int64
 }
 
 template <typename T, typename G, bool kForward>
-int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split) {
+int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split = 1) {
     return run<T, G, kForward>(ops, s, whole, split, [&](const ProductArgs &a, dim3 grid, uint32_t tiles) {
         const dim3 block(G::kThreads);
         if (far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, true>), grid, block, 0, s, a);
         else hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
-        if (a.split > 1)
-            hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3((tiles * (G::kTB * G::kWaves) + 3) / 4), dim3(256), 0, s, a);
+        if constexpr (G::kSplit) {
+            if (a.split > 1)
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3(tiles * (G::kTok * G::kP / (kForward ? 4096 : 2048))), dim3(256), 0, s, a);
+        }
     });
 }
 template <typename T, bool kForward>
@@ -749,7 +785,7 @@ int run_rows(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, 
         else if (a.M <= 8) with(Two{}, One{});
         else with(Two{}, Four{});
         if constexpr (!kForward) {
-            if (a.split > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(rows_join_kernel<T>), dim3(tiles), dim3(256), 0, s, a);
+            if (a.split > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, Rows, false>), dim3(tiles), dim3(256), 0, s, a);
         }
     });
 }
@@ -758,8 +794,28 @@ int run_rows(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, 
 constexpr int64_t kFarBytes = 1 << 23;
 inline bool is_far(const Matrix &m, int64_t size) { return m.ld * size >= kFarBytes; }
 
-using Large = Tile<4, 2, 2, 4, 1>;    // 256 x 256
-using Small = Tile<2, 2, 2, 2, 2>;    // 128 x 128
+using Large = Tile<4, 2, 2, 4, 1, 2>;    // 256 x 256
+using Middle = Tile<3, 1, 2, 4, 1, 3>;   // 192 x 128
+using Small = Tile<2, 2, 2, 2, 2, 2>;    // 128 x 128
+using Few = Tile<2, 2, 2, 2, 1, 4>;      // 128 x 128, for splits: four steps in the LDS
+
+inline int64_t rounds(int64_t tiles, int64_t places) { return (tiles + places - 1) / places; }
+template <typename T, bool kForward>
+int64_t steps_of(const ProductArgs &a) {
+    return (kForward ? 1 : 2) * rounds(static_cast<int64_t>(a.C) * static_cast<int64_t>(sizeof(T)), kRow);
+}
+// Few tiles: their sums are split until the card is full, but not below 12 steps (adding up is another launch, 4 us).  1, 2, 4 and 8 parts, us:
+// backward 64 x 4096 x 10944 (32 tiles, 342 steps) 142, 82, 51, 44; 512 x 768 x 2048 (24, 64) 37, 28, 22, 22; 301 x 1000 x 1500 f16 (24, 48) 38, 30, 26.5, 26;
+// forward 64 x 4096 x 2048 (32, 64) 35, 25, 20, 21; 301 x 1000 x 1500 (72, 16) 17, 19, 26; 64 x 4096 x 10944 (171, 64) 47, 61.
+inline int64_t parts_of(int64_t tiles, int64_t places, int64_t steps) {
+    const int64_t fill = places / tiles, most = steps / 12;
+    return fill < most ? fill : most;
+}
+template <typename G, bool kForward>
+int64_t tiles_of(const ProductArgs &a) {
+    constexpr int64_t kWide = kForward ? G::kP / 2 : G::kP;
+    return ((a.M + G::kTok - 1) / G::kTok) * ((a.R + kWide - 1) / kWide);
+}
 
 }  // namespace
 

@@ -398,6 +398,18 @@ def test_gated_backward(ops, dtype, M, K, F):
 def test_gated_backward_of_many_tokens(ops, dtype, F):
     check_gated_backward(ops, dtype, 4_100, 3_999, F, odd=True)
     check_gated_backward(ops, dtype, 4_096, 4_096, F)
+    check_gated_backward(ops, dtype, 8_190, 767, F)    # (tiles of 192 columns)
+    check_gated_backward(ops, dtype, 8_192, 768, F, act="gelu")
+    check_gated_backward(ops, dtype, 2_049, 2_100, F)  # (... of 128)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gated_with_split_sums(ops, dtype):
+    """Few tiles and long sums, of which the last step is a part of one, or there is none."""
+    for M, K, F in ((40, 1_700, 100), (64, 2_048, 64), (200, 3_001, 130)):
+        check_gated(ops, dtype, M, K, F, act="gelu", bias="f32")
+        check_gated_backward(ops, dtype, M, F, K, act="gelu")
+        check_gated_backward(ops, dtype, M, F, K, odd=True)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -543,7 +555,7 @@ def test_captured_and_replayed(ops, M, K, F):
 
 def test_two_graphs_and_eager_calls_side_by_side(ops):
     """Graphs of one handle captured on one stream, launched on two, beside eager calls on a third: each has scratch memory of its own."""
-    M, K, F = 100, 1_024, 96                           # (split sums, forward and backward)
+    M, K, F = 100, 2_048, 1_024                        # (split sums, forward and backward)
     p, x, dy = setting(M, K, F)
     want = outputs(M, K, F)
     block(ops, want, p, x, dy, kept(M, K, F))
@@ -570,7 +582,7 @@ def test_two_graphs_and_eager_calls_side_by_side(ops):
 def test_threads_and_streams_share_a_handle(ops):
     import threading
     jobs = []
-    for k, (M, K, F) in enumerate(((100, 1_024, 96), (7, 500, 200), (300, 300, 300))):
+    for k, (M, K, F) in enumerate(((100, 2_048, 1_024), (7, 500, 200), (300, 300, 300))):
         p, x, dy = setting(M, K, F, k)
         want = outputs(M, K, F)
         block(ops, want, p, x, dy, kept(M, K, F))
@@ -614,8 +626,8 @@ def test_rows_too_far_apart_for_32_bits(ops):
 
 def test_refused_allocation_is_an_error_and_the_next_call_works(tuning):
     h = P.tensile_ops_create()
-    p, x, dy = setting(100, 1_024, 96)
-    o, c = outputs(100, 1_024, 96), kept(100, 1_024, 96)
+    p, x, dy = setting(100, 2_048, 1_024)
+    o, c = outputs(100, 2_048, 1_024), kept(100, 2_048, 1_024)
     tuning("alloc_fail", 1)
     with pytest.raises(P.TensileError) as e:
         P.tensile_gated_linear(h, x, p["wg"], p["wu"], o["h"])

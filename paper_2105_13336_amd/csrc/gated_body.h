@@ -361,6 +361,24 @@ struct Steps {
         u32x4 p[kPB], q[kTB];
     };
     using Sums = f32x16[kPB][kTB];
+    // In 32 bits nothing is rounded but the sums themselves: every step's is taken by itself and then added to the others', so that a term passes through 32 +
+    // (steps) roundings instead of one for every term behind it.  (In 16 bits a matrix instruction adds 16 products at once, and results are rounded to 16 bits.)
+    static constexpr bool kByStep = sizeof(T) == 4;
+    static __device__ __forceinline__ void add_step(Sums &acc, Sums &total) {
+        if constexpr (kByStep) {
+#pragma unroll
+            for (int b = 0; b < kPB; ++b)
+#pragma unroll
+                for (int t = 0; t < kTB; ++t) {
+                    total[b][t] += acc[b][t];
+                    acc[b][t] = f32x16{};
+                }
+        }
+    }
+    static __device__ __forceinline__ const Sums &result(const Sums &acc, const Sums &total) {
+        if constexpr (kByStep) return total;
+        else return acc;
+    }
 
     __device__ __forceinline__ Steps(const ProductArgs &args, const Place &w, char *slots, int number)
         : a(args), lds(slots), m0(w.m0), r0(w.r0), lane(threadIdx.x & 63), wave(number), wave_p(number / G::kWT), wave_t(number % G::kWT) {
@@ -541,7 +559,7 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place w = place<G, kForward>(a);
     const S st(a, w, lds, wave);
-    typename S::Sums acc = {};
+    typename S::Sums acc = {}, total = {};
     typename S::Fragments f[2];
     const int whole = S::kSums * st.n_whole, rest_from = st.n_whole * S::kStep, rests = (a.C - rest_from + S::kStep - 1) / S::kStep;
     int from = 0, to = whole + S::kSums * rests;                         // (at most 2^26: a step is 32 elements at least)
@@ -566,6 +584,7 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             st.read(f[0], 0, (slot + 1) % kSlots);
             if (decltype(steady)::value || s + kSlots < end) st.bring(s + kSlots, slot);
             S::multiply(f[(kParts - 1) & 1], acc);
+            S::add_step(acc, total);
             __builtin_amdgcn_sched_barrier(0);
         };
         if (begin < end) {
@@ -590,7 +609,9 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
     for (int s = from < whole ? whole : from; s < to; ++s) {
         const int k = s - whole >= rests;
         st.rest(k, rest_from + static_cast<int64_t>(s - whole - (k ? rests : 0)) * S::kStep, acc, [] { __syncthreads(); });
+        S::add_step(acc, total);
     }
+    const typename S::Sums &sums = S::result(acc, total);
     __syncthreads();
     float *const region = reinterpret_cast<float *>(lds + wave * E::kBytes);
     auto write = [&](int t) __attribute__((always_inline)) {
@@ -598,7 +619,7 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
         for (int tt = 0; tt < G::kTB; ++tt)
             if (t == tt) {
 #pragma unroll
-                for (int b = 0; b < G::kPB; ++b) E::put(region, b, acc[b][tt]);
+                for (int b = 0; b < G::kPB; ++b) E::put(region, b, sums[b][tt]);
             }
     };
     if constexpr (G::kSplit) {
@@ -625,11 +646,11 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Place w = place<Rows, kForward>(a);
     const S st(a, w, lds + wave * kRing * S::kSlot, 0);
-    typename S::Sums acc = {};
+    typename S::Sums acc = {}, total = {};
     if constexpr (!kFar) {
         // the wavefront's steps: first, first + stride, ... : n of them
-        const int stride = kWaves * static_cast<int>(a.split), first = static_cast<int>(w.split) * kWaves + wave, total = S::kSums * st.n_whole;
-        const int n = total > first ? (total - first + stride - 1) / stride : 0;
+        const int stride = kWaves * static_cast<int>(a.split), first = static_cast<int>(w.split) * kWaves + wave, whole = S::kSums * st.n_whole;
+        const int n = whole > first ? (whole - first + stride - 1) / stride : 0;
         auto step = [&](int i, int slot, auto steady) __attribute__((always_inline)) {
             if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRing - 1) * (S::kLoadsP + kQ)) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -640,6 +661,7 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
                 if (e + 1 < kParts) st.read(f[(e + 1) & 1], e + 1, slot);
                 S::multiply(f[e & 1], acc);
             }
+            S::add_step(acc, total);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (decltype(steady)::value || i + kRing < n) st.template bring<kQ>(first + (i + kRing) * stride, slot);
         };
@@ -661,13 +683,15 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
     {
         const int64_t c0 = static_cast<int64_t>(st.n_whole) * S::kStep, per = (a.C - c0 + S::kStep - 1) / S::kStep, n = per * S::kSums;
         const int64_t stride = static_cast<int64_t>(kWaves) * a.split;
-        for (int64_t s = (static_cast<int64_t>(w.split) * kWaves + wave + stride - S::kSums * static_cast<int64_t>(st.n_whole) % stride) % stride; s < n; s += stride)
+        for (int64_t s = (static_cast<int64_t>(w.split) * kWaves + wave + stride - S::kSums * static_cast<int64_t>(st.n_whole) % stride) % stride; s < n; s += stride) {
             st.rest(s >= per, c0 + (s >= per ? s - per : s) * S::kStep, acc, [] { E::order(); });
+            S::add_step(acc, total);
+        }
     }
     __syncthreads();
     float *const region = reinterpret_cast<float *>(lds);
 #pragma unroll
-    for (int b = 0; b < Rows::kPB; ++b) E::put(reinterpret_cast<float *>(lds + wave * E::kBytes), b, acc[b][0]);
+    for (int b = 0; b < Rows::kPB; ++b) E::put(reinterpret_cast<float *>(lds + wave * E::kBytes), b, S::result(acc, total)[b][0]);
     __syncthreads();
     if (a.split > 1)
         leave_part<Rows::kPB, kForward, kWaves>(a.part + (static_cast<int64_t>(w.tile) * a.split + w.split) * (Rows::kP * Rows::kTok), Rows::kTok, E::kWide, 0, 0, region,

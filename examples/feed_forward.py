@@ -6,11 +6,17 @@ Forward keeps of every norm the normalised rows (8 bits) and of every GELU its i
 reads them as they are: the norm's backward pass, the GELU's (which makes the checkpoint of `a` that W2's gradient needs), and
 the weight gradients - that of W1 from the checkpoint of the norm in front of it.  The products with the weights are torch's.
 
+With --gated the blocks are gated ones, with a root-mean-square norm in front of each and the residual path beside it:
+
+    n = norm(s);  a = silu(n Wg^T) * (n Wu^T);  s' = s + a W2^T                 (and a last norm behind them)
+
+of which the norm's rows and both projections are kept in 8 bits; Wg and Wu are the halves of one matrix, W1, and have one gradient.
+
 Every operator of the iteration is recorded with the tensors that it reads and makes, their sizes and its time: the tensor
 access sequence for which the planner then decides what has to leave the GPU.  The same iteration with 16-bit activations
-(kept: the norm's sum and output, u and a) is recorded next to it.
+(kept: the norm's sum and output, the projections and a) is recorded next to it.
 
-    python examples/feed_forward.py [--layers 12 --tokens 8192 --hidden 768 --ffn 3072]
+    python examples/feed_forward.py [--layers 12 --tokens 8192 --hidden 768 --ffn 3072] [--gated]
 """
 from __future__ import annotations
 
@@ -181,6 +187,114 @@ class FeedForward:
             self.p[n].sub_((rate * g.float()).to(self.p[n].dtype))
 
 
+class GatedFeedForward(FeedForward):
+    """The same of gated blocks: W1 [2 * ffn, hidden] is Wg above Wu."""
+
+    def __init__(self, layers: int, hidden: int, ffn: int, seed: int = 0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        w = lambda n, k: (torch.randn(n, k, generator=gen, device="cuda") * k ** -0.5).bfloat16()
+        self.layers, self.hidden, self.ffn, self.ops = layers, hidden, ffn, P.tensile_ops_create()
+        self.no_beta = torch.zeros(hidden, device="cuda")
+        self.p = {}
+        for l in range(layers):
+            self.p |= {f"w1.{l}": w(2 * ffn, hidden), f"w2.{l}": w(hidden, ffn)}
+        for l in range(layers + 1):
+            self.p[f"g.{l}"] = torch.ones(hidden, device="cuda")
+
+    def _in_8_bits(self, rec, p, ops, x, target):
+        M, L, F = x.shape[0], self.layers, self.ffn
+        new = lambda n, dtype=x.dtype: torch.empty(M, n, dtype=dtype, device="cuda")
+        like = lambda n: torch.empty_like(p[n])
+
+        def norm(l, v, s):
+            n, t, c, rstd = new(self.hidden), new(self.hidden), P.Checkpoint.empty(M, self.hidden), torch.empty(M, device="cuda")
+            P.tensile_rms_norm(ops, v, p[f"g.{l}"], n, eps=EPS, residual=s, total=None if s is None else t, xhat=c, rstd=rstd)
+            return (n, c, rstd) if s is None else (n, c, rstd, t)
+
+        def gated(l, n):
+            a, g, u = new(F), P.Checkpoint.empty(M, F), P.Checkpoint.empty(M, F)
+            P.tensile_gated_linear(ops, n, p[f"w1.{l}"][:F], p[f"w1.{l}"][F:], a, gate=g, up=u)
+            return a, g, u
+
+        def gated_backward(l, da, g, u):
+            d, dn, a8 = new(2 * F), new(self.hidden), P.Checkpoint.empty(M, F)
+            P.tensile_gated_linear_backward(ops, da, g, u, d[:, :F], d[:, F:], w_gate=p[f"w1.{l}"][:F], w_up=p[f"w1.{l}"][F:], dx=dn, h_ckpt=a8)
+            return d, dn, a8
+
+        def norm_backward(l, dn, ds):
+            dx, dg = torch.empty_like(dn), like(f"g.{l}")
+            P.tensile_rms_norm_backward(ops, dn, xhat[l], rstd[l], p[f"g.{l}"], dx, dg, dresidual=ds)
+            return dx, dg
+
+        def weight(name, dy, c, gamma=None):
+            dw = like(name)
+            P.tensile_linear_grad(ops, dy, c, dw, gamma=gamma, beta=None if gamma is None else self.no_beta)
+            return dw
+
+        xhat, rstd, g8, u8 = {}, {}, {}, {}
+        s = x
+        n, xhat[0], rstd[0] = rec.op(["x", "g.0"], ["n.0", "xhat.0", "rstd.0"], lambda: norm(0, x, None))
+        for l in range(L):
+            a, g8[l], u8[l] = rec.op([f"n.{l}", f"w1.{l}"], [f"a.{l}", f"g8.{l}", f"u8.{l}"], lambda: gated(l, n))
+            v = rec.op([f"a.{l}", f"w2.{l}"], [f"v.{l}"], lambda: a @ p[f"w2.{l}"].t())
+            n, xhat[l + 1], rstd[l + 1], s = rec.op([f"v.{l}", f"s.{l}" if l else "x", f"g.{l + 1}"], [f"n.{l + 1}", f"xhat.{l + 1}", f"rstd.{l + 1}", f"s.{l + 1}"],
+                                                    lambda: norm(l + 1, v, s))
+            del a, v
+        rec.ids[f"h.{L}"] = rec.ids[f"n.{L}"]
+        loss, dh = self._loss(rec, n, target)
+        grads = {}
+        ds, grads[f"g.{L}"] = rec.op([f"dh.{L}", f"xhat.{L}", f"rstd.{L}", f"g.{L}"], [f"ds.{L}", f"dg.{L}"], lambda: norm_backward(L, dh, None))
+        for l in reversed(range(L)):
+            da = rec.op([f"ds.{l + 1}", f"w2.{l}"], [f"da.{l}"], lambda: ds @ p[f"w2.{l}"])
+            d, dn, a8 = rec.op([f"da.{l}", f"g8.{l}", f"u8.{l}", f"w1.{l}"], [f"d.{l}", f"dn.{l}", f"a8.{l}"], lambda: gated_backward(l, da, g8.pop(l), u8.pop(l)))
+            grads[f"w2.{l}"] = rec.op([f"ds.{l + 1}", f"a8.{l}"], [f"dw2.{l}"], lambda: weight(f"w2.{l}", ds, a8))
+            grads[f"w1.{l}"] = rec.op([f"d.{l}", f"xhat.{l}", f"g.{l}"], [f"dw1.{l}"], lambda: weight(f"w1.{l}", d, xhat[l], p[f"g.{l}"]))
+            ds, grads[f"g.{l}"] = rec.op([f"dn.{l}", f"ds.{l + 1}", f"xhat.{l}", f"rstd.{l}", f"g.{l}"], [f"ds.{l}", f"dg.{l}"], lambda: norm_backward(l, dn, ds))
+            del da, d, dn, a8
+        return loss, grads
+
+    def _in_16_bits(self, rec, p, ops, x, target):
+        """The same with torch's operators, what backward needs kept as it is."""
+        L, F = self.layers, self.ffn
+        s, n, rstd, both, a = {0: x}, {}, {}, {}, {}
+
+        def norm(l, v, r):
+            total = v if r is None else v + r
+            rs = torch.rsqrt(total.float().square().mean(1, keepdim=True) + EPS)
+            y = (total * rs * p[f"g.{l}"]).to(x.dtype)
+            return (y, rs) if r is None else (y, rs, total)
+
+        def norm_backward(l, dn, ds):
+            xhat, t = s[l].float() * rstd[l], dn.float() * p[f"g.{l}"]
+            dx = rstd[l] * (t - xhat * (t * xhat).mean(1, keepdim=True))
+            return (dx if ds is None else dx + ds).to(x.dtype), (dn * xhat).sum(0)
+
+        def gated_backward(l, da):
+            g, u = both[l][:, :F], both[l][:, F:]
+            d = torch.cat([torch.ops.aten.silu_backward(da * u, g), da * torch.nn.functional.silu(g)], 1)
+            return d, d @ p[f"w1.{l}"]
+
+        n[0], rstd[0] = rec.op(["x", "g.0"], ["n.0", "rstd.0"], lambda: norm(0, x, None))
+        for l in range(L):
+            both[l] = rec.op([f"n.{l}", f"w1.{l}"], [f"both.{l}"], lambda: n[l] @ p[f"w1.{l}"].t())
+            a[l] = rec.op([f"both.{l}"], [f"a.{l}"], lambda: torch.nn.functional.silu(both[l][:, :F]) * both[l][:, F:])
+            v = rec.op([f"a.{l}", f"w2.{l}"], [f"v.{l}"], lambda: a[l] @ p[f"w2.{l}"].t())
+            n[l + 1], rstd[l + 1], s[l + 1] = rec.op([f"v.{l}", f"s.{l}" if l else "x", f"g.{l + 1}"], [f"n.{l + 1}", f"rstd.{l + 1}", f"s.{l + 1}"],
+                                                     lambda: norm(l + 1, v, s[l]))
+        rec.ids[f"h.{L}"] = rec.ids[f"n.{L}"]
+        loss, dh = self._loss(rec, n[L], target)
+        grads = {}
+        ds, grads[f"g.{L}"] = rec.op([f"dh.{L}", f"s.{L}" if L else "x", f"rstd.{L}", f"g.{L}"], [f"ds.{L}", f"dg.{L}"], lambda: norm_backward(L, dh, None))
+        for l in reversed(range(L)):
+            da = rec.op([f"ds.{l + 1}", f"w2.{l}"], [f"da.{l}"], lambda: ds @ p[f"w2.{l}"])
+            grads[f"w2.{l}"] = rec.op([f"ds.{l + 1}", f"a.{l}"], [f"dw2.{l}"], lambda: ds.t() @ a[l])
+            d, dn = rec.op([f"da.{l}", f"both.{l}", f"w1.{l}"], [f"d.{l}", f"dn.{l}"], lambda: gated_backward(l, da))
+            grads[f"w1.{l}"] = rec.op([f"d.{l}", f"n.{l}"], [f"dw1.{l}"], lambda: d.t() @ n[l])
+            ds, grads[f"g.{l}"] = rec.op([f"dn.{l}", f"ds.{l + 1}", f"s.{l}" if l else "x", f"rstd.{l}", f"g.{l}"], [f"ds.{l}", f"dg.{l}"],
+                                         lambda: norm_backward(l, dn, ds))
+        return loss, grads
+
+
 def plan(tas: TAS, budget: int) -> dict:
     """The planner's swaps for the recorded iteration, until it fits the budget or nothing more can be done."""
     h = P.tas_load(tas)
@@ -195,8 +309,9 @@ def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     for name, value in (("layers", 12), ("tokens", 8192), ("hidden", 768), ("ffn", 3072), ("steps", 5)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--gated", action="store_true")
     args = ap.parse_args()
-    model = FeedForward(args.layers, args.hidden, args.ffn)
+    model = (GatedFeedForward if args.gated else FeedForward)(args.layers, args.hidden, args.ffn)
     gen = torch.Generator(device="cuda").manual_seed(1)
     x, target = (torch.randn(args.tokens, args.hidden, generator=gen, device="cuda").bfloat16() for _ in range(2))
     grads, sequences = {}, {}

@@ -10,14 +10,14 @@ int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
     const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
     if (a.M <= 32) return run_rows<T, true>(ops, s, a, far, 1, (a.R + 31) / 32 <= ops->num_cus);
     const int64_t cus = ops->num_cus, small = tiles_of<Small, true>(a);
-    if (small <= cus) return run_tiles<T, Few, true>(ops, s, a, far, parts_of(small, cus, steps_of<T, true>(a)));
+    if (small <= cus || far) return run_tiles<T, Few, true>(ops, s, a, far, parts_of(small, cus, steps_of<T, true>(a)));
     // A round of tiles, as many as the card has places for, takes 1 where they are large and 0.65 where they are small (two to a CU).  Large and small (us, with
     // checkpoints): 8192 x 4096 x 10944 1180 and 1450; 8192 x 768 x 2048 67 and 81; 4096 x 768 x 2048 33 and 37; 2048 x 768 x 2048 28 and 20.
     // (In 32 bits, where the matrix instructions take 16 times as long, small tiles do, which have the registers to add up by steps.)
     if constexpr (sizeof(T) == 2) {
-        if (20 * rounds(tiles_of<Large, true>(a), cus) <= 13 * rounds(small, 2 * cus)) return run_tiles<T, Large, true>(ops, s, a, far);
+        if (20 * rounds(tiles_of<Large, true>(a), cus) <= 13 * rounds(small, 2 * cus)) return run_tiles<T, Large, true>(ops, s, a);
     }
-    return run_tiles<T, Small, true>(ops, s, a, far);
+    return run_tiles<T, Small, true>(ops, s, a);
 }
 
 }  // namespace

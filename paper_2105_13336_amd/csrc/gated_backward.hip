@@ -49,16 +49,16 @@ int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
         return run_rows<T, false>(ops, s, a, far, split, tiles * split <= ops->num_cus);
     }
     const int64_t cus = ops->num_cus, small = tiles_of<Small, false>(a);
-    if (small <= cus) return run_tiles<T, Few, false>(ops, s, a, far, parts_of(small, cus, steps_of<T, false>(a)));
+    if (small <= cus || far) return run_tiles<T, Few, false>(ops, s, a, far, parts_of(small, cus, steps_of<T, false>(a)));
     // A round of tiles, as many as the card has places for, takes 1 where they are large, 0.47 of middle size and 0.65 where they are small (two to a CU).
     // Large, middle and small (us, dx alone): 8192 x 4096 x 10944 1113, 1497 and 1442; 8192 x 768 x 2048 88, 52 and 58.
     // (In 32 bits, where the matrix instructions take 16 times as long, small tiles do, which have the registers to add up by steps.)
     if constexpr (sizeof(T) == 2) {
         const int64_t l = 100 * rounds(tiles_of<Large, false>(a), cus), m = 47 * rounds(tiles_of<Middle, false>(a), cus), n = 65 * rounds(small, 2 * cus);
-        if (l <= m && l <= n) return run_tiles<T, Large, false>(ops, s, a, far);
-        if (m <= n) return run_tiles<T, Middle, false>(ops, s, a, far);
+        if (l <= m && l <= n) return run_tiles<T, Large, false>(ops, s, a);
+        if (m <= n) return run_tiles<T, Middle, false>(ops, s, a);
     }
-    return run_tiles<T, Small, false>(ops, s, a, far);
+    return run_tiles<T, Small, false>(ops, s, a);
 }
 
 }  // namespace

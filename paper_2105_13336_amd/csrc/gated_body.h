@@ -85,6 +85,7 @@ struct ProductArgs {
     int64_t M;                        // tokens
     int32_t C;                        // length of a sum (backward: of each of the two)
     int32_t R;                        // features of the result
+    int32_t n_whole;                  // steps of a sum that can be brought whole (of each of the two)
     Matrix q[2];                      // tokens x C: x, or dgate and dup
     Matrix p[2];                      // Wg, Wu: R x C forward, C x R backward
     // forward
@@ -294,7 +295,7 @@ struct Tile {
     static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_, kSlots = kSlots_;   // kSlots: steps in the LDS
     static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
     static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
-    static constexpr bool kSplit = kSlots > 3;                           // sums are split where tiles of this kind are taken
+    static constexpr bool kSplit = kSlots > 3;                           // what is split, or far, takes tiles of this kind
 };
 
 // A step takes kRow bytes of a row, a line of the caches (with half a line to a step the L2 is asked twice as often: it answers a line or half of one in the same
@@ -354,8 +355,6 @@ struct Steps {
     char *const lds;
     const int64_t m0;
     const int r0, lane, wave, wave_p, wave_t;
-    int n_whole = 0;                  // whole steps (backward: of each sum)
-
     // What a lane multiplies of a part of a step, and the sums.  (Not members: the compiler would keep them in memory.)
     struct Fragments {
         u32x4 p[kPB], q[kTB];
@@ -382,16 +381,6 @@ struct Steps {
 
     __device__ __forceinline__ Steps(const ProductArgs &args, const Place &w, char *slots, int number)
         : a(args), lds(slots), m0(w.m0), r0(w.r0), lane(threadIdx.x & 63), wave(number), wave_p(number / G::kWT), wave_t(number % G::kWT) {
-        if constexpr (!kFar) {
-            if constexpr (kForward) {
-                n_whole = a.C / kStep;
-            } else {
-                // A load of columns reads what lies behind the row's last one, up to the end of the row's last chunk: not where that is behind the matrix.
-                const int64_t least = a.p[0].ld < a.p[1].ld ? a.p[0].ld : a.p[1].ld;
-                const int64_t behind = a.R % kPer == 0 ? 0 : (kPer - 1 + least - 1) / least;   // rows at the end that are not read whole
-                n_whole = a.C > behind ? static_cast<int>((a.C - behind) / kStep) : 0;
-            }
-        }
         places();
         if constexpr (!kFar) offsets();
     }
@@ -446,8 +435,8 @@ struct Steps {
     // Step s, of 2 * n_whole backward (gate, then up); kQ: of the tokens' loads the first ones only
     template <int kQ = kLoadsQ>
     __device__ __forceinline__ void bring(int s, int slot) const {
-        const bool second = !kForward && s >= n_whole;
-        const int64_t at = static_cast<int64_t>(second ? s - n_whole : s) * kStep;
+        const bool second = !kForward && s >= a.n_whole;
+        const int64_t at = static_cast<int64_t>(second ? s - a.n_whole : s) * kStep;
         const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char *)lds)) + slot * kSlot;
         if constexpr (kForward) {
 #pragma unroll
@@ -561,7 +550,7 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
     const S st(a, w, lds, wave);
     typename S::Sums acc = {}, total = {};
     typename S::Fragments f[2];
-    const int whole = S::kSums * st.n_whole, rest_from = st.n_whole * S::kStep, rests = (a.C - rest_from + S::kStep - 1) / S::kStep;
+    const int whole = S::kSums * a.n_whole, rest_from = a.n_whole * S::kStep, rests = (a.C - rest_from + S::kStep - 1) / S::kStep;
     int from = 0, to = whole + S::kSums * rests;                         // (at most 2^26: a step is 32 elements at least)
     if (a.split > 1) {                                                   // (a division of 64 bits is some hundred instructions)
         const int64_t n = to;
@@ -649,7 +638,7 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
     typename S::Sums acc = {}, total = {};
     if constexpr (!kFar) {
         // the wavefront's steps: first, first + stride, ... : n of them
-        const int stride = kWaves * static_cast<int>(a.split), first = static_cast<int>(w.split) * kWaves + wave, whole = S::kSums * st.n_whole;
+        const int stride = kWaves * static_cast<int>(a.split), first = static_cast<int>(w.split) * kWaves + wave, whole = S::kSums * a.n_whole;
         const int n = whole > first ? (whole - first + stride - 1) / stride : 0;
         auto step = [&](int i, int slot, auto steady) __attribute__((always_inline)) {
             if constexpr (decltype(steady)::value) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRing - 1) * (S::kLoadsP + kQ)) : "memory");
@@ -681,10 +670,12 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
     }
     // (the rest goes on in turn behind the whole steps: kFar all of it)
     {
-        const int64_t c0 = static_cast<int64_t>(st.n_whole) * S::kStep, per = (a.C - c0 + S::kStep - 1) / S::kStep, n = per * S::kSums;
-        const int64_t stride = static_cast<int64_t>(kWaves) * a.split;
-        for (int64_t s = (static_cast<int64_t>(w.split) * kWaves + wave + stride - S::kSums * static_cast<int64_t>(st.n_whole) % stride) % stride; s < n; s += stride) {
-            st.rest(s >= per, c0 + (s >= per ? s - per : s) * S::kStep, acc, [] { E::order(); });
+        // (in 32 bits: for a comparison of two 64-bit numbers, uniform as they are, hipcc of ROCm 7.2 has put a vector comparison in front of a scalar selection)
+        const int from = a.n_whole * S::kStep, per = (a.C - from + S::kStep - 1) / S::kStep, stride = kWaves * static_cast<int>(a.split);
+        const int own = static_cast<int>(w.split) * kWaves + wave;
+        for (int s = (own + stride - S::kSums * a.n_whole % stride) % stride; s < S::kSums * per; s += stride) {
+            const int k = s >= per;
+            st.rest(k, from + static_cast<int64_t>(s - (k ? per : 0)) * S::kStep, acc, [] { E::order(); });
             S::add_step(acc, total);
         }
     }
@@ -736,7 +727,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a) {
 // Cuts the result into tiles of G and launches for them.  A launch takes kMost tiles each way at most (it has room for 2^32 threads, and wraps silently beyond).
 constexpr int64_t kMost = 1 << 11;
 template <typename T, typename G, bool kForward, typename Launch>
-int run(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, int64_t split, Launch launch) {
+int run(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split, Launch launch) {
     constexpr int64_t kWide = kForward ? G::kP / 2 : G::kP, kSize = sizeof(T);
     const int64_t tiles_m = (whole.M + G::kTok - 1) / G::kTok, tiles_r = (whole.R + kWide - 1) / kWide;
     const int64_t steps = (kForward ? 1 : 2) * ((static_cast<int64_t>(whole.C) * kSize + kRow - 1) / kRow);
@@ -752,6 +743,14 @@ int run(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, int64
         if (rc != TENSILE_OK) return rc;
         part = scratch.buf.p;
     }
+    // Backward a load of columns reads what lies behind the row's last one, up to the end of the row's last chunk: not where that is behind the matrix.
+    constexpr int64_t kPer = kPer16<T>, kStep = kRow / kSize;
+    int64_t behind = 0;                                                  // rows at the end that are not brought whole
+    if (!kForward && whole.R % kPer) {
+        const int64_t least = whole.p[0].ld < whole.p[1].ld ? whole.p[0].ld : whole.p[1].ld;
+        behind = (kPer - 1 + least - 1) / least;
+    }
+    const int64_t n_whole = far || whole.C < behind ? 0 : (whole.C - behind) / kStep;
     auto moved = [](Matrix m, int64_t rows, int64_t cols) {
         return Matrix{m.p ? static_cast<char *>(m.p) + (rows * m.ld + cols) * kSize : nullptr, m.ld};
     };
@@ -763,6 +762,7 @@ int run(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, int64
             a.tiles_m = static_cast<uint32_t>(tiles_m - m < kMost ? tiles_m - m : kMost);
             a.split = static_cast<uint32_t>(split);
             a.part = part;
+            a.n_whole = static_cast<int32_t>(n_whole);
             a.M -= m0;
             a.R -= static_cast<int32_t>(r0);
             a.out = moved(a.out, m0, r0);
@@ -782,11 +782,13 @@ int run(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, int64
 }
 
 template <typename T, typename G, bool kForward>
-int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split = 1) {
-    return run<T, G, kForward>(ops, s, whole, split, [&](const ProductArgs &a, dim3 grid, uint32_t tiles) {
+int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far = false, int64_t split = 1) {
+    return run<T, G, kForward>(ops, s, whole, far, split, [&](const ProductArgs &a, dim3 grid, uint32_t tiles) {
         const dim3 block(G::kThreads);
-        if (far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
+        if constexpr (G::kSplit) {
+            if (far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, true>), grid, block, 0, s, a);
+        }
+        if (!far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
         if constexpr (G::kSplit) {
             if (a.split > 1)
                 hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3(tiles * (G::kTok * G::kP / (kForward ? 4096 : 2048))), dim3(256), 0, s, a);
@@ -795,7 +797,7 @@ int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole,
 }
 template <typename T, bool kForward>
 int run_rows(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, bool far, int64_t split, bool four) {
-    return run<T, Rows, kForward>(ops, s, whole, split, [&](const ProductArgs &a, dim3 grid, uint32_t tiles) {
+    return run<T, Rows, kForward>(ops, s, whole, far, split, [&](const ProductArgs &a, dim3 grid, uint32_t tiles) {
         auto with = [&](auto waves, auto q) {
             constexpr int kWaves = decltype(waves)::value, kQ = decltype(q)::value;
             hipLaunchKernelGGL(HIP_KERNEL_NAME(product_rows_kernel<T, kForward, false, kWaves, kQ>), grid, dim3(64 * kWaves), 0, s, a);

@@ -374,6 +374,7 @@ int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensil
         TS_TRY(check_activation(activation, who));
         if (gate) TS_TRY(check_ckpt(gate, h->rows, h->cols, who, "gate"));
         if (up) TS_TRY(check_ckpt(up, h->rows, h->cols, who, "up"));
+        if (gate && up && h->rows > 0 && (gate->q == up->q || gate->scale == up->scale)) return refuse(who, "up", "is gate");
         if (x->rows == 0) return TENSILE_OK;
         GatedArgs a{};
         a.M = x->rows;

@@ -624,6 +624,46 @@ def test_rows_too_far_apart_for_32_bits(ops):
         near(dx, host(dx0), 4 * ROUND[dtype] * np.abs(host(dx0)) + 100 * U * size, dtype)
 
 
+@pytest.mark.parametrize("M,wide", [(40, 70), (256, 32_768), (130, 49_152)])
+def test_tiles_of_rows_too_far_apart_for_32_bits(ops, M, wide):
+    """The same with more tokens: few tiles, whose sums are split, and more than the card has places for."""
+    rng = np.random.default_rng(M)
+    short = 1_600 if wide < 100 else 40
+    far = lambda a, ld: torch.empty(a.shape[0] * ld, dtype=torch.bfloat16, device="cuda").as_strided(a.shape, (ld, 1)).copy_(a)
+    x, wg, wu = (up(rng.standard_normal(s) * short ** -0.5, "bf16") for s in ((M, short), (wide, short), (wide, short)))
+    h, want = room(M, wide, "bf16"), room(M, wide, "bf16")
+    P.tensile_gated_linear(ops, far(x, (1 << 22) + 8), wg, wu, h)
+    P.tensile_gated_linear(ops, x, wg, wu, want)
+    # the same products in another order: to a rounding of each and the sums' own
+    off = (h.double() - want.double()).abs()
+    assert bool((off <= 4 * ROUND["bf16"] * want.double().abs() + 100 * U * short).all())
+    dgate, dup, dx, dx0 = room(M, short, "bf16"), far(room(M, short, "bf16"), (1 << 22) + 8), room(M, wide, "bf16"), room(M, wide, "bf16")
+    g, _ = filled(rng.standard_normal((M, short)))
+    wg, wu = wg.t().contiguous(), wu.t().contiguous()
+    P.tensile_gated_linear_backward(ops, x, g, g, dgate, dup, w_gate=wg, w_up=wu, dx=dx)
+    P.tensile_gated_linear_backward(ops, x, g, g, dgate, dup.contiguous(), w_gate=wg, w_up=wu, dx=dx0)
+    size = dgate.double().abs() @ wg.double().abs() + dup.double().abs() @ wu.double().abs()
+    assert bool(((dx.double() - dx0.double()).abs() <= 4 * ROUND["bf16"] * dx0.double().abs() + 100 * U * size).all())
+
+
+def test_gated_backward_keeps_a_lost_group_to_itself(ops):
+    """A NaN group of gate or up spoils its own columns of dgate and dup (up: of dgate), its row of dx, and nothing else - also at the end of a row."""
+    M, K, F = 70, 50, 72
+    rng = np.random.default_rng(3)
+    g, u = rng.standard_normal((M, F)), rng.standard_normal((M, F))
+    g[4, 70], u[9, 3] = np.inf, np.nan
+    (cg, _), (cu, _) = filled(g), filled(u)
+    w = torch.ones(F, K, device="cuda")
+    dgate, dup, dx, c = room(M, F, "f32"), room(M, F, "f32"), room(M, K, "f32"), ckpt(M, F)
+    P.tensile_gated_linear_backward(ops, torch.ones(M, F, device="cuda"), cg, cu, dgate, dup, w_gate=w, w_up=w, dx=dx, h_ckpt=c)
+    where = lambda *cells: np.array([[any(r == a and b <= k < e for a, b, e in cells) for k in range(F)] for r in range(M)])
+    assert np.array_equal(np.isnan(host(dgate)), where((4, 64, 72), (9, 0, 32)))
+    assert np.array_equal(np.isnan(host(dup)), where((4, 64, 72)))
+    assert np.array_equal(np.isnan(host(dx)).any(1), np.isin(np.arange(M), (4, 9))) and bool(dx[[4, 9]].isnan().all())
+    code = c.scale.cpu().numpy()
+    assert code[4].tolist()[2] == 255 and code[9].tolist()[0] == 255 and (code == 255).sum() == 2
+
+
 def test_refused_allocation_is_an_error_and_the_next_call_works(tuning):
     h = P.tensile_ops_create()
     p, x, dy = setting(100, 2_048, 1_024)
@@ -684,6 +724,7 @@ def test_refusals(ops):
     refused(lambda: gated(ops, x, w, w, h, act="relu"), "relu")
     refused(lambda: gated(ops, x, w, w, h, gate=P.Checkpoint.empty(4, 31)), "gate")
     refused(lambda: gated(ops, x, w, w, h, up=P.Checkpoint.empty(3, 32)), "up")
+    refused(lambda: gated(ops, x, w, w, h, gate=ch, up=ch), "up is gate")
     refused(lambda: back(ops, None, ch, ch, h, h), "dh")
     refused(lambda: back(ops, h, None, ch, h, f(4, 32)), "gate")
     refused(lambda: back(ops, h, ch, P.Checkpoint.empty(4, 31), h, f(4, 32)), "up")

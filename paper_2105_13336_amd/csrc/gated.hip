@@ -8,7 +8,14 @@ namespace {
 template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
     const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
-    if (a.M <= 32) return run_rows<T, true>(ops, s, a, far, 1, (a.R + 31) / 32 <= ops->num_cus);
+    if (a.M <= 32) {
+        // Few features and long sums: these are split, where that saves more than the 4 us that it takes to add them up.  A wavefront's step takes some 0.4 us, 1.1
+        // in 32 bits, four wavefronts to a part.
+        const int64_t tiles = (a.R + 31) / 32, each = steps_of<T, true>(a) / 4, fill = ops->num_cus / tiles;
+        constexpr int64_t kLong = sizeof(T) == 2 ? 16 : 6, kLeast = sizeof(T) == 2 ? 4 : 2;
+        const int64_t most = each >= kLong ? each / kLeast : 1;
+        return run_rows<T, true>(ops, s, a, far, fill < most ? fill : most, tiles <= ops->num_cus);
+    }
     const int64_t cus = ops->num_cus, small = tiles_of<Small, true>(a);
     if (small <= cus || far) return run_tiles<T, Few, true>(ops, s, a, far, parts_of(small, cus, steps_of<T, true>(a)));
     // A round of tiles, as many as the card has places for, takes 1 where they are large and 0.65 where they are small (two to a CU).  Large and small (us, with

@@ -691,12 +691,18 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
 }
 
 // split > 1: the parts of a sum added up in a fixed order, then as above.  Eight features of a token to a thread.
+template <typename G, bool kForward>
+struct Join {
+    static constexpr int kWide = kForward ? G::kP / 2 : G::kP, kPlane = G::kTok * kWide, kUnits = kPlane / 8;
+    static constexpr int kThreads = kUnits < 256 ? kUnits : 256, kBlocks = kUnits / kThreads;    // of a tile
+    static_assert(kUnits % kThreads == 0, "");
+};
 template <typename T, typename G, bool kForward>
-__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a) {
-    constexpr int kWide = kForward ? G::kP / 2 : G::kP, kPlane = G::kTok * kWide, kPart = G::kP * G::kTok, kUnits = kPlane / 8;
-    static_assert(kUnits % 256 == 0, "");
-    const uint32_t tile = blockIdx.x / (kUnits / 256);
-    const int unit = blockIdx.x % (kUnits / 256) * 256 + threadIdx.x;
+__global__ __launch_bounds__((Join<G, kForward>::kThreads)) void product_join_kernel(ProductArgs a) {
+    using J = Join<G, kForward>;
+    constexpr int kWide = J::kWide, kPlane = J::kPlane, kPart = G::kP * G::kTok;
+    const uint32_t tile = blockIdx.x / J::kBlocks;
+    const int unit = blockIdx.x % J::kBlocks * J::kThreads + threadIdx.x;
     const Place w = place_of<G, kForward>(a, tile);
     const int64_t token = w.m0 + unit / (kWide / 8);
     const int r = w.r0 + unit % (kWide / 8) * 8, left = a.R - r;
@@ -791,7 +797,8 @@ int run_tiles(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole,
         if (!far) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_kernel<T, G, kForward, false>), grid, block, 0, s, a);
         if constexpr (G::kSplit) {
             if (a.split > 1)
-                hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3(tiles * (G::kTok * G::kP / (kForward ? 4096 : 2048))), dim3(256), 0, s, a);
+                hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, G, kForward>), dim3(tiles * Join<G, kForward>::kBlocks),
+                                   dim3(Join<G, kForward>::kThreads), 0, s, a);
         }
     });
 }
@@ -810,9 +817,9 @@ int run_rows(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, 
         else if (four) with(Four{}, Four{});
         else if (a.M <= 8) with(Two{}, One{});
         else with(Two{}, Four{});
-        if constexpr (!kForward) {
-            if (a.split > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, Rows, false>), dim3(tiles), dim3(256), 0, s, a);
-        }
+        if (a.split > 1)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<T, Rows, kForward>), dim3(tiles * Join<Rows, kForward>::kBlocks),
+                               dim3(Join<Rows, kForward>::kThreads), 0, s, a);
     });
 }
 

@@ -180,8 +180,8 @@ __device__ __forceinline__ void load_bias(const ProductArgs &a, int r, int left,
         for (int j = 0; j < 8; ++j) bias[k][j] = a.bias[0] && j < left ? param_at<T>(a.param_type, a.bias[k], r + j) : 0.0f;
 }
 // Gate and up, v and u, of a token's eight features, of which `left` exist (kWhole: all): biases, checkpoints, activation, product.  Four neighbouring lanes
-// hold a group and call this together, `there` or not.
-template <typename T, bool kWhole>
+// hold a group and call this together, `there` or not.  kPast: stores past the caches.
+template <typename T, bool kWhole, bool kPast>
 __device__ __forceinline__ void finish_gated(const ProductArgs &a, float (&v)[8], float (&u)[8], const float (&bias)[2][8], const Target<T, true> &to, int left, bool there) {
     const int n = kWhole ? kChunk : left;
     if (a.bias[0]) {
@@ -202,7 +202,10 @@ __device__ __forceinline__ void finish_gated(const ProductArgs &a, float (&v)[8]
         if (!a.kept[k].q) continue;
         uint32_t code;
         const u32x2 w = pack8(k ? u : v, static_cast<uint32_t>(a.cap), code);
-        if (there) store_q(to.q[k], w, n);
+        if (there) {
+            if constexpr (kPast) store_q_past(to.q[k], w, n);
+            else store_q(to.q[k], w, n);
+        }
         if (there && (threadIdx.x & 3) == 0) *to.scale[k] = static_cast<uint8_t>(code);
     }
     auto apply = [&](auto act) __attribute__((always_inline)) {
@@ -212,12 +215,15 @@ __device__ __forceinline__ void finish_gated(const ProductArgs &a, float (&v)[8]
     if (a.act == TENSILE_SILU) apply(Silu{});
     else if (a.act == TENSILE_GELU) apply(Gelu<false>{});
     else apply(Gelu<true>{});
-    if (there) store8(to.out, v, n);
+    if (there) {
+        if constexpr (kPast) store8_past(to.out, v, n);
+        else store8(to.out, v, n);
+    }
 }
 
 // Tokens from first_token on, 32 at a time, `times` times, and features from r0 on: write(t) puts what belongs to the t-th 32 tokens into the region (kRegions of
 // them: each wavefront's part of the sums).  A wavefront goes through them from pass `start` on, every `stride`-th one.
-template <typename T, int kPB, bool kForward, int kRegions, typename Write>
+template <typename T, int kPB, bool kForward, int kRegions, bool kPast, typename Write>
 __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int64_t first_token, int r0, int times, int start, int stride, Write write) {
     using E = Exchange<kPB, kForward>;
     static_assert(!kForward || E::kEven, "");
@@ -244,9 +250,10 @@ __device__ __forceinline__ void finish(const ProductArgs &a, float *region, int6
                 if constexpr (kForward) {
                     float u[8];
                     E::template get<kRegions>(region, 1, in, u);
-                    finish_gated<T, kWhole>(a, v, u, bias, to, left, there);
+                    finish_gated<T, kWhole, kPast>(a, v, u, bias, to, left, there);
                 } else if (there) {
-                    store8(to.out, v, kWhole ? kChunk : left);
+                    if constexpr (kPast) store8_past(to.out, v, kWhole ? kChunk : left);
+                    else store8(to.out, v, kWhole ? kChunk : left);
                 }
                 to.go_on(a, stride * E::kAtOnce);
                 token += stride * E::kAtOnce;
@@ -295,6 +302,9 @@ struct Tile {
     static constexpr int kPB = kPB_, kTB = kTB_, kWP = kWP_, kWT = kWT_, kPerCu = kPerCu_, kSlots = kSlots_;   // kSlots: steps in the LDS
     static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
     static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
+    // Large tiles end at about the same time, each with 64 KB of h and as much of the checkpoints; together that is what the L2 holds, and there it displaces what
+    // the next tiles share (8192 x 4096 x 10944 with checkpoints 1198 us, past the caches 1156; 8192 x 768 x 2048 65.2 and 58.5).
+    static constexpr bool kPast = kP * kTok >= 192 * 128;
     static constexpr bool kSplit = kSlots > 3;                           // what is split, or far, takes tiles of this kind
 };
 
@@ -618,7 +628,7 @@ __global__ __launch_bounds__(G::kThreads, G::kPerCu * G::kWaves / 4) void produc
             return;
         }
     }
-    finish<T, G::kPB, kForward, 1>(a, region, w.m0 + st.wave_t * G::kTB * 32, w.r0 + st.wave_p * E::kWide, G::kTB, 0, 1, write);
+    finish<T, G::kPB, kForward, 1, G::kPast>(a, region, w.m0 + st.wave_t * G::kTB * 32, w.r0 + st.wave_p * E::kWide, G::kTB, 0, 1, write);
 }
 
 // Up to 32 tokens: the weights are read once and that is what it costs.  A workgroup has 32 features (backward 64), of whose sums each wavefront takes every
@@ -691,7 +701,7 @@ __global__ __launch_bounds__(64 * kWaves) void product_rows_kernel(ProductArgs a
     if (a.split > 1)
         leave_part<Rows::kPB, kForward, kWaves>(a.part + (static_cast<int64_t>(w.tile) * a.split + w.split) * (Rows::kP * Rows::kTok), Rows::kTok, E::kWide, 0, 0, region,
                                                 1, wave, kWaves, [](int) {});
-    else finish<T, Rows::kPB, kForward, kWaves>(a, region, w.m0, w.r0, 1, wave, kWaves, [](int) {});
+    else finish<T, Rows::kPB, kForward, kWaves, false>(a, region, w.m0, w.r0, 1, wave, kWaves, [](int) {});
 }
 
 // split > 1: the parts of a sum added up in a fixed order, then as above.  Eight features of a token to a thread.
@@ -728,7 +738,7 @@ __global__ __launch_bounds__((Join<G, kForward>::kThreads)) void product_join_ke
     if constexpr (kForward) {
         float bias[2][8];
         load_bias<T>(a, r, left, bias);
-        finish_gated<T, false>(a, sum[0], sum[1], bias, to, left, there);
+        finish_gated<T, false, false>(a, sum[0], sum[1], bias, to, left, there);
     } else if (there) {
         store8(to.out, sum[0], left);
     }

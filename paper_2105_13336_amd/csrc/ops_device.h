@@ -122,6 +122,21 @@ __device__ __forceinline__ void store8(T *p, const float (&f)[8], int left) {
     store_raw(p, r, left);
 }
 
+// The same past the caches (for what is larger than they are): of eight whole elements, else as above.
+typedef u32x4 u32x4_loose __attribute__((aligned(1)));
+typedef u32x2 u32x2_loose __attribute__((aligned(1)));
+template <typename T>
+__device__ __forceinline__ void store8_past(T *p, const float (&f)[8], int left) {
+    Raw8<T> r;
+    narrow(f, r);
+    if (left < kChunk) {
+        store_raw(p, r, left);
+        return;
+    }
+    __builtin_nontemporal_store(r.v, reinterpret_cast<u32x4_loose *>(p));
+    if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(r.w, reinterpret_cast<u32x4_loose *>(p + 4));
+}
+
 // One element, for what is not a hot path.
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(bf16_t x) { return as_f32(static_cast<uint32_t>(x.bits) << 16); }
@@ -160,6 +175,11 @@ __device__ __forceinline__ void store_q(int8_t *p, u32x2 w, int left) {
         for (int j = 0; j < kChunk; ++j)
             if (j < left) p[j] = static_cast<int8_t>(w[j / 4] >> (8 * (j % 4)));
     }
+}
+
+__device__ __forceinline__ void store_q_past(int8_t *p, u32x2 w, int left) {
+    if (left >= kChunk) __builtin_nontemporal_store(w, reinterpret_cast<u32x2_loose *>(p));
+    else store_q(p, w, left);
 }
 
 // 2^(code-127): the code is the scale's exponent field; 255 stands for NaN.

@@ -2,6 +2,10 @@
 //   g[m,f] = sum_k x[m,k]*Wg[f,k],  u[m,f] = sum_k x[m,k]*Wu[f,k]          (and from both act(g)*u, in the registers that hold them)
 //   dx[m,k] = sum_f dgate[m,f]*Wg[f,k] + sum_f dup[m,f]*Wu[f,k]
 //
+// Long batches are bound by the matrix instructions and the clock that the chip can keep up with them (1.6 to 1.7 GHz, 66 to 72 % of its cycles): 8192 x 4096 x
+// 10944 bf16 1107 us (1327 TFLOP/s; a library's product of the same size alone 1124), with checkpoints 1157; backward 1111 after 144 for the elementwise part.  f32
+// 2048 x 4096 x 4096 970 us (141 TFLOP/s of 157).  Single tokens are bound by the weights' bytes: 1 x 4096 x 10944 38 us (4.7 TB/s), 1 x 4096 x 43776 120 (6.0).
+//
 // On the matrix instructions with 32-bit sums: bf16 and f16 as they are, f32 on those for 32 bits (products and sums as in ordinary arithmetic).
 // A block of the result is 32 x 32; its rows are weights (f, or k backward) and its columns tokens, so that a lane holds 16 of the 32
 // features of one token, and gate and up of the same f and m lie in the same register of two blocks.
@@ -104,8 +108,9 @@ __device__ __forceinline__ float param_at(int type, const void *p, int64_t at) {
 }
 
 // What becomes of the sums of a wavefront's kPB blocks (32 rows each) of 32 tokens.  They go through the LDS, so that a lane has eight features of a token and a
-// store whole lines of memory, in a loop: in registers it takes a copy of all of this for every block, which the instruction cache does not hold
-// (8192 x 4096 x 10944 with checkpoints 1356 us, so LATER).
+// store whole lines of memory, in a loop: in registers it takes a copy of all of this for every block, and spills (8192 x 4096 x 10944 with checkpoints 1356 us against
+// 1278, the rest unchanged).  It takes 7 us a tile of 256 x 128, 10 with checkpoints, of which the stores are most and the activation 2: 8192 x 256 x 2048, two tiles
+// to a CU, 32 and 39 us, without all of this 17.
 template <int kPB_, bool kForward>
 struct Exchange {
     static constexpr int kPB = kPB_, kWide = kForward ? kPB * 16 : kPB * 32;           // features
@@ -303,13 +308,13 @@ struct Tile {
     static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
     static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
     // Large tiles end at about the same time, each with 64 KB of h and as much of the checkpoints; together that is what the L2 holds, and there it displaces what
-    // the next tiles share (8192 x 4096 x 10944 with checkpoints 1198 us, past the caches 1156; 8192 x 768 x 2048 65.2 and 58.5).
+    // the next tiles share (8192 x 4096 x 10944 with checkpoints 1198 us, past the caches 1160; 8192 x 768 x 2048 65 and 59; backward 96.5 and 93.8 in all).
     static constexpr bool kPast = kP * kTok >= 192 * 128;
     static constexpr bool kSplit = kSlots > 3;                           // what is split, or far, takes tiles of this kind
 };
 
-// A step takes kRow bytes of a row, a line of the caches (with half a line to a step the L2 is asked twice as often: it answers a line or half of one in the same
-// time): kParts fragments.
+// A step takes kRow bytes of a row, a line of the caches (with half a line to a step the L2 is asked twice as often, and answers a line or half of one in the same
+// time: 8192 x 4096 x 10944 1230 us against 1183): kParts fragments.
 constexpr int kRow = 128, kParts = kRow / 32;
 
 // Of staged rows the 16-byte chunks are stored in an order that depends on the row, so that 16 rows' chunks of the same number lie in different banks.
@@ -841,6 +846,8 @@ int run_rows(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, 
 constexpr int64_t kFarBytes = 1 << 23;
 inline bool is_far(const Matrix &m, int64_t size) { return m.ld * size >= kFarBytes; }
 
+// (Four wavefronts of 128 x 128, one to a SIMD, read the LDS a third less and are slower all the same, 1461 us against 1138 at 8192 x 4096 x 10944: nothing runs while
+// one waits.  256 x 128 with three steps of half lines, two workgroups to a CU: 1399 against 1230 then.)
 using Large = Tile<4, 2, 2, 4, 1, 2>;    // 256 x 256
 using Middle = Tile<3, 1, 2, 4, 1, 3>;   // 192 x 128
 using Small = Tile<2, 2, 2, 2, 2, 2>;    // 128 x 128

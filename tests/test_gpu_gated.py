@@ -406,7 +406,7 @@ def test_gated_backward_of_many_tokens(ops, dtype, F):
 @pytest.mark.parametrize("dtype", TYPES)
 def test_gated_with_split_sums(ops, dtype):
     """Few tiles and long sums, of which the last step is a part of one, or there is none."""
-    for M, K, F in ((40, 1_700, 100), (64, 2_048, 64), (200, 3_001, 130), (3, 8_200, 33), (32, 9_001, 64)):
+    for M, K, F in ((40, 1_700, 100), (64, 2_048, 64), (200, 3_001, 130), (3, 8_200, 33), (32, 9_001, 64), (20, 1_700, 40)):
         check_gated(ops, dtype, M, K, F, act="gelu", bias="f32")
         check_gated_backward(ops, dtype, M, F, K, act="gelu")
         check_gated_backward(ops, dtype, M, F, K, odd=True)

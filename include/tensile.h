@@ -399,7 +399,6 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
 #define TENSILE_BF16 1
 #define TENSILE_F16 2
 
-
 typedef struct tensile_ops tensile_ops; /* opaque; owns the scratch memory of the calls below */
 
 /* Creates a handle for the current HIP device; the calls that take it are made
@@ -473,8 +472,8 @@ int tensile_gelu_backward(tensile_ops *ops, const tensile_matrix *dy, const tens
 
 /* Root-mean-square norm of every row, after an optional residual sum:
  *   s = x (+ residual);  rstd = 1/sqrt(mean of s^2 over the row + eps);  xhat = s*rstd;  y = xhat*gamma
- * Arguments as in tensile_layer_norm.  (Squares are summed in 32 bits: a row whose sum of squares is no finite 32-bit number has
- * rstd 0.  s is rounded for total only.) */
+ * Arguments as in tensile_layer_norm.  (Squares are summed in 32 bits: where their sum is too large for a 32-bit number, rstd is 0;
+ * squares below 2^-149 count as 0.  s is rounded for total only.) */
 int tensile_rms_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *residual, const void *gamma,
                      int32_t param_type, double eps, const tensile_matrix *y, const tensile_matrix *total,
                      const tensile_ckpt *xhat, float *rstd, void *hip_stream);
@@ -499,7 +498,7 @@ int tensile_rms_norm_backward(tensile_ops *ops, const tensile_matrix *dy, const 
  * Products are summed in 32 bits; nothing is rounded before h and the checkpoints are.
  *   w_gate, w_up  F x K, of x's type; b_gate, b_up [F] of param_type (TENSILE_F32 or x's type), both or neither NULL
  *   activation    TENSILE_SILU, TENSILE_GELU or TENSILE_GELU_TANH
- *   h             M x F, of x's type
+ *   h             M x F, of x's type; not x itself (it is written while others still read x)
  *   gate, up      checkpoints (M x F) of g and of u, what the backward pass reads; either may be NULL */
 int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix *w_gate, const tensile_matrix *w_up,
                          const void *b_gate, const void *b_up, int32_t param_type, int32_t activation,
@@ -512,7 +511,7 @@ int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensil
  *   dgate, dup    like dh; one of them may be dh itself
  *   h_c           checkpoint of act(g)*u, for the weight gradient of the layer that read h, or NULL; may be gate or up itself
  *   w_gate, w_up, dx  F x K, F x K and M x K, of dh's type; all or none NULL (dx is not wanted then).  dx is summed from dgate
- *                 and dup as they were rounded: the gradient that belongs to those */
+ *                 and dup as they were rounded: the gradient that belongs to those; it may be dh where neither of them is, not one of them */
 int tensile_gated_linear_backward(tensile_ops *ops, const tensile_matrix *dh, const tensile_ckpt *gate, const tensile_ckpt *up,
                                   int32_t activation, const tensile_matrix *dgate, const tensile_matrix *dup,
                                   const tensile_ckpt *h_c, const tensile_matrix *w_gate, const tensile_matrix *w_up,

@@ -366,6 +366,7 @@ int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensil
         if (w_gate->rows > kMostCols) { set_error("gated_linear: w_gate has more than 2^30 rows"); return TENSILE_E_RANGE; }
         TS_TRY(check_matrix(h, who, "h"));
         if (h->rows != x->rows || h->cols != w_gate->rows || h->type != x->type) return refuse(who, "h", "is not (rows of x) x (rows of w_gate), or not of x's type");
+        if (h->rows > 0 && (h->data == x->data || h->data == w_gate->data || h->data == w_up->data)) return refuse(who, "h", "is x or a weight matrix");
         if (!b_gate != !b_up) return refuse(who, "b_gate, b_up", "are given one without the other");
         if (b_gate) {
             TS_TRY(check_param(b_gate, param_type, x->type, who, "b_gate"));
@@ -412,6 +413,8 @@ int tensile_gated_linear_backward(tensile_ops *ops, const tensile_matrix *dh, co
             if (w_gate->rows != dh->cols || w_gate->type != dh->type) return refuse(who, "w_gate", "has not a row for each column of dh, or is not of dh's type");
             TS_TRY(check_matrix(dx, who, "dx"));
             if (dx->rows != dh->rows || dx->cols != w_gate->cols || dx->type != dh->type) return refuse(who, "dx", "is not (rows of dh) x (columns of w_gate), or not of dh's type");
+            if (dx->rows > 0 && (dx->data == dgate->data || dx->data == dup->data || dx->data == w_gate->data || dx->data == w_up->data))
+                return refuse(who, "dx", "is dgate, dup or a weight matrix");
         }
         if (dh->rows == 0) return TENSILE_OK;
         GatedArgs a{};

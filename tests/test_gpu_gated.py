@@ -738,3 +738,28 @@ def test_refusals(ops):
     closed = P.tensile_ops_create()
     closed.close()
     refused(lambda: gated(closed, x, w, w, h), "freed")
+
+
+def test_results_in_the_place_of_what_is_read(ops):
+    """h over x, or dx over dgate or dup, of one size: other workgroups still read those, so the calls are refused; dx over dh is no such case."""
+    M, n = 70, 96
+    rng = np.random.default_rng(8)
+    x, wg, wu = up(rng.standard_normal((M, n)), "bf16"), up(rng.standard_normal((n, n)) / 8, "bf16"), up(rng.standard_normal((n, n)) / 8, "bf16")
+    x0 = x.clone()
+    for h, word in ((x, "h is x"), (wg[:M], "h is x or a weight"), (wu[:M], "h is x or a weight")):
+        with pytest.raises(P.TensileError) as e:
+            P.tensile_gated_linear(ops, x, wg, wu, h)
+        assert e.value.code == P.binding.TENSILE_E_INVAL and word in str(e.value)
+    h, cg, cu = torch.empty_like(x), ckpt(M, n), ckpt(M, n)
+    P.tensile_gated_linear(ops, x, wg, wu, h, gate=cg, up=cu)
+    dh = up(rng.standard_normal((M, n)), "bf16")
+    dgate, dup, dx = (torch.empty_like(x) for _ in range(3))
+    P.tensile_gated_linear_backward(ops, dh, cg, cu, dgate, dup, w_gate=wg, w_up=wu, dx=dx)
+    for into in (dgate, dup, wg[:M], wu[:M]):
+        with pytest.raises(P.TensileError) as e:
+            P.tensile_gated_linear_backward(ops, dh, cg, cu, dgate, dup, w_gate=wg, w_up=wu, dx=into)
+        assert e.value.code == P.binding.TENSILE_E_INVAL and "dx is dgate" in str(e.value)
+    with pytest.raises(P.TensileError):
+        P.tensile_gated_linear_backward(ops, dh, cg, cu, dh, dup, w_gate=wg, w_up=wu, dx=dh)
+    P.tensile_gated_linear_backward(ops, dh, cg, cu, dgate, dup, w_gate=wg, w_up=wu, dx=dh)
+    assert torch.equal(x, x0) and torch.equal(dh, dx)

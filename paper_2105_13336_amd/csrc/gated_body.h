@@ -4,7 +4,8 @@
 //
 // Long batches are bound by the matrix instructions and the clock that the chip can keep up with them (1.6 to 1.7 GHz, 64 to 72 % of its cycles): 8192 x 4096 x
 // 10944 bf16 1084 us (1354 TFLOP/s; a library's product of the same size alone 1115), with checkpoints 1115 to 1133; backward 1090 to 1107 after 143 for the
-// elementwise part (a library's product alone, weights as they lie, 1040).  f32 2048 x 4096 x 4096 970 us (141 TFLOP/s of 157).  Single tokens are bound by the weights' bytes: 1 x 4096 x 10944 38 us (4.7 TB/s), 1 x 4096 x 43776 120 (6.0).
+// elementwise part (a library's product alone, weights as they lie, 1040).  f32 2048 x 4096 x 4096 970 us (141 TFLOP/s of 157).  Single tokens are bound by
+// the weights' bytes: 1 x 4096 x 10944 38 us (4.7 TB/s), 1 x 4096 x 43776 120 (6.0).
 //
 // On the matrix instructions with 32-bit sums: bf16 and f16 as they are, f32 on those for 32 bits (products and sums as in ordinary arithmetic).
 // A block of the result is 32 x 32; its rows are weights (f, or k backward) and its columns tokens, so that a lane holds 16 of the 32

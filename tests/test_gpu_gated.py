@@ -763,3 +763,14 @@ def test_results_in_the_place_of_what_is_read(ops):
         P.tensile_gated_linear_backward(ops, dh, cg, cu, dh, dup, w_gate=wg, w_up=wu, dx=dh)
     P.tensile_gated_linear_backward(ops, dh, cg, cu, dgate, dup, w_gate=wg, w_up=wu, dx=dh)
     assert torch.equal(x, x0) and torch.equal(dh, dx)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_more_tiles_than_a_launch_takes(ops, dtype):
+    """Over 2,048 tiles in a direction are several launches: of 32 and of 64 features, of 64 columns backward, and of 128 tokens."""
+    check_gated(ops, dtype, 2, 24, 70_001, act="gelu", bias="f32", odd=True)
+    check_gated(ops, dtype, 40, 16, 140_003, bias="f32", odd=True)
+    check_gated_backward(ops, dtype, 3, 140_003, 24, odd=True)
+    check_gated_backward(ops, dtype, 33, 270_000, 16)
+    check_gated(ops, dtype, 270_001, 8, 9, act="gelu_tanh", bias=dtype, odd=True)
+    check_gated_backward(ops, dtype, 270_001, 8, 9, odd=True)

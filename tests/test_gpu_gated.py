@@ -774,3 +774,50 @@ def test_more_tiles_than_a_launch_takes(ops, dtype):
     check_gated_backward(ops, dtype, 33, 270_000, 16)
     check_gated(ops, dtype, 270_001, 8, 9, act="gelu_tanh", bias=dtype, odd=True)
     check_gated_backward(ops, dtype, 270_001, 8, 9, odd=True)
+
+
+def test_offsets_beyond_32_bits(ops):
+    """1,050,000 tokens of 2,056 columns: elements and bytes, of matrices and of checkpoints, beyond 2^31.  First, last and middle rows against 64 bits."""
+    M, n, dtype = 1_050_000, 2_056, "bf16"
+    rng = np.random.default_rng(9)
+    torch.manual_seed(9)
+    x = torch.randn(M, n, device="cuda", dtype=torch.bfloat16)
+    gamma = up(1 + 0.2 * rng.standard_normal(n))
+    wg, wu = (up(rng.standard_normal((n, n)) * n ** -0.5, dtype) for _ in range(2))
+    y, h, xhat, cg, cu, ch, rstd = torch.empty_like(x), torch.empty_like(x), ckpt(M, n), ckpt(M, n), ckpt(M, n), ckpt(M, n), torch.empty(M, device="cuda")
+    P.tensile_rms_norm(ops, x, gamma, y, xhat=xhat, rstd=rstd)
+    P.tensile_gated_linear(ops, y, wg, wu, h, gate=cg, up=cu)
+    dgate, dup, dx, ds, dgamma = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty_like(gamma)
+    P.tensile_gated_linear_backward(ops, x, cg, cu, dgate, dup, w_gate=wg, w_up=wu, dx=dx, h_ckpt=ch)
+    P.tensile_rms_norm_backward(ops, dx, xhat, rstd, gamma, ds, dgamma, dresidual=x)
+    wg0, wu0, gamma0 = host(wg), host(wu), host(gamma)
+    chain, chain2 = plain.chain(n, dtype, 64), plain.chain(2 * n, dtype, 64)
+    for first in (0, 1_044_400, M - 40):         # (row 1,044,496 is where 2^31 elements end)
+        at = slice(first, first + 100)
+        part = lambda c: P.Checkpoint(c.q[at], c.scale[at])
+        held = lambda c: ops_plain.unpack(c.q[at].cpu().numpy(), c.scale[at].cpu().numpy())
+        y0, xh0, rstd0 = plain.rms_norm(host(x[at]), gamma0, 1e-6)
+        unit = (48 / 2 + 4) * U
+        near(y[at], y0, ROUND[dtype] * np.abs(y0) + (1.01 * unit + 4 * U) * np.abs(xh0 * gamma0), "y")
+        holds(part(xhat), xh0, (unit + 2 * U) * np.abs(xh0), dtype, "xhat")
+        h0, g0, u0 = plain.gated(host(y[at]), wg0, wu0, 0.0, 0.0, "silu")
+        eg, eu = (chain * U * (np.abs(host(y[at])) @ np.abs(w).T) for w in (wg0, wu0))
+        holds(part(cg), g0, eg, dtype, "gate")
+        holds(part(cu), u0, eu, dtype, "up")
+        value, error = np.abs(plain.activation(g0, "silu")[0]), 1.13 * eg + plain.activation_error(g0, "silu", dtype)[0]
+        near(h[at], h0, (ROUND[dtype] + 2 * U) * np.abs(h0) + FLOOR[dtype] + 1.01 * (error * (np.abs(u0) + eu) + value * eu), "h")
+        g, u, d = held(cg), held(cu), host(x[at])
+        dg0, du0, again = plain.gated_grad(d, g, u, "silu")
+        ev, es = plain.activation_error(g, "silu", dtype)
+        near(dgate[at], dg0, (ROUND[dtype] + 3 * U) * np.abs(dg0) + FLOOR[dtype] + es * np.abs(d * u), "dgate")
+        near(dup[at], du0, (ROUND[dtype] + 3 * U) * np.abs(du0) + FLOOR[dtype] + ev * np.abs(d), "dup")
+        holds(part(ch), again, ev * np.abs(u) + 2 * U * np.abs(again), dtype, "h in 8 bits")
+        a, b = host(dgate[at]), host(dup[at])
+        want = a @ wg0 + b @ wu0
+        near(dx[at], want, (ROUND[dtype] + U) * np.abs(want) + FLOOR[dtype] + chain2 * U * (np.abs(a) @ np.abs(wg0) + np.abs(b) @ np.abs(wu0)), "dx")
+        xh, t = held(xhat), np.abs(host(dx[at]) * gamma0)
+        r0 = host(rstd[at])
+        want = plain.rms_norm_backward(host(dx[at]), xh, r0, gamma0)[0]
+        size = r0[:, None] * (t + np.abs(xh) * (t * np.abs(xh)).mean(axis=1, keepdims=True))
+        near(ds[at], want + d, (ROUND[dtype] + U) * np.abs(want + d) + FLOOR[dtype] + 80 * U * size + 2 * U * np.abs(d), "ds")
+    assert bool(dgamma.isfinite().all())

@@ -3,6 +3,7 @@
 
 #include <atomic>
 #include <cfloat>
+#include <initializer_list>
 #include <new>
 
 namespace tensile {
@@ -162,6 +163,62 @@ float held_eps(double eps) {
 int check_activation(int32_t activation, const char *who) {
     const bool known = activation == TENSILE_SILU || activation == TENSILE_GELU || activation == TENSILE_GELU_TANH;
     return known ? TENSILE_OK : refuse(who, "activation", "is not one of TENSILE_SILU, TENSILE_GELU, TENSILE_GELU_TANH");
+}
+
+// Where a matrix lies, in bytes: `rows` times `wide` bytes, `pitch` apart.  A result must not meet anything else that the call reads or writes: it is
+// written while others read.
+struct Span {
+    const char *name;
+    int64_t at, rows, wide, pitch;     // rows 0: nothing there
+};
+Span span(const tensile_matrix *m, const char *name) {
+    if (!m || m->rows == 0) return {name, 0, 0, 0, 0};
+    const int64_t size = static_cast<int64_t>(element_size(m->type));
+    return {name, reinterpret_cast<int64_t>(m->data), m->rows, m->cols * size, m->ld * size};
+}
+Span span(const tensile_ckpt *c, const char *name) {
+    if (!c || c->rows == 0) return {name, 0, 0, 0, 0};
+    return {name, reinterpret_cast<int64_t>(c->q), c->rows, c->cols, c->ld_q};
+}
+Span scale_span(const tensile_ckpt *c, const char *name) {
+    if (!c || c->rows == 0) return {name, 0, 0, 0, 0};
+    return {name, reinterpret_cast<int64_t>(c->scale), c->rows, (c->cols + kGroup - 1) / kGroup, c->ld_scale};
+}
+bool identical(const Span &a, const Span &b) { return a.at == b.at && a.rows == b.rows && a.wide == b.wide && (a.rows < 2 || a.pitch == b.pitch); }
+
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }        // (b > 0)
+// Rows j of b, first to last of b.rows, of which a byte lies in [from, from + wide).
+bool meets_row(const Span &b, int64_t from, int64_t wide) {
+    const int64_t first = floor_div(from - b.wide - b.at, b.pitch) + 1, last = -floor_div(-(from + wide - b.at), b.pitch) - 1;
+    return (first > 0 ? first : 0) <= (last < b.rows - 1 ? last : b.rows - 1);
+}
+// Whether a byte belongs to both.  Exact: rows of one may lie between those of the other, as the halves of a matrix's columns do.
+bool meet(const Span &a, const Span &b) {
+    if (a.rows == 0 || b.rows == 0) return false;
+    if (a.at + (a.rows - 1) * a.pitch + a.wide <= b.at || b.at + (b.rows - 1) * b.pitch + b.wide <= a.at) return false;
+    if (a.rows == 1) return meets_row(b, a.at, a.wide);
+    if (b.rows == 1) return meets_row(a, b.at, b.wide);
+    if (a.pitch == b.pitch) {
+        // the first row of a, moved by the differences of row numbers that there are, against b's first
+        const Span moved{b.name, b.at - (a.rows - 1) * b.pitch, a.rows + b.rows - 1, b.wide, b.pitch};
+        return meets_row(moved, a.at, a.wide);
+    }
+    const Span &few = a.rows < b.rows ? a : b, &many = a.rows < b.rows ? b : a;
+    for (int64_t i = 0; i < few.rows; ++i)
+        if (meets_row(many, few.at + i * few.pitch, few.wide)) return true;
+    return false;
+}
+// out, a result, against `others` - of which `may_be` are those that it may be itself, row for row
+int check_apart(const char *who, const Span &out, std::initializer_list<Span> others, std::initializer_list<Span> may_be = {}) {
+    auto refused = [&](const Span &s) {
+        set_error("%s: %s overlaps %s", who, out.name, s.name);
+        return TENSILE_E_INVAL;
+    };
+    for (const Span &s : others)
+        if (meet(out, s)) return refused(s);
+    for (const Span &s : may_be)
+        if (!identical(out, s) && meet(out, s)) return refused(s);
+    return TENSILE_OK;
 }
 
 Matrix view(const tensile_matrix *m) { return m ? Matrix{m->data, m->ld} : Matrix{nullptr, 0}; }
@@ -377,6 +434,13 @@ int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensil
         if (up) TS_TRY(check_ckpt(up, h->rows, h->cols, who, "up"));
         if (gate && up && h->rows > 0 && (gate->q == up->q || gate->scale == up->scale)) return refuse(who, "up", "is gate");
         if (x->rows == 0) return TENSILE_OK;
+        const Span x_at = span(x, "x"), wg_at = span(w_gate, "w_gate"), wu_at = span(w_up, "w_up"), h_at = span(h, "h"), g_at = span(gate, "gate"),
+                   g_scales = scale_span(gate, "gate.scale"), u_at = span(up, "up"), u_scales = scale_span(up, "up.scale");
+        TS_TRY(check_apart(who, h_at, {x_at, wg_at, wu_at, g_at, g_scales, u_at, u_scales}));
+        TS_TRY(check_apart(who, g_at, {x_at, wg_at, wu_at, g_scales, u_at, u_scales}));
+        TS_TRY(check_apart(who, g_scales, {x_at, wg_at, wu_at, u_at, u_scales}));
+        TS_TRY(check_apart(who, u_at, {x_at, wg_at, wu_at, u_scales}));
+        TS_TRY(check_apart(who, u_scales, {x_at, wg_at, wu_at}));
         GatedArgs a{};
         a.M = x->rows;
         a.K = static_cast<int32_t>(x->cols);
@@ -417,6 +481,20 @@ int tensile_gated_linear_backward(tensile_ops *ops, const tensile_matrix *dh, co
                 return refuse(who, "dx", "is dgate, dup or a weight matrix");
         }
         if (dh->rows == 0) return TENSILE_OK;
+        const Span dh_at = span(dh, "dh"), g_at = span(gate, "gate"), g_scales = scale_span(gate, "gate.scale"), u_at = span(up, "up"),
+                   u_scales = scale_span(up, "up.scale"), wg_at = span(w_gate, "w_gate"), wu_at = span(w_up, "w_up"), dgate_at = span(dgate, "dgate"),
+                   dup_at = span(dup, "dup"), dx_at = span(dx, "dx"), h_at = span(h_c, "h_c"), h_scales = scale_span(h_c, "h_c.scale");
+        TS_TRY(check_apart(who, dgate_at, {g_at, g_scales, u_at, u_scales, wg_at, wu_at, dup_at, dx_at, h_at, h_scales}, {dh_at}));
+        TS_TRY(check_apart(who, dup_at, {g_at, g_scales, u_at, u_scales, wg_at, wu_at, dx_at, h_at, h_scales}, {dh_at}));
+        TS_TRY(check_apart(who, dx_at, {g_at, g_scales, u_at, u_scales, wg_at, wu_at, h_at, h_scales}, {dh_at}));
+        // (gate's bytes and its scales, or up's, or neither)
+        const bool over_gate = h_c && identical(h_at, g_at) && identical(h_scales, g_scales), over_up = h_c && identical(h_at, u_at) && identical(h_scales, u_scales);
+        TS_TRY(check_apart(who, h_at, {dh_at, wg_at, wu_at, h_scales}));
+        TS_TRY(check_apart(who, h_scales, {dh_at, wg_at, wu_at}));
+        if (!over_gate) TS_TRY(check_apart(who, h_at, {g_at, g_scales}));
+        if (!over_gate) TS_TRY(check_apart(who, h_scales, {g_at, g_scales}));
+        if (!over_up) TS_TRY(check_apart(who, h_at, {u_at, u_scales}));
+        if (!over_up) TS_TRY(check_apart(who, h_scales, {u_at, u_scales}));
         GatedArgs a{};
         a.M = dh->rows;
         a.F = static_cast<int32_t>(dh->cols);

@@ -1,0 +1,117 @@
+"""Calls of the operators that are refused, without a GPU (host_calls.py): results that overlap what else a call reads or writes."""
+import random
+
+import pytest
+
+from host_calls import BF16, F32, SIZE, Host, ckpt, mat
+
+G = 1 << 34                                             # places that are far from each other
+INVAL = -1
+SILU = 0
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    h = Host(tmp_path_factory.mktemp("host"))
+    yield h
+    h.close()
+
+
+def allowed(reply):
+    assert reply.code == 0 and reply.launches, reply
+
+
+def refused(reply, message):
+    assert reply.code == INVAL and reply.error == message and not reply.launches, reply
+
+
+def place(k, rows, cols, **more):
+    return ckpt(k * G, k * G + G // 2, rows, cols, **more)
+
+
+# ------------------------------------------------------------------ gated layer
+
+def gated(host, M=40, K=48, F=48, x=None, wg=None, wu=None, h=None, gate=None, up=None, type=BF16):
+    return host("gated_linear", x or mat(1 * G, M, K, type=type), wg or mat(2 * G, F, K, type=type), wu or mat(3 * G, F, K, type=type), None, None, F32, SILU,
+                h or mat(4 * G, M, F, type=type), gate, up)
+
+
+def back(host, M=40, K=48, F=64, dh=None, gate=None, up=None, dgate=None, dup=None, h_c=None, wg=None, wu=None, dx=None, product=True):
+    ws = (wg or mat(6 * G, F, K), wu or mat(7 * G, F, K), dx or mat(8 * G, M, K)) if product else (None, None, None)
+    return host("gated_linear_backward", dh or mat(1 * G, M, F), gate or place(2, M, F), up or place(3, M, F), SILU, dgate or mat(4 * G, M, F),
+                dup or mat(5 * G, M, F), h_c, *ws)
+
+
+def test_a_gradient_in_the_place_of_dh_has_its_rows(host):
+    M, F = 40, 64
+    allowed(back(host, dgate=mat(G, M, F)))
+    allowed(back(host, dup=mat(G, M, F)))
+    allowed(back(host, dh=mat(G, M, F, 2 * F), dgate=mat(G, M, F, 2 * F), dup=mat(G + 2 * F, M, F, 2 * F)))
+    # dh is contiguous, dgate the first half of a wider matrix that begins there: its row 1 is dh's row 2
+    refused(back(host, dgate=mat(G, M, F, 2 * F)), "gated_linear_backward: dgate overlaps dh")
+    refused(back(host, dup=mat(G, M, F, 2 * F)), "gated_linear_backward: dup overlaps dh")
+    refused(back(host, dup=mat(G + 2 * F, M, F, 2 * F)), "gated_linear_backward: dup overlaps dh")         # (... the second half)
+    refused(back(host, dh=mat(G, M, F, 2 * F), dgate=mat(G, M, F)), "gated_linear_backward: dgate overlaps dh")
+    allowed(back(host, M=1, dh=mat(G, 1, F), dgate=mat(G, 1, F, 2 * F)))                                   # (one row)
+    refused(back(host, dx=mat(G, M, 48)), "gated_linear_backward: dx overlaps dh")
+    allowed(back(host, K=F, wg=mat(6 * G, F, F), wu=mat(7 * G, F, F), dx=mat(G, M, F)))
+    refused(back(host, K=F, wg=mat(6 * G, F, F), wu=mat(7 * G, F, F), dx=mat(G, M, F, F + 8)), "gated_linear_backward: dx overlaps dh")
+    refused(back(host, dx=mat(4 * G + 2, M, 48)), "gated_linear_backward: dgate overlaps dx")
+    refused(back(host, dx=mat(5 * G + 2 * F, M, 48, 100)), "gated_linear_backward: dup overlaps dx")
+    refused(back(host, dx=mat(7 * G + 6, M, 48)), "gated_linear_backward: dx overlaps w_up")
+
+
+def test_a_checkpoint_in_the_place_of_another_is_all_of_it(host):
+    M, F = 40, 64
+    for product in (True, False):
+        allowed(back(host, h_c=place(2, M, F), product=product))
+        allowed(back(host, h_c=place(3, M, F), product=product))
+        allowed(back(host, up=place(2, M, F), h_c=place(2, M, F), product=product))
+        allowed(back(host, gate=place(2, M, F, ld_q=80, ld_scale=5), h_c=place(2, M, F, ld_q=80, ld_scale=5), product=product))
+        refused(back(host, h_c=place(2, M, F, ld_q=80), product=product), "gated_linear_backward: h_c overlaps gate")
+        refused(back(host, h_c=place(3, M, F, ld_scale=5), product=product), "gated_linear_backward: h_c overlaps up")
+        refused(back(host, h_c=ckpt(2 * G, 9 * G, M, F), product=product), "gated_linear_backward: h_c overlaps gate")
+        refused(back(host, h_c=ckpt(9 * G, 3 * G + G // 2, M, F), product=product), "gated_linear_backward: h_c.scale overlaps up.scale")
+        refused(back(host, h_c=ckpt(2 * G, 3 * G + G // 2, M, F), product=product), "gated_linear_backward: h_c overlaps gate")
+        refused(back(host, h_c=ckpt(4 * G, 9 * G, M, F), product=product), "gated_linear_backward: dgate overlaps h_c")
+
+
+def test_h_and_its_checkpoints_lie_by_themselves(host):
+    M, F = 40, 48
+    allowed(gated(host))
+    allowed(gated(host, gate=place(5, M, F), up=place(6, M, F)))
+    refused(gated(host, h=mat(G, M, F)), "gated_linear: h is x or a weight matrix")
+    refused(gated(host, h=mat(G + 2, M, F)), "gated_linear: h overlaps x")
+    refused(gated(host, h=mat(G + 8, M, F, 200)), "gated_linear: h overlaps x")
+    refused(gated(host, h=mat(3 * G - 64, M, F)), "gated_linear: h overlaps w_up")
+    refused(gated(host, gate=ckpt(4 * G, 9 * G, M, F)), "gated_linear: h overlaps gate")
+    refused(gated(host, up=ckpt(9 * G, 2 * G + 7, M, F)), "gated_linear: up.scale overlaps w_gate")
+    refused(gated(host, gate=ckpt(5 * G, 5 * G + 40, M, F)), "gated_linear: gate overlaps gate.scale")
+    refused(gated(host, gate=place(5, M, F), up=ckpt(5 * G + 8, 9 * G, M, F)), "gated_linear: gate overlaps up")
+    # the two halves of a matrix's columns, and rows that take turns with those of x
+    allowed(gated(host, x=mat(G, M, 48, 96), h=mat(G + 96, M, F, 96)))
+    allowed(gated(host, x=mat(G, M, 48, 100), h=mat(G + 98, M, F, 100)))
+    refused(gated(host, x=mat(G, M, 48, 96), h=mat(G + 94, M, F, 96)), "gated_linear: h overlaps x")
+    refused(gated(host, x=mat(G, M, 48, 96), h=mat(G + 98, M, F, 96)), "gated_linear: h overlaps x")
+    allowed(gated(host, x=mat(G, M, 48, 96), h=mat(G + 96 + 192 * (M - 1), M, F, 96)))
+    allowed(gated(host, M=1, x=mat(G, 1, 48), h=mat(G + 96, 1, F)))
+
+
+def test_overlaps_are_those_of_the_bytes(host):
+    """Random places, against the sets of bytes."""
+    rng = random.Random(4)
+    met = 0
+    for _ in range(600):
+        M, K, F, type = rng.randint(1, 6), rng.randint(1, 5), rng.randint(1, 5), rng.choice([BF16, F32])
+        size = SIZE[type]
+        ld_x = rng.choice([K, K + rng.randint(0, 12), 12])
+        ld_h = rng.choice([F, F + rng.randint(0, 12), 12, max(ld_x, F)])
+        at = G + size * rng.randint(-30, 60)
+        row = lambda begin, ld, n: {b for r in range(M) for b in range(begin + r * ld * size, begin + (r * ld + n) * size)}
+        meets = bool(row(G, ld_x, K) & row(at, ld_h, F))
+        reply = gated(host, M, K, F, x=mat(G, M, K, ld_x, type), h=mat(at, M, F, ld_h, type), type=type)
+        assert (reply.code == INVAL) == meets and bool(reply.launches) != meets, (M, K, F, ld_x, ld_h, at - G, reply)
+        if meets:
+            assert reply.error in ("gated_linear: h overlaps x", "gated_linear: h is x or a weight matrix")
+        met += meets
+    assert 100 < met < 500

@@ -79,6 +79,12 @@ OpsScratch &ops_scratch(const tensile_ops *ops, hipStream_t stream) {
 
 namespace {
 
+#define TS_TRY(call)                          \
+    do {                                      \
+        const int rc_ = (call);               \
+        if (rc_ != TENSILE_OK) return rc_;    \
+    } while (0)
+
 constexpr int64_t kMostCols = int64_t{1} << 30;   // columns are counted in 32 bits
 constexpr int64_t kMostRows = int64_t{1} << 40;
 
@@ -221,6 +227,19 @@ int check_apart(const char *who, const Span &out, std::initializer_list<Span> ot
     return TENSILE_OK;
 }
 
+int check_norm_places(const char *who, const tensile_matrix *x, const tensile_matrix *residual, const tensile_matrix *y, const tensile_matrix *total,
+                      const tensile_ckpt *xhat) {
+    const Span x_at = span(x, "x"), r_at = span(residual, "residual"), y_at = span(y, "y"), t_at = span(total, "total"), c_at = span(xhat, "xhat"),
+               scales = scale_span(xhat, "xhat.scale");
+    TS_TRY(check_apart(who, y_at, {t_at, c_at, scales}, {x_at, r_at}));
+    TS_TRY(check_apart(who, t_at, {c_at, scales}, {x_at, r_at}));
+    TS_TRY(check_apart(who, c_at, {x_at, r_at, scales}));
+    return check_apart(who, scales, {x_at, r_at});
+}
+int check_norm_backward_places(const char *who, const tensile_matrix *dy, const tensile_ckpt *xhat, const tensile_matrix *dresidual, const tensile_matrix *dx) {
+    return check_apart(who, span(dx, "dx"), {span(xhat, "xhat"), scale_span(xhat, "xhat.scale")}, {span(dy, "dy"), span(dresidual, "dresidual")});
+}
+
 Matrix view(const tensile_matrix *m) { return m ? Matrix{m->data, m->ld} : Matrix{nullptr, 0}; }
 Ckpt view(const tensile_ckpt *c) { return c ? Ckpt{c->q, c->scale, c->ld_q, c->ld_scale} : Ckpt{nullptr, nullptr, 0, 0}; }
 
@@ -237,12 +256,6 @@ int guarded(const char *who, F f) {
         return TENSILE_E_HIP;
     }
 }
-
-#define TS_TRY(call)                          \
-    do {                                      \
-        const int rc_ = (call);               \
-        if (rc_ != TENSILE_OK) return rc_;    \
-    } while (0)
 
 }  // namespace
 
@@ -370,6 +383,7 @@ int tensile_rms_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_ma
         TS_TRY(check_param(gamma, param_type, x->type, who, "gamma"));
         TS_TRY(check_eps(eps, who));
         if (x->rows == 0) return TENSILE_OK;
+        TS_TRY(check_norm_places(who, x, residual, y, total, xhat));
         NormArgs a{};
         a.rows = x->rows;
         a.cols = static_cast<int32_t>(x->cols);
@@ -397,6 +411,7 @@ int tensile_rms_norm_backward(tensile_ops *ops, const tensile_matrix *dy, const 
         TS_TRY(check_param(gamma, param_type, dy->type, who, "gamma"));
         if (dgamma) TS_TRY(check_param(dgamma, param_type, dy->type, who, "dgamma"));
         if (dy->rows == 0 && !dgamma) return TENSILE_OK;
+        TS_TRY(check_norm_backward_places(who, dy, xhat, dresidual, dx));
         NormArgs a{};
         a.rows = dy->rows;
         a.cols = static_cast<int32_t>(dy->cols);

@@ -3,7 +3,7 @@ import random
 
 import pytest
 
-from host_calls import BF16, F32, SIZE, Host, ckpt, mat
+from host_calls import BF16, F32, SIZE, Host, ckpt, mat, ptr
 
 G = 1 << 34                                             # places that are far from each other
 INVAL = -1
@@ -115,3 +115,56 @@ def test_overlaps_are_those_of_the_bytes(host):
             assert reply.error in ("gated_linear: h overlaps x", "gated_linear: h is x or a weight matrix")
         met += meets
     assert 100 < met < 500
+
+
+# ------------------------------------------------------------------ norms
+
+def norm(host, name="rms_norm", M=40, K=48, x=None, residual=None, y=None, total=None, xhat=None):
+    params = [ptr(9 * G)] if name == "rms_norm" else [ptr(9 * G), ptr(10 * G)]
+    return host(name, x or mat(1 * G, M, K), residual, *params, F32, 1e-6, y or mat(3 * G, M, K), total, xhat, ptr(8 * G))
+
+
+def norm_back(host, name="rms_norm_backward", M=40, K=48, dy=None, xhat=None, dresidual=None, dx=None):
+    params = [ptr(10 * G)] if name == "rms_norm_backward" else [ptr(10 * G), ptr(11 * G)]
+    return host(name, dy or mat(1 * G, M, K), xhat or place(2, M, K), ptr(8 * G), ptr(9 * G), F32, dresidual, dx or mat(4 * G, M, K), *params)
+
+
+@pytest.mark.parametrize("name", ["rms_norm"])
+def test_a_norm_in_place_has_its_inputs_rows(host, name):
+    M, K = 40, 48
+    call = lambda **a: norm(host, name, **a)
+    r = mat(2 * G, M, K, 60)
+    allowed(call(residual=r, total=mat(4 * G, M, K), xhat=place(5, M, K)))
+    allowed(call(y=mat(G, M, K)))
+    allowed(call(residual=r, y=r, total=mat(G, M, K)))
+    allowed(call(residual=mat(G, M, K), y=mat(G, M, K)))
+    allowed(call(M=1, y=mat(G, 1, K, 100)))
+    allowed(call(x=mat(G, M, K, 96), y=mat(G + 96, M, K, 96)))
+    refused(call(y=mat(G, M, K, 56)), f"{name}: y overlaps x")
+    refused(call(x=mat(G, M, K, 56), y=mat(G, M, K)), f"{name}: y overlaps x")
+    refused(call(residual=r, y=mat(2 * G, M, K)), f"{name}: y overlaps residual")
+    refused(call(residual=r, total=mat(2 * G, M, K)), f"{name}: total overlaps residual")
+    refused(call(total=mat(G, M, K, 64)), f"{name}: total overlaps x")
+    refused(call(total=mat(3 * G, M, K, 64)), f"{name}: total is y")
+    refused(call(total=mat(3 * G + 8, M, K, 64)), f"{name}: y overlaps total")
+    refused(call(y=mat(G + 2, M, K)), f"{name}: y overlaps x")
+    refused(call(xhat=ckpt(G, 6 * G, M, K)), f"{name}: xhat overlaps x")
+    refused(call(xhat=ckpt(6 * G, 3 * G + 5, M, K)), f"{name}: y overlaps xhat.scale")
+    refused(call(xhat=ckpt(6 * G, 6 * G + 47, M, K)), f"{name}: xhat overlaps xhat.scale")
+
+
+@pytest.mark.parametrize("name", ["rms_norm_backward"])
+def test_a_norms_gradient_in_place_has_its_rows(host, name):
+    M, K = 40, 48
+    call = lambda **a: norm_back(host, name, **a)
+    d = mat(3 * G, M, K, 60)
+    allowed(call(dresidual=d))
+    allowed(call(dx=mat(G, M, K)))
+    allowed(call(dresidual=d, dx=d))
+    allowed(call(dresidual=mat(G, M, K), dx=mat(G, M, K)))
+    allowed(call(M=1, dx=mat(G, 1, K, 100)))
+    refused(call(dx=mat(G, M, K, 56)), f"{name}: dx overlaps dy")
+    refused(call(dresidual=d, dx=mat(3 * G, M, K)), f"{name}: dx overlaps dresidual")
+    refused(call(dresidual=mat(G, M, K), dy=mat(5 * G, M, K), dx=mat(G + 4, M, K)), f"{name}: dx overlaps dresidual")
+    refused(call(dx=mat(2 * G - 2, M, K)), f"{name}: dx overlaps xhat")
+    refused(call(dx=mat(2 * G + G // 2 + 2, M, K)), f"{name}: dx overlaps xhat.scale")

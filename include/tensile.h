@@ -383,8 +383,8 @@ int tensile_greedy_plan(const tensile_tas *tas, int64_t budget_bytes, const tens
  * contiguous; rows may lie further apart than cols (ld), at any alignment that
  * suits the element.  Pointers are DEVICE pointers.  rows == 0 is allowed everywhere (gradients of
  * parameters are then zero); cols >= 1.  An output may be the very matrix (its rows as far apart) or checkpoint (its bytes and its scales) that is
- * named for it below and must not overlap any other input or output: it would be written while others read.  (The root-mean-square
- * norm, the gated layer and their backward passes refuse matrices and checkpoints that do; rows that lie between another's rows do not.)  The
+ * named for it below and must not overlap any other input or output: it would be written while others read.  (Calls refuse matrices
+ * and checkpoints that do; rows that lie between another's rows do not.)  The
  * calls are asynchronous on hip_stream and never wait for the device.  Results do not
  * depend on timing: the same call on the same inputs gives the same bits.
  *

@@ -227,14 +227,21 @@ int check_apart(const char *who, const Span &out, std::initializer_list<Span> ot
     return TENSILE_OK;
 }
 
+int check_ckpt_apart(const char *who, const tensile_ckpt *c, const char *name, const char *scale_name, std::initializer_list<Span> others) {
+    const Span scales = scale_span(c, scale_name);
+    TS_TRY(check_apart(who, span(c, name), others));
+    TS_TRY(check_apart(who, span(c, name), {scales}));
+    return check_apart(who, scales, others);
+}
+bool same_ckpt(const tensile_ckpt *a, const tensile_ckpt *b) { return identical(span(a, ""), span(b, "")) && identical(scale_span(a, ""), scale_span(b, "")); }
+
 int check_norm_places(const char *who, const tensile_matrix *x, const tensile_matrix *residual, const tensile_matrix *y, const tensile_matrix *total,
                       const tensile_ckpt *xhat) {
     const Span x_at = span(x, "x"), r_at = span(residual, "residual"), y_at = span(y, "y"), t_at = span(total, "total"), c_at = span(xhat, "xhat"),
                scales = scale_span(xhat, "xhat.scale");
     TS_TRY(check_apart(who, y_at, {t_at, c_at, scales}, {x_at, r_at}));
     TS_TRY(check_apart(who, t_at, {c_at, scales}, {x_at, r_at}));
-    TS_TRY(check_apart(who, c_at, {x_at, r_at, scales}));
-    return check_apart(who, scales, {x_at, r_at});
+    return xhat ? check_ckpt_apart(who, xhat, "xhat", "xhat.scale", {x_at, r_at}) : TENSILE_OK;
 }
 int check_norm_backward_places(const char *who, const tensile_matrix *dy, const tensile_ckpt *xhat, const tensile_matrix *dresidual, const tensile_matrix *dx) {
     return check_apart(who, span(dx, "dx"), {span(xhat, "xhat"), scale_span(xhat, "xhat.scale")}, {span(dy, "dy"), span(dresidual, "dresidual")});
@@ -293,6 +300,7 @@ int tensile_ckpt_pack(tensile_ops *ops, const tensile_matrix *x, const tensile_c
         TS_TRY(check_matrix(x, who, "x"));
         TS_TRY(check_ckpt(c, x->rows, x->cols, who, "c"));
         if (x->rows == 0) return TENSILE_OK;
+        TS_TRY(check_ckpt_apart(who, c, "c", "c.scale", {span(x, "x")}));
         EachArgs a{x->rows, x->cols, view(x), {}, view(c), {}, largest_code(x->type)};
         return launch_pack(ops, static_cast<hipStream_t>(hip_stream), a, x->type);
     });
@@ -305,6 +313,7 @@ int tensile_ckpt_unpack(tensile_ops *ops, const tensile_ckpt *c, const tensile_m
         TS_TRY(check_matrix(y, who, "y"));
         TS_TRY(check_ckpt(c, y->rows, y->cols, who, "c"));
         if (y->rows == 0) return TENSILE_OK;
+        TS_TRY(check_apart(who, span(y, "y"), {span(c, "c"), scale_span(c, "c.scale")}));
         EachArgs a{y->rows, y->cols, {}, view(y), view(c), {}, 0};
         return launch_unpack(ops, static_cast<hipStream_t>(hip_stream), a, y->type);
     });
@@ -326,6 +335,7 @@ int tensile_layer_norm(tensile_ops *ops, const tensile_matrix *x, const tensile_
         TS_TRY(check_param(beta, param_type, x->type, who, "beta"));
         TS_TRY(check_eps(eps, who));
         if (x->rows == 0) return TENSILE_OK;
+        TS_TRY(check_norm_places(who, x, residual, y, total, xhat));
         NormArgs a{};
         a.rows = x->rows;
         a.cols = static_cast<int32_t>(x->cols);
@@ -357,6 +367,7 @@ int tensile_layer_norm_backward(tensile_ops *ops, const tensile_matrix *dy, cons
             TS_TRY(check_param(dbeta, param_type, dy->type, who, "dbeta"));
         }
         if (dy->rows == 0 && !dgamma) return TENSILE_OK;
+        TS_TRY(check_norm_backward_places(who, dy, xhat, dresidual, dx));
         NormArgs a{};
         a.rows = dy->rows;
         a.cols = static_cast<int32_t>(dy->cols);
@@ -452,10 +463,8 @@ int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensil
         const Span x_at = span(x, "x"), wg_at = span(w_gate, "w_gate"), wu_at = span(w_up, "w_up"), h_at = span(h, "h"), g_at = span(gate, "gate"),
                    g_scales = scale_span(gate, "gate.scale"), u_at = span(up, "up"), u_scales = scale_span(up, "up.scale");
         TS_TRY(check_apart(who, h_at, {x_at, wg_at, wu_at, g_at, g_scales, u_at, u_scales}));
-        TS_TRY(check_apart(who, g_at, {x_at, wg_at, wu_at, g_scales, u_at, u_scales}));
-        TS_TRY(check_apart(who, g_scales, {x_at, wg_at, wu_at, u_at, u_scales}));
-        TS_TRY(check_apart(who, u_at, {x_at, wg_at, wu_at, u_scales}));
-        TS_TRY(check_apart(who, u_scales, {x_at, wg_at, wu_at}));
+        if (gate) TS_TRY(check_ckpt_apart(who, gate, "gate", "gate.scale", {x_at, wg_at, wu_at, u_at, u_scales}));
+        if (up) TS_TRY(check_ckpt_apart(who, up, "up", "up.scale", {x_at, wg_at, wu_at}));
         GatedArgs a{};
         a.M = x->rows;
         a.K = static_cast<int32_t>(x->cols);
@@ -502,14 +511,11 @@ int tensile_gated_linear_backward(tensile_ops *ops, const tensile_matrix *dh, co
         TS_TRY(check_apart(who, dgate_at, {g_at, g_scales, u_at, u_scales, wg_at, wu_at, dup_at, dx_at, h_at, h_scales}, {dh_at}));
         TS_TRY(check_apart(who, dup_at, {g_at, g_scales, u_at, u_scales, wg_at, wu_at, dx_at, h_at, h_scales}, {dh_at}));
         TS_TRY(check_apart(who, dx_at, {g_at, g_scales, u_at, u_scales, wg_at, wu_at, h_at, h_scales}, {dh_at}));
-        // (gate's bytes and its scales, or up's, or neither)
-        const bool over_gate = h_c && identical(h_at, g_at) && identical(h_scales, g_scales), over_up = h_c && identical(h_at, u_at) && identical(h_scales, u_scales);
-        TS_TRY(check_apart(who, h_at, {dh_at, wg_at, wu_at, h_scales}));
-        TS_TRY(check_apart(who, h_scales, {dh_at, wg_at, wu_at}));
-        if (!over_gate) TS_TRY(check_apart(who, h_at, {g_at, g_scales}));
-        if (!over_gate) TS_TRY(check_apart(who, h_scales, {g_at, g_scales}));
-        if (!over_up) TS_TRY(check_apart(who, h_at, {u_at, u_scales}));
-        if (!over_up) TS_TRY(check_apart(who, h_scales, {u_at, u_scales}));
+        if (h_c) {
+            TS_TRY(check_ckpt_apart(who, h_c, "h_c", "h_c.scale", {dh_at, wg_at, wu_at}));
+            if (!same_ckpt(h_c, gate)) TS_TRY(check_ckpt_apart(who, h_c, "h_c", "h_c.scale", {g_at, g_scales}));
+            if (!same_ckpt(h_c, up)) TS_TRY(check_ckpt_apart(who, h_c, "h_c", "h_c.scale", {u_at, u_scales}));
+        }
         GatedArgs a{};
         a.M = dh->rows;
         a.F = static_cast<int32_t>(dh->cols);
@@ -533,6 +539,8 @@ int tensile_gelu(tensile_ops *ops, const tensile_matrix *x, const tensile_matrix
         TS_TRY(check_like(y, x, who, "y"));
         if (c) TS_TRY(check_ckpt(c, x->rows, x->cols, who, "c"));
         if (x->rows == 0) return TENSILE_OK;
+        TS_TRY(check_apart(who, span(y, "y"), {}, {span(x, "x")}));
+        if (c) TS_TRY(check_ckpt_apart(who, c, "c", "c.scale", {span(x, "x"), span(y, "y")}));
         EachArgs a{x->rows, x->cols, view(x), view(y), view(c), {}, largest_code(x->type)};
         return launch_gelu(ops, static_cast<hipStream_t>(hip_stream), a, x->type, tanh_form != 0);
     });
@@ -548,6 +556,9 @@ int tensile_gelu_backward(tensile_ops *ops, const tensile_matrix *dy, const tens
         TS_TRY(check_like(dx, dy, who, "dx"));
         if (y_c) TS_TRY(check_ckpt(y_c, dy->rows, dy->cols, who, "y_c"));
         if (dy->rows == 0) return TENSILE_OK;
+        TS_TRY(check_apart(who, span(dx, "dx"), {span(c, "c"), scale_span(c, "c.scale")}, {span(dy, "dy")}));
+        if (y_c) TS_TRY(check_ckpt_apart(who, y_c, "y_c", "y_c.scale", {span(dy, "dy"), span(dx, "dx")}));
+        if (y_c && !same_ckpt(y_c, c)) TS_TRY(check_ckpt_apart(who, y_c, "y_c", "y_c.scale", {span(c, "c"), scale_span(c, "c.scale")}));
         EachArgs a{dy->rows, dy->cols, view(dy), view(dx), view(c), view(y_c), largest_code(dy->type)};
         return launch_gelu_backward(ops, static_cast<hipStream_t>(hip_stream), a, dy->type, tanh_form != 0);
     });
@@ -570,6 +581,7 @@ int tensile_linear_grad(tensile_ops *ops, const tensile_matrix *dy, const tensil
             TS_TRY(check_param(beta, param_type, dy->type, who, "beta"));
         }
         if (dbias && reinterpret_cast<uintptr_t>(dbias) % element_size(dw->type)) return refuse(who, "dbias", "is not aligned to its elements");
+        TS_TRY(check_apart(who, span(dw, "dw"), {span(dy, "dy"), span(c, "c"), scale_span(c, "c.scale")}));
         LinearArgs a{};
         a.M = dy->rows;
         a.N = static_cast<int32_t>(dy->cols);

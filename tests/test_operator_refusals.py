@@ -129,7 +129,7 @@ def norm_back(host, name="rms_norm_backward", M=40, K=48, dy=None, xhat=None, dr
     return host(name, dy or mat(1 * G, M, K), xhat or place(2, M, K), ptr(8 * G), ptr(9 * G), F32, dresidual, dx or mat(4 * G, M, K), *params)
 
 
-@pytest.mark.parametrize("name", ["rms_norm"])
+@pytest.mark.parametrize("name", ["rms_norm", "layer_norm"])
 def test_a_norm_in_place_has_its_inputs_rows(host, name):
     M, K = 40, 48
     call = lambda **a: norm(host, name, **a)
@@ -153,7 +153,7 @@ def test_a_norm_in_place_has_its_inputs_rows(host, name):
     refused(call(xhat=ckpt(6 * G, 6 * G + 47, M, K)), f"{name}: xhat overlaps xhat.scale")
 
 
-@pytest.mark.parametrize("name", ["rms_norm_backward"])
+@pytest.mark.parametrize("name", ["rms_norm_backward", "layer_norm_backward"])
 def test_a_norms_gradient_in_place_has_its_rows(host, name):
     M, K = 40, 48
     call = lambda **a: norm_back(host, name, **a)
@@ -168,3 +168,43 @@ def test_a_norms_gradient_in_place_has_its_rows(host, name):
     refused(call(dresidual=mat(G, M, K), dy=mat(5 * G, M, K), dx=mat(G + 4, M, K)), f"{name}: dx overlaps dresidual")
     refused(call(dx=mat(2 * G - 2, M, K)), f"{name}: dx overlaps xhat")
     refused(call(dx=mat(2 * G + G // 2 + 2, M, K)), f"{name}: dx overlaps xhat.scale")
+
+
+# ------------------------------------------------------------------ elementwise calls and the weight gradient
+
+def test_elementwise_calls_in_place_have_their_inputs_rows(host):
+    M, K = 40, 48
+    x, c = mat(G, M, K), place(2, M, K)
+    gelu = lambda **a: host("gelu", a.get("x", x), a.get("y", mat(3 * G, M, K)), a.get("c"), 0)
+    allowed(gelu(c=c))
+    allowed(gelu(y=x))
+    allowed(gelu(x=mat(G, M, K, 96), y=mat(G + 96, M, K, 96)))
+    refused(gelu(y=mat(G, M, K, 56)), "gelu: y overlaps x")
+    refused(gelu(y=mat(G + 2, M, K)), "gelu: y overlaps x")
+    refused(gelu(c=ckpt(G + 1, 9 * G, M, K)), "gelu: c overlaps x")
+    refused(gelu(c=ckpt(9 * G, 3 * G + 1, M, K)), "gelu: c.scale overlaps y")
+    refused(gelu(c=ckpt(9 * G, 9 * G + 1, M, K)), "gelu: c overlaps c.scale")
+    back = lambda **a: host("gelu_backward", a.get("dy", x), a.get("c", c), a.get("dx", mat(3 * G, M, K)), a.get("y_c"), 0)
+    allowed(back(y_c=place(4, M, K)))
+    allowed(back(y_c=c, dx=x))
+    refused(back(dx=mat(G, M, K, 56)), "gelu_backward: dx overlaps dy")
+    refused(back(y_c=place(2, M, K, ld_q=64)), "gelu_backward: y_c overlaps c")
+    refused(back(y_c=place(2, M, K, ld_scale=4)), "gelu_backward: y_c overlaps c")
+    refused(back(y_c=ckpt(2 * G, 9 * G, M, K)), "gelu_backward: y_c overlaps c")
+    refused(back(y_c=ckpt(9 * G, 2 * G + G // 2, M, K)), "gelu_backward: y_c.scale overlaps c.scale")
+    refused(back(y_c=ckpt(9 * G, 3 * G, M, K)), "gelu_backward: y_c.scale overlaps dx")
+    allowed(host("ckpt_pack", x, c))
+    refused(host("ckpt_pack", x, ckpt(G, 9 * G, M, K)), "ckpt_pack: c overlaps x")
+    refused(host("ckpt_pack", x, ckpt(9 * G, G + 2 * M * K - 1, M, K)), "ckpt_pack: c.scale overlaps x")
+    allowed(host("ckpt_pack", x, ckpt(9 * G, G + 2 * M * K, M, K)))
+    allowed(host("ckpt_unpack", c, x))
+    refused(host("ckpt_unpack", ckpt(G, 9 * G, M, K), x), "ckpt_unpack: y overlaps c")
+
+
+def test_a_weight_gradient_lies_by_itself(host):
+    M, N, K = 40, 24, 48
+    grad = lambda dw: host("linear_grad", mat(G, M, N), place(2, M, K), None, None, F32, dw, None)
+    allowed(grad(mat(3 * G, N, K)))
+    refused(grad(mat(G, N, K)), "linear_grad: dw overlaps dy")
+    refused(grad(mat(2 * G + 4, N, K)), "linear_grad: dw overlaps c")
+    refused(grad(mat(2 * G + G // 2, N, K, type=F32)), "linear_grad: dw overlaps c.scale")

@@ -44,13 +44,20 @@ __global__ __launch_bounds__(kEachThreads) void gated_grad_kernel(Walk w, Matrix
 template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
     const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.q[1], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
+    const int64_t cus = ops->num_cus;
     if (a.M <= 32) {
         const int64_t tiles = (a.R + 63) / 64, steps = 2 * static_cast<int64_t>(a.C) * static_cast<int64_t>(sizeof(T)) / kRow;
-        int64_t split = 2 * static_cast<int64_t>(ops->num_cus) / tiles;
+        int64_t split = 2 * cus / tiles;
         if (split > steps / 4) split = steps / 4;
-        return run_rows<T, false>(ops, s, a, far, split, tiles * split <= ops->num_cus);
+        if (split < 1) split = 1;
+        // Four wavefronts, one workgroup to a CU, or two and two: a round of the former takes half as long, one of the latter hides where workgroups begin and end.
+        // Four and two, us, bf16, tiles x length of each sum: 625 x 60 15.5 and 13.2; 750 x 512 25.2 and 23.2; 750 x 1024 38.3 and 37.5; 750 x 1500 64 and 66.5; 625 x 2048
+        // 69 and 76; 1250 x 2048 128 and 132; 1024 x 512 31.5 and 27.5; 2048 x 1024 115 and 108; f32 625 x 2048 140 and 164, 1024 x 512 71 and 60.
+        const int64_t n = tiles * split;
+        const bool four = n <= cus || (steps >= 40 && rounds(n, cus) < 2 * rounds(n, 2 * cus));
+        return run_rows<T, false>(ops, s, a, far, split, four);
     }
-    const int64_t cus = ops->num_cus, small = tiles_of<Small, false>(a);
+    const int64_t small = tiles_of<Small, false>(a);
     if (small <= cus || far) return run_tiles<T, Few, false>(ops, s, a, far, parts_of(small, cus, steps_of<T, false>(a)));
     // A round of tiles, as many as the card has places for, takes 1 where they are large, 0.47 of middle size and 0.65 where they are small (two to a CU).
     // Large, middle and small (us, dx alone): 8192 x 4096 x 10944 1113, 1497 and 1442; 8192 x 768 x 2048 88, 52 and 58.

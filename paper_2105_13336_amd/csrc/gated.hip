@@ -7,22 +7,22 @@ namespace {
 
 template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
-    const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
     if (a.M <= 32) {
         // Few features and long sums: these are split, four wavefronts to a part, where that saves more than adding them up and its launch take (4 us, and 2.5 on the
         // host).  Whole and split, us: f32 32 x 784 x 512 14 and 9 + 4, 32 x 1568 x 544 20 and 8 + 4, 32 x 3136 x 576 33 and 9 + 5; bf16 32 x 6272 x 800 16 and 8.5 + 4.
         const int64_t tiles = (a.R + 31) / 32, each = steps_of<T, true>(a) / 4, fill = ops->num_cus / tiles;
         constexpr int64_t kLong = sizeof(T) == 2 ? 32 : 12, kLeast = sizeof(T) == 2 ? 4 : 2;
         const int64_t most = each >= kLong ? each / kLeast : 1;
-        return run_rows<T, true>(ops, s, a, far, fill < most ? fill : most, tiles <= ops->num_cus);
+        return run_rows<T, true>(ops, s, a, is_far<T, Rows, true>(a), fill < most ? fill : most, tiles <= ops->num_cus);
     }
     const int64_t cus = ops->num_cus, small = tiles_of<Small, true>(a);
+    const bool far = is_far<T, Few, true>(a);                            // (tiles of Small are as large)
     if (small <= cus || far) return run_tiles<T, Few, true>(ops, s, a, far, parts_of(small, cus, steps_of<T, true>(a)));
     // A round of tiles, as many as the card has places for, takes 1 where they are large and 0.65 where they are small (two to a CU).  Large and small (us, with
     // checkpoints): 8192 x 4096 x 10944 1180 and 1450; 8192 x 768 x 2048 67 and 81 (both before stores went past the caches); 4096 x 768 x 2048 33 and 37; 2048 x 768 x 2048 28 and 20.
     // (In 32 bits, where the matrix instructions take 16 times as long, small tiles do, which have the registers to add up by steps.)
     if constexpr (sizeof(T) == 2) {
-        if (20 * rounds(tiles_of<Large, true>(a), cus) <= 13 * rounds(small, 2 * cus)) return run_tiles<T, Large, true>(ops, s, a);
+        if (!is_far<T, Large, true>(a) && 20 * rounds(tiles_of<Large, true>(a), cus) <= 13 * rounds(small, 2 * cus)) return run_tiles<T, Large, true>(ops, s, a);
     }
     return run_tiles<T, Small, true>(ops, s, a);
 }

@@ -43,7 +43,6 @@ __global__ __launch_bounds__(kEachThreads) void gated_grad_kernel(Walk w, Matrix
 
 template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
-    const bool far = is_far(a.q[0], sizeof(T)) || is_far(a.q[1], sizeof(T)) || is_far(a.p[0], sizeof(T)) || is_far(a.p[1], sizeof(T));
     const int64_t cus = ops->num_cus;
     if (a.M <= 32) {
         const int64_t tiles = (a.R + 63) / 64, steps = 2 * static_cast<int64_t>(a.C) * static_cast<int64_t>(sizeof(T)) / kRow;
@@ -55,16 +54,17 @@ int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
         // 69 and 76; 1250 x 2048 128 and 132; 1024 x 512 31.5 and 27.5; 2048 x 1024 115 and 108; f32 625 x 2048 140 and 164, 1024 x 512 71 and 60.
         const int64_t n = tiles * split;
         const bool four = n <= cus || (steps >= 40 && rounds(n, cus) < 2 * rounds(n, 2 * cus));
-        return run_rows<T, false>(ops, s, a, far, split, four);
+        return run_rows<T, false>(ops, s, a, is_far<T, Rows, false>(a), split, four);
     }
     const int64_t small = tiles_of<Small, false>(a);
+    const bool far = is_far<T, Few, false>(a);                           // (tiles of Small and Middle are as many tokens)
     if (small <= cus || far) return run_tiles<T, Few, false>(ops, s, a, far, parts_of(small, cus, steps_of<T, false>(a)));
     // A round of tiles, as many as the card has places for, takes 1 where they are large, 0.47 of middle size and 0.65 where they are small (two to a CU).
     // Large, middle and small (us, dx alone): 8192 x 4096 x 10944 1113, 1497 and 1442; 8192 x 768 x 2048 88, 52 and 58.
     // (In 32 bits, where the matrix instructions take 16 times as long, small tiles do, which have the registers to add up by steps.)
     if constexpr (sizeof(T) == 2) {
         const int64_t l = 100 * rounds(tiles_of<Large, false>(a), cus), m = 47 * rounds(tiles_of<Middle, false>(a), cus), n = 65 * rounds(small, 2 * cus);
-        if (l <= m && l <= n) return run_tiles<T, Large, false>(ops, s, a);
+        if (l <= m && l <= n && !is_far<T, Large, false>(a)) return run_tiles<T, Large, false>(ops, s, a);
         if (m <= n) return run_tiles<T, Middle, false>(ops, s, a);
     }
     return run_tiles<T, Small, false>(ops, s, a);

@@ -873,16 +873,28 @@ int run_rows(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &whole, 
     });
 }
 
-// Rows further apart than this are reached by 64-bit addresses only (256 of them, or 32 of a step, from a scalar one).
-constexpr int64_t kFarBytes = 1 << 23;
-inline bool is_far(const Matrix &m, int64_t size) { return m.ld * size >= kFarBytes; }
-
 // (Four wavefronts of 128 x 128, one to a SIMD, read the LDS a third less and are slower all the same, 1461 us against 1138 at 8192 x 4096 x 10944: nothing runs while
 // one waits.  256 x 128 with three steps of half lines, two workgroups to a CU: 1399 against 1230 then.)
 using Large = Tile<4, 2, 2, 4, 1, 2>;    // 256 x 256
 using Middle = Tile<3, 1, 2, 4, 1, 3>;   // 192 x 128
 using Small = Tile<2, 2, 2, 2, 2, 2>;    // 128 x 128
 using Few = Tile<2, 2, 2, 2, 1, 4>;      // 128 x 128, for splits: four steps in the LDS
+
+// Whether the rows that a tile of G reads from one scalar address lie too far apart for offsets of 32 bits (kept below 2^31): its tokens, its features forward, a
+// step's rows of the weights backward.  They are reached by 64-bit addresses then, and every step goes by way of registers.  24 x 4096 x 10944 bf16, us: tokens 8 KB, 16 MB and
+// 64 MB apart 42.1, 43.5 and 43.0; 96 MB apart, which is too far, 73.6.
+constexpr int64_t kFarBytes = (int64_t{1} << 31) - (1 << 12);            // (less than a row's part of a step)
+inline bool is_far(const Matrix &m, int64_t rows, int64_t at_once, int64_t size) {
+    return (rows < at_once ? rows - 1 : at_once - 1) * m.ld * size >= kFarBytes;
+}
+template <typename T, typename G, bool kForward>
+bool is_far(const ProductArgs &a) {
+    constexpr int64_t kSize = sizeof(T);
+    bool far = false;
+    for (int k = 0; k < 2; ++k)
+        far = far || is_far(a.q[k], a.M, G::kTok, kSize) || is_far(a.p[k], kForward ? a.R : a.C, kForward ? G::kP / 2 : kRow / kSize, kSize);
+    return far;
+}
 
 inline int64_t rounds(int64_t tiles, int64_t places) { return (tiles + places - 1) / places; }
 template <typename T, bool kForward>

@@ -5,7 +5,7 @@ import pytest
 
 from host_calls import BF16, F16, F32, Host, ckpt, mat
 
-G = 1 << 36                                             # places that are far from each other
+G = 1 << 44                                             # places that are far from each other
 
 
 @pytest.fixture(scope="module")
@@ -60,3 +60,56 @@ def test_few_tokens_backward_by_the_workgroups_that_there_are(host):
     for tiles in (16, 256):
         assert backward(host, 8, 64 * tiles, 60) == [("rows4", tiles)]
     assert backward(host, 8, 64 * 256, 4_096) == [("rows2", 512), ("join", 256)]
+
+
+def test_rows_are_too_far_apart_where_a_tiles_offsets_pass_32_bits(host):
+    """From the first to the last of the rows that a workgroup reads from one address, 2 GiB less 4 KiB; not by the distance of two rows alone."""
+    span = (1 << 31) - (1 << 12)                        # bytes
+    near = lambda rows: (span - 1) // (rows - 1) // 2   # elements of 16 bits
+    # the last tokens of 24 sequences, up to 32 tokens
+    for M in (2, 24, 32):
+        assert forward(host, M, 4_096, 10_944, ld_x=1 << 23) == [("rows2", 342)]
+        assert forward(host, M, 4_096, 10_944, ld_x=near(M)) == [("rows2", 342)]
+        assert forward(host, M, 4_096, 10_944, ld_x=near(M) + 1) == [("rows4 far", 342)]
+        assert backward(host, M, 4_096, 10_944, ld=near(M)) == [("rows2", 512), ("join", 64)]
+        assert backward(host, M, 4_096, 10_944, ld=near(M) + 1) == [("rows4 far", 512), ("join", 64)]
+    assert forward(host, 1, 4_096, 10_944, ld_x=1 << 40) == [("rows2", 342)]
+    assert forward(host, 24, 4_096, 10_944, ld_w=near(32)) == [("rows2", 342)]
+    assert forward(host, 24, 4_096, 10_944, ld_w=near(32) + 1) == [("rows4 far", 342)]
+    assert backward(host, 24, 4_096, 10_944, ld_w=near(64)) == [("rows2", 512), ("join", 64)]
+    assert backward(host, 24, 4_096, 10_944, ld_w=near(64) + 1) == [("rows4 far", 512), ("join", 64)]
+    # tiles: 128 tokens and 64 features, large ones 256 and 128
+    assert forward(host, 100, 512, 640, ld_x=near(100)) == [("few", 10)]
+    assert forward(host, 100, 512, 640, ld_x=near(100) + 1) == [("few far", 10)]
+    assert forward(host, 2_048, 768, 4_096) == [("large", 256)]
+    assert forward(host, 2_048, 768, 4_096, ld_x=near(256)) == [("large", 256)]
+    assert forward(host, 2_048, 768, 4_096, ld_x=near(256) + 1) == [("small", 1_024)]
+    assert forward(host, 2_048, 768, 4_096, ld_x=near(128)) == [("small", 1_024)]
+    assert forward(host, 2_048, 768, 4_096, ld_x=near(128) + 1) == [("few far", 1_024)]
+    assert forward(host, 2_048, 768, 4_096, ld_w=near(128)) == [("large", 256)]
+    assert forward(host, 2_048, 768, 4_096, ld_w=near(128) + 1) == [("small", 1_024)]
+    assert forward(host, 2_048, 768, 4_096, ld_w=near(64) + 1) == [("few far", 1_024)]
+    assert backward(host, 4_096, 4_096, 330) == [("large", 256)]
+    assert backward(host, 4_096, 4_096, 330, ld=near(256)) == [("large", 256)]
+    assert backward(host, 4_096, 4_096, 330, ld=near(256) + 1) == [("small", 1_024)]
+    assert backward(host, 4_096, 4_096, 330, ld=near(128) + 1) == [("few far", 1_024)]
+    assert backward(host, 4_096, 4_096, 330, ld_w=near(64)) == [("large", 256)]
+    assert backward(host, 4_096, 4_096, 330, ld_w=near(64) + 1) == [("few far", 1_024)]
+    # in 32 bits half as many rows of the weights to a step
+    assert backward(host, 2_049, 2_100, 230, F32, ld_w=(span - 1) // 31 // 4) == [("small", 289)]
+    assert backward(host, 2_049, 2_100, 230, F32, ld_w=(span - 1) // 31 // 4 + 1) == [("few far", 289)]
+    # what test_gpu_gated_kernels.py means by far, and by what offsets still reach
+    whole = 1 << 31
+    for type, size, step in ((BF16, 2, 64), (F16, 2, 64), (F32, 4, 32)):
+        for M, K, F, ld in ((24, 520, 200, (16 << 20) // size), (32, 333, 100, (64 << 20) // size)):
+            for name, _ in forward(host, M, K, F, type, ld_x=ld) + backward(host, M, K, F, type, ld=ld):
+                assert name in ("rows4", "rows2", "join")
+        for M, K, F, ld in ((5, 520, 200, whole // 4 // size + 8), (32, 333, 700, whole // 31 // size + 8)):
+            assert forward(host, M, K, F, type, ld_x=ld)[0][0] == "rows4 far" and backward(host, M, K, F, type, ld=ld)[0][0] == "rows4 far"
+        assert forward(host, 7, 130, 100, type, ld_w=(16 << 20) // size)[0][0] == "rows4" and backward(host, 7, 130, 100, type, ld_w=(16 << 20) // size)[0][0] == "rows4"
+        ld = whole // (step - 1) // size + 8
+        assert backward(host, 20, 130, 65, type, ld_w=ld)[0][0] == "rows4 far" and backward(host, 200, 300, 150, type, ld_w=ld)[0][0] == "few far"
+        assert forward(host, 20, 130, 33, type, ld_w=whole // 31 // size + 8)[0][0] == "rows4 far"
+        assert forward(host, 100, 520, 200, type, ld_x=(16 << 20) // size)[0][0] == "few" and backward(host, 100, 520, 200, type, ld=(16 << 20) // size)[0][0] == "few"
+        for M, K, F, ld in ((130, 130, 2_000, whole // 127 // size + 8), (40, 1_700, 90, whole // 39 // size + 8), (256, 40, 9_000, whole // 127 // size + 8)):
+            assert forward(host, M, K, F, type, ld_x=ld)[0][0] == "few far" and backward(host, M, K, F, type, ld=ld)[0][0] == "few far"

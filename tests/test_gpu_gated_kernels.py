@@ -1,0 +1,92 @@
+"""The gated layer's kernels at sizes that reach each of them (test_gated_kernels.py asserts which sizes do), against 64 bits."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import gated_plain as plain  # noqa: E402
+import paper_2105_13336_amd as P  # noqa: E402
+from ops_plain import CAP, FLOOR, ROUND, U  # noqa: E402
+from test_gpu_gated import T, TYPES, filled, host, near, room, say, up  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def ops():
+    h = P.tensile_ops_create()
+    yield h
+    h.close()
+
+
+# ------------------------------------------------------------------ rows far apart
+
+def apart(a, ld, dtype):
+    """a with its rows ld elements apart"""
+    buf = torch.empty(((a.shape[0] - 1) * ld + a.shape[1],), dtype=T[dtype], device="cuda")
+    return buf.as_strided(a.shape, (ld, 1)).copy_(a)
+
+
+def check_apart(ops, dtype, M, K, F, ld_tokens=None, ld_weights=None):
+    """x, dgate and dup, or the weights, with their rows so far apart, against 64 bits."""
+    say(f"{dtype} {M}x{K}x{F}, rows {ld_tokens}, {ld_weights} apart")
+    rng = np.random.default_rng(M + K + F)
+    far = lambda t, ld: apart(t, ld, dtype) if ld else t
+    x = far(up(rng.standard_normal((M, K)), dtype), ld_tokens)
+    wg, wu = (far(up(rng.standard_normal((F, K)) * K ** -0.5, dtype), ld_weights) for _ in range(2))
+    h = room(M, F, dtype)
+    P.tensile_gated_linear(ops, x, wg, wu, h)
+    x0, wg0, wu0 = host(x), host(wg), host(wu)
+    h0, g0, u0 = plain.gated(x0, wg0, wu0, 0.0, 0.0, "silu")
+    n = plain.chain(K, dtype, 64)
+    eg, eu = (n * U * (np.abs(x0) @ np.abs(w).T) for w in (wg0, wu0))
+    value, ev = np.abs(plain.activation(g0, "silu")[0]), 1.13 * eg + plain.activation_error(g0, "silu", dtype)[0]
+    near(h, h0, (ROUND[dtype] + 2 * U) * np.abs(h0) + FLOOR[dtype] + 1.01 * (ev * (np.abs(u0) + eu) + value * eu), "h")
+    del x, h
+    (cg, _), (cu, _) = (filled(rng.standard_normal((M, F)), CAP[dtype]) for _ in range(2))
+    dgate, dup, dx = far(room(M, F, dtype), ld_tokens), far(room(M, F, dtype), ld_tokens), room(M, K, dtype)
+    P.tensile_gated_linear_backward(ops, up(rng.standard_normal((M, F)), dtype), cg, cu, dgate, dup, w_gate=wg, w_up=wu, dx=dx)
+    a, b = host(dgate), host(dup)
+    want = a @ wg0 + b @ wu0
+    size = np.abs(a) @ np.abs(wg0) + np.abs(b) @ np.abs(wu0)
+    near(dx, want, (ROUND[dtype] + U) * np.abs(want) + FLOOR[dtype] + plain.chain(2 * F, dtype, 64) * U * size, "dx")
+
+
+SPAN = 1 << 31                                          # bytes from the first row to the last
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tokens_far_apart_up_to_32(ops, dtype):
+    """The last tokens of sequences: 16 MiB apart, whose offsets fit 32 bits, and too far."""
+    size = 4 if dtype == "f32" else 2
+    check_apart(ops, dtype, 24, 520, 200, ld_tokens=(16 << 20) // size)
+    check_apart(ops, dtype, 32, 333, 100, ld_tokens=(64 << 20) // size)
+    check_apart(ops, dtype, 5, 520, 200, ld_tokens=SPAN // 4 // size + 8)
+    check_apart(ops, dtype, 32, 333, 700, ld_tokens=SPAN // 31 // size + 8)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_weights_far_apart_up_to_32_tokens(ops, dtype):
+    size, step = (4, 32) if dtype == "f32" else (2, 64)
+    check_apart(ops, dtype, 7, 130, 100, ld_weights=(16 << 20) // size)
+    check_apart(ops, dtype, 20, 130, 65, ld_weights=SPAN // (step - 1) // size + 8)
+    check_apart(ops, dtype, 20, 130, 33, ld_weights=SPAN // 31 // size + 8)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tiles_of_rows_far_apart(ops, dtype):
+    """Up to 16 MiB apart, and too far: 128 tokens (few, with sums split and whole, and many), 64 features, a step's rows of the weights."""
+    size = 4 if dtype == "f32" else 2
+    check_apart(ops, dtype, 100, 520, 200, ld_tokens=(16 << 20) // size)
+    check_apart(ops, dtype, 130, 130, 2_000, ld_tokens=SPAN // 127 // size + 8)
+    check_apart(ops, dtype, 40, 1_700, 90, ld_tokens=SPAN // 39 // size + 8)
+    check_apart(ops, dtype, 256, 40, 9_000, ld_tokens=SPAN // 127 // size + 8)
+    check_apart(ops, dtype, 200, 300, 150, ld_weights=SPAN // (31 if dtype == "f32" else 63) // size + 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_large_tiles_of_rows_far_apart_are_small_ones(ops, dtype):
+    check_apart(ops, dtype, 2_040, 200, 3_901, ld_tokens=(9 << 20) // 2)
+    check_apart(ops, dtype, 2_040, 200, 3_901, ld_tokens=(8 << 20) // 2)

@@ -3,6 +3,7 @@ import re
 
 import pytest
 
+import gated_sizes
 from host_calls import BF16, F16, F32, Host, ckpt, mat
 
 G = 1 << 44                                             # places that are far from each other
@@ -113,3 +114,23 @@ def test_rows_are_too_far_apart_where_a_tiles_offsets_pass_32_bits(host):
         assert forward(host, 100, 520, 200, type, ld_x=(16 << 20) // size)[0][0] == "few" and backward(host, 100, 520, 200, type, ld=(16 << 20) // size)[0][0] == "few"
         for M, K, F, ld in ((130, 130, 2_000, whole // 127 // size + 8), (40, 1_700, 90, whole // 39 // size + 8), (256, 40, 9_000, whole // 127 // size + 8)):
             assert forward(host, M, K, F, type, ld_x=ld)[0][0] == "few far" and backward(host, M, K, F, type, ld=ld)[0][0] == "few far"
+
+
+SLOTS = {"large": 2, "middle": 3, "small": 2, "few": 4, "rows2": 3, "rows4": 3}
+
+
+@pytest.mark.parametrize("way", ["forward", "backward"])
+def test_sizes_reach_the_kernels_that_they_are_for(host, way):
+    types = {"bf16": BF16, "f16": F16, "f32": F32}
+    for kernel, dtype, M, K, F in gated_sizes.cases(gated_sizes.FORWARD if way == "forward" else gated_sizes.BACKWARD):
+        found = (forward if way == "forward" else backward)(host, M, K, F, types[dtype])
+        name, groups = found[0]
+        split = kernel.endswith(", split")
+        assert name == kernel.split(",")[0] and (found[1:] != []) == split and all(k == "join" for k, _ in found[1:]), (kernel, dtype, M, K, F, found)
+        # whole steps of 128 bytes (backward of gate and of up; rows whose last load reads behind them leave their last one out), a workgroup's or wavefront's share
+        per = 32 if dtype == "f32" else 64
+        whole = K // per if way == "forward" else 2 * ((F - 8) // per)
+        tiles_m, wide = {"large": (256, 128), "middle": (128, 96), "small": (128, 64), "few": (128, 64)}.get(name, (32, 32))
+        tiles = -(-M // tiles_m) * -(-(F if way == "forward" else K) // (wide if way == "forward" else 2 * wide))
+        each = whole * tiles // groups // (int(name[4:]) if name.startswith("rows") else 1)
+        assert each >= 2 * SLOTS[name] + 1 or (way, kernel) == ("backward", "rows4, split"), (kernel, dtype, M, K, F, each)

@@ -9,9 +9,10 @@ if not torch.cuda.is_available():
     pytest.skip("needs a GPU", allow_module_level=True)
 
 import gated_plain as plain  # noqa: E402
+import gated_sizes  # noqa: E402
 import paper_2105_13336_amd as P  # noqa: E402
 from ops_plain import CAP, FLOOR, ROUND, U  # noqa: E402
-from test_gpu_gated import T, TYPES, filled, host, near, room, say, up  # noqa: E402
+from test_gpu_gated import T, TYPES, check_gated, check_gated_backward, filled, host, near, room, say, up  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -19,6 +20,24 @@ def ops():
     h = P.tensile_ops_create()
     yield h
     h.close()
+
+
+# ------------------------------------------------------------------ every kernel, with its loop in its steady state
+
+@pytest.mark.parametrize("kernel,dtype,M,K,F", gated_sizes.cases(gated_sizes.FORWARD))
+def test_forward(ops, kernel, dtype, M, K, F):
+    """Every activation, with and without biases, checkpoints, gaps between rows."""
+    check_gated(ops, dtype, M, K, F, act="gelu_tanh", bias="f32", odd=True)
+    check_gated(ops, dtype, M, K, F, act="silu", keep=False)
+    if M * F < 1_000_000 or (M, F) == (2_040, 3_901):
+        check_gated(ops, dtype, M, K, F, act="gelu", bias=dtype)
+
+
+@pytest.mark.parametrize("kernel,dtype,M,K,F", gated_sizes.cases(gated_sizes.BACKWARD))
+def test_backward(ops, kernel, dtype, M, K, F):
+    check_gated_backward(ops, dtype, M, K, F, act="gelu_tanh", odd=True)
+    if M * K < 10_000_000:
+        check_gated_backward(ops, dtype, M, K, F, act="silu", keep=False)
 
 
 # ------------------------------------------------------------------ rows far apart

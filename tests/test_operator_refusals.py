@@ -3,7 +3,7 @@ import random
 
 import pytest
 
-from host_calls import BF16, F32, SIZE, Host, ckpt, mat, ptr
+from host_calls import BF16, F16, F32, SIZE, Host, ckpt, mat, ptr
 
 G = 1 << 34                                             # places that are far from each other
 INVAL = -1
@@ -208,3 +208,90 @@ def test_a_weight_gradient_lies_by_itself(host):
     refused(grad(mat(G, N, K)), "linear_grad: dw overlaps dy")
     refused(grad(mat(2 * G + 4, N, K)), "linear_grad: dw overlaps c")
     refused(grad(mat(2 * G + G // 2, N, K, type=F32)), "linear_grad: dw overlaps c.scale")
+
+
+# ------------------------------------------------------------------ every argument by its name, and the reason
+
+def test_norm_refusals_name_the_argument(host):
+    M, K = 4, 64
+    x, g, y = mat(G, M, K), ptr(9 * G), mat(3 * G, M, K)
+    full = dict(x=x, residual=None, gamma=g, param=F32, eps=1e-6, y=y, total=None, xhat=None, rstd=ptr(8 * G))
+
+    def call(**a):
+        a = {**full, **a}
+        return host("rms_norm", a["x"], a["residual"], a["gamma"], a["param"], a["eps"], a["y"], a["total"], a["xhat"], a["rstd"])
+    allowed(call())
+    for args, message in [(dict(x=None), "x is NULL"), (dict(y=None), "y is NULL"), (dict(gamma=None), "gamma is NULL"),
+                          (dict(x=mat(0, M, K)), "x has no data (NULL)"), (dict(x=mat(G, M, K, type=7)), "x has an unknown type"),
+                          (dict(x=mat(G + 1, M, K)), "x is not aligned to its elements"), (dict(x=mat(G, M, K, K - 1)), "x has rows that overlap (ld < cols)"),
+                          (dict(x=mat(G, M, 0, 1)), "x needs rows >= 0 and cols >= 1"), (dict(x=mat(G, -1, K)), "x needs rows >= 0 and cols >= 1"),
+                          (dict(y=mat(3 * G, M, K, type=F16)), "y differs in shape or type"), (dict(y=mat(3 * G, M, K - 1)), "y differs in shape or type"),
+                          (dict(y=mat(3 * G + 1, M, K)), "y is not aligned to its elements"), (dict(residual=mat(2 * G, M + 1, K)), "residual differs in shape or type"),
+                          (dict(total=mat(2 * G, M, K, type=F32)), "total differs in shape or type"), (dict(total=y), "total is y"),
+                          (dict(xhat=place(2, M, K - 1)), "xhat differs in shape"), (dict(xhat=ckpt(2 * G, 0, M, K)), "xhat has no data (NULL)"),
+                          (dict(xhat=place(2, M, K, ld_scale=1)), "xhat has rows that overlap (ld < cols)"),
+                          (dict(param=F16), "param_type is neither TENSILE_F32 nor the activations' type"), (dict(gamma=ptr(9 * G + 2)), "gamma is not aligned to its elements"),
+                          (dict(eps=-1.0), "eps is negative or not a finite 32-bit number"), (dict(eps=1e39), "eps is negative or not a finite 32-bit number")]:
+        refused(call(**args), "rms_norm: " + message)
+
+    full_b = dict(dy=x, xhat=place(2, M, K), rstd=ptr(8 * G), gamma=g, param=F32, dresidual=None, dx=y, dgamma=ptr(7 * G))
+
+    def back_call(**a):
+        a = {**full_b, **a}
+        return host("rms_norm_backward", a["dy"], a["xhat"], a["rstd"], a["gamma"], a["param"], a["dresidual"], a["dx"], a["dgamma"])
+    allowed(back_call())
+    allowed(back_call(dgamma=None))
+    for args, message in [(dict(dy=None), "dy is NULL"), (dict(xhat=None), "xhat is NULL"), (dict(rstd=None), "rstd is NULL"), (dict(gamma=None), "gamma is NULL"),
+                          (dict(dx=None), "dx is NULL"), (dict(xhat=place(2, M, K + 1)), "xhat differs in shape"), (dict(dx=mat(3 * G, M, K + 1)), "dx differs in shape or type"),
+                          (dict(dresidual=mat(4 * G, M, K, type=F32)), "dresidual differs in shape or type"), (dict(dgamma=ptr(7 * G + 2)), "dgamma is not aligned to its elements"),
+                          (dict(param=7), "param_type is neither TENSILE_F32 nor the activations' type")]:
+        refused(back_call(**args), "rms_norm_backward: " + message)
+
+
+def test_gated_refusals_name_the_argument(host):
+    M, K, F = 4, 64, 32
+    x, w, v, h = mat(G, M, K), mat(2 * G, F, K), mat(3 * G, F, K), mat(4 * G, M, F)
+    full = dict(x=x, wg=w, wu=v, bg=None, bu=None, param=F32, act=SILU, h=h, gate=None, up=None)
+
+    def call(**a):
+        a = {**full, **a}
+        return host("gated_linear", *[a[n] for n in ("x", "wg", "wu", "bg", "bu", "param", "act", "h", "gate", "up")])
+    allowed(call())
+    allowed(call(bg=ptr(5 * G), bu=ptr(6 * G), gate=place(7, M, F), up=place(8, M, F)))
+    allowed(call(wu=w))                                                 # (weights may be one matrix: they are only read)
+    size = "is not (rows of x) x (rows of w_gate), or not of x's type"
+    for args, message in [(dict(x=None), "x is NULL"), (dict(wg=None), "w_gate is NULL"), (dict(wu=None), "w_up is NULL"), (dict(h=None), "h is NULL"),
+                          (dict(wu=mat(3 * G, F - 1, K)), "w_up differs in shape or type"), (dict(wg=mat(2 * G, F, K - 1), wu=mat(3 * G, F, K - 1)), "w_gate has not the columns of x"),
+                          (dict(wg=mat(2 * G, F, K, type=F16), wu=mat(3 * G, F, K, type=F16)), "w_gate is not of x's type"),
+                          (dict(wg=mat(2 * G, 0, K), wu=mat(3 * G, 0, K)), "w_gate has no rows"), (dict(h=mat(4 * G, M, F + 1)), "h " + size),
+                          (dict(h=mat(4 * G, M + 1, F)), "h " + size), (dict(h=mat(4 * G, M, F, type=F32)), "h " + size), (dict(h=mat(4 * G + 1, M, F)), "h is not aligned to its elements"),
+                          (dict(h=mat(G, M, F)), "h is x or a weight matrix"), (dict(h=mat(3 * G, M, F)), "h is x or a weight matrix"),
+                          (dict(bg=ptr(5 * G)), "b_gate, b_up are given one without the other"), (dict(bu=ptr(5 * G)), "b_gate, b_up are given one without the other"),
+                          (dict(bg=ptr(5 * G), bu=ptr(6 * G), param=F16), "param_type is neither TENSILE_F32 nor the activations' type"),
+                          (dict(bg=ptr(5 * G + 2), bu=ptr(6 * G)), "b_gate is not aligned to its elements"), (dict(bg=ptr(5 * G), bu=ptr(6 * G + 1)), "b_up is not aligned to its elements"),
+                          (dict(act=3), "activation is not one of TENSILE_SILU, TENSILE_GELU, TENSILE_GELU_TANH"),
+                          (dict(act=-1), "activation is not one of TENSILE_SILU, TENSILE_GELU, TENSILE_GELU_TANH"),
+                          (dict(gate=place(7, M, F - 1)), "gate differs in shape"), (dict(up=place(7, M - 1, F)), "up differs in shape"),
+                          (dict(gate=place(7, M, F), up=place(7, M, F)), "up is gate")]:
+        refused(call(**args), "gated_linear: " + message)
+
+    dh, gate, up, dgate, dup = h, place(5, M, F), place(6, M, F), mat(7 * G, M, F), mat(8 * G, M, F)
+    full_b = dict(dh=dh, gate=gate, up=up, act=SILU, dgate=dgate, dup=dup, h_c=None, wg=w, wu=v, dx=mat(9 * G, M, K))
+
+    def back_call(**a):
+        a = {**full_b, **a}
+        return host("gated_linear_backward", *[a[n] for n in ("dh", "gate", "up", "act", "dgate", "dup", "h_c", "wg", "wu", "dx")])
+    allowed(back_call())
+    allowed(back_call(wg=None, wu=None, dx=None))
+    together, like_w = "w_gate, w_up, dx are given one without the others", "w_gate has not a row for each column of dh, or is not of dh's type"
+    for args, message in [(dict(dh=None), "dh is NULL"), (dict(gate=None), "gate is NULL"), (dict(up=None), "up is NULL"), (dict(dgate=None), "dgate is NULL"), (dict(dup=None), "dup is NULL"),
+                          (dict(gate=place(5, M, F + 1)), "gate differs in shape"), (dict(up=place(6, M + 1, F)), "up differs in shape"), (dict(h_c=place(1, M, F - 1)), "h_c differs in shape"),
+                          (dict(dgate=mat(7 * G, M, F + 1)), "dgate differs in shape or type"), (dict(dup=mat(8 * G, M, F, type=F16)), "dup differs in shape or type"),
+                          (dict(dup=dgate), "dup is dgate"), (dict(act=5), "activation is not one of TENSILE_SILU, TENSILE_GELU, TENSILE_GELU_TANH"),
+                          (dict(dx=None), together), (dict(wg=None), together), (dict(wu=None), together), (dict(wg=None, wu=None), together), (dict(wu=None, dx=None), together),
+                          (dict(wg=mat(2 * G, F - 1, K), wu=mat(3 * G, F - 1, K)), like_w), (dict(wg=mat(2 * G, F, K, type=F32), wu=mat(3 * G, F, K, type=F32)), like_w),
+                          (dict(wu=mat(3 * G, F, K + 1)), "w_up differs in shape or type"),
+                          (dict(dx=mat(9 * G, M, K - 1)), "dx is not (rows of dh) x (columns of w_gate), or not of dh's type"),
+                          (dict(dx=mat(9 * G, M, K, type=F16)), "dx is not (rows of dh) x (columns of w_gate), or not of dh's type"),
+                          (dict(dx=mat(7 * G, M, K)), "dx is dgate, dup or a weight matrix"), (dict(dx=mat(3 * G, M, K)), "dx is dgate, dup or a weight matrix")]:
+        refused(back_call(**args), "gated_linear_backward: " + message)

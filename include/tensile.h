@@ -490,6 +490,8 @@ int tensile_rms_norm_backward(tensile_ops *ops, const tensile_matrix *dy, const 
                               const void *gamma, int32_t param_type, const tensile_matrix *dresidual,
                               const tensile_matrix *dx, void *dgamma, void *hip_stream);
 
+/* SiLU is within 2^-24 * (8 + 2|g|) of itself, relatively, for g >= -87.3, and 0 or off by at most 1.1e-36 below (of -inf NaN); its derivative is within
+ * 2^-24 * (8 + 2|g|)*(1 + |g|) there, and 1.1e-36 below.  The GELUs are those of tensile_gelu and tensile_gelu_backward. */
 #define TENSILE_SILU 0      /* act(g) = g/(1 + exp(-g))            */
 #define TENSILE_GELU 1      /* as tensile_gelu, tanh_form 0        */
 #define TENSILE_GELU_TANH 2 /* ... and 1                           */
@@ -512,7 +514,9 @@ int tensile_gated_linear(tensile_ops *ops, const tensile_matrix *x, const tensil
  *   dgate, dup    like dh; one of them may be dh itself
  *   h_c           checkpoint of act(g)*u, for the weight gradient of the layer that read h, or NULL; may be gate or up itself
  *   w_gate, w_up, dx  F x K, F x K and M x K, of dh's type; all or none NULL (dx is not wanted then).  dx is summed from dgate
- *                 and dup as they were rounded: the gradient that belongs to those; it may be dh where neither of them is, not one of them */
+ *                 and dup as they were rounded: the gradient that belongs to those; it may be dh where neither of them is, not one of them.
+ *                 (In TENSILE_F16 so a dgate or dup beyond 65,504 is infinite and makes its row of dx infinite or NaN, and one below 2^-14 has
+ *                 fewer bits, none below 2^-25: gradients are scaled by the program, as for any product of f16 matrices.) */
 int tensile_gated_linear_backward(tensile_ops *ops, const tensile_matrix *dh, const tensile_ckpt *gate, const tensile_ckpt *up,
                                   int32_t activation, const tensile_matrix *dgate, const tensile_matrix *dup,
                                   const tensile_ckpt *h_c, const tensile_matrix *w_gate, const tensile_matrix *w_up,

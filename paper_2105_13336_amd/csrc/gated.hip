@@ -9,7 +9,9 @@ template <typename T>
 int choose(const ::tensile_ops *ops, hipStream_t s, const ProductArgs &a) {
     if (a.M <= 32) {
         // Few features and long sums: these are split, four wavefronts to a part, where that saves more than adding them up and its launch take (4 us, and 2.5 on the
-        // host).  Whole and split, us: f32 32 x 784 x 512 14 and 9 + 4, 32 x 1568 x 544 20 and 8 + 4, 32 x 3136 x 576 33 and 9 + 5; bf16 32 x 6272 x 800 16 and 8.5 + 4.
+        // host).  Whole and split, us, one call after the other: f32 (from 1536 columns) 32 x 784 x 512 14 and 9 + 4, 32 x 1024 x 512 15.4 and 11.6, 32 x 1568 x 512 20.8 and 12.8; bf16
+        // (from 8192) 32 x 4096 x 800 12.9 and 12.8, 32 x 6272 x 800 17.3 and 14.0, 32 x 8192 x 800 20.0 and 14.4, 32 x 16384 x 512 51 and 17.7, 8 x 8192 x 2000 28.4 and 23.3.  Up to
+        // 2.5 us of the difference a host pays that waits for each call.
         const int64_t tiles = (a.R + 31) / 32, each = steps_of<T, true>(a) / 4, fill = ops->num_cus / tiles;
         constexpr int64_t kLong = sizeof(T) == 2 ? 32 : 12, kLeast = sizeof(T) == 2 ? 4 : 2;
         const int64_t most = each >= kLong ? each / kLeast : 1;

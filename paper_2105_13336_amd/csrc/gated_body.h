@@ -3,9 +3,10 @@
 //   dx[m,k] = sum_f dgate[m,f]*Wg[f,k] + sum_f dup[m,f]*Wu[f,k]
 //
 // Long batches are bound by the matrix instructions and the clock that the chip can keep up with them (1.6 to 1.7 GHz, 64 to 72 % of its cycles): 8192 x 4096 x
-// 10944 bf16 1084 us (1354 TFLOP/s; a library's product of the same size alone 1115), with checkpoints 1115 to 1133; backward 1090 to 1107 after 143 for the
-// elementwise part (a library's product alone, weights as they lie, 1040).  f32 2048 x 4096 x 4096 970 us (141 TFLOP/s of 157).  Single tokens are bound by
-// the weights' bytes: 1 x 4096 x 10944 38 us (4.7 TB/s), 1 x 4096 x 43776 120 (6.0).
+// 10944 bf16 1084 to 1089 us (1350 TFLOP/s; a library's product of the same size alone 1115 to 1124), with checkpoints 1115 to 1133; backward 1090 to 1107 after 143 for the
+// elementwise part (a library's product alone, weights as they lie, 1040 to 1080).  These are the best of loops over the one call; with inputs in turn and other kernels
+// between, on a chip that is warm, the products take 1200 to 1260 and 1110 to 1250.  f32 2048 x 4096 x 4096 970 us (141 TFLOP/s of 157), backward 1005 + 20.6
+// (137).  Single tokens are bound by the weights' bytes: 1 x 4096 x 10944 38 us (4.7 TB/s), 1 x 4096 x 43776 120 (6.0).
 //
 // On the matrix instructions with 32-bit sums: bf16 and f16 as they are, f32 on those for 32 bits (products and sums as in ordinary arithmetic).
 // A block of the result is 32 x 32; its rows are weights (f, or k backward) and its columns tokens, so that a lane holds 16 of the 32
@@ -309,9 +310,11 @@ struct Tile {
     static constexpr int kWaves = kWP * kWT, kThreads = 64 * kWaves;
     static constexpr int kP = 32 * kPB * kWP, kTok = 32 * kTB * kWT;
     // Large tiles end at about the same time, each with 64 KB of h and as much of the checkpoints; together that is what the L2 holds, and there it displaces what
-    // the next tiles share (8192 x 4096 x 10944 with checkpoints 1198 us, past the caches 1160; 8192 x 768 x 2048 65 and 59; backward 96.5 and 93.8 in all).
+    // the next tiles share (8192 x 4096 x 10944 with checkpoints 1198 us, past the caches 1160; 8192 x 768 x 2048 65 and 59; backward 96.5 and 93.8 in all).  It is no
+    // cost put off to the reader: the layer and the product that reads h together, through the caches and past them, us: 4096 x 768 x 2048, whose h is 16 MB, 61.1 and 57.6, 8192 x
+    // 768 x 2048 104 and 95, 8192 x 4096 x 10944 1642 and 1633; the backward pass and the norm's that reads dx, of 13 and 67 MB, 98.3 and 97.0, 1279 and 1277.
     static constexpr bool kPast = kP * kTok >= 192 * 128;
-    static constexpr bool kSplit = kSlots > 3;                           // what is split, or far, takes tiles of this kind
+    static constexpr bool kSplit = kSlots > 3;                           // what is split, or far, takes tiles of this kind (Few, which alone has the LDS for a fourth step)
 };
 
 // A step takes kRow bytes of a row, a line of the caches (with half a line to a step the L2 is asked twice as often, and answers a line or half of one in the same

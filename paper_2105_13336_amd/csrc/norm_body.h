@@ -538,9 +538,10 @@ uint32_t grid_of(int64_t rows, int64_t teams, int64_t most) {
 template <bool kCentred>
 int norm_forward(const ::tensile_ops *ops, hipStream_t s, const NormArgs &a, int type, int param_type) {
     const int64_t cus = ops->num_cus;
-    // The smallest team that holds the row: fewer barriers and sums, and no idle lanes.  Against the next larger one (us): 65536 x 128
+    // The smallest team that holds the row: fewer barriers and sums, and no idle lanes.  Against the next larger one, layer norm (us): 65536 x 128
     // 11.5 and 25.3; 8192 x 512 7.2 and 8.7; x 768 10.1 and 15.2; x 2048 24.5 and 25.6; x 8192 90 and 99; 4096 x 16384 89 and,
-    // in three passes, 140.
+    // in three passes, 140.  Root-mean-square norm (with a residual, its sum and a checkpoint, inputs in turn): 65536 x 128 18.2 and 26.6; 8192 x 512 10.0 and 10.2; x 768 15.0 and
+    // 15.8; x 2048 30.5 and 30.6; x 4096 57.8 and 57.2; x 8192 114 and 109; 4096 x 16384 115 and, in two passes, 137.
     by_types(type, param_type, a.cols % kChunk == 0, [&](auto t, auto p, auto even) {
         using T = decltype(t);
         using P = decltype(p);
@@ -571,9 +572,11 @@ int norm_backward(const ::tensile_ops *ops, hipStream_t s, const NormArgs &args,
     const int64_t cus = ops->num_cus;
     NormArgs a = args;
     // workgroups: what is resident, two of 512 threads to a CU (partial sums take 8 bytes a column each)
-    // Teams as above; against the next larger one (us): 65536 x 128 12.7 and 23.3; 8192 x 512 10.0 and 12.0; x 768 12.7 and 17.1; x 2048
-    // 21.4 and 26.5; x 4096 41 and 55; 4096 x 16384 113 and, in two passes, 144.
-    // (1024 threads have room for two chunks each of 16-bit gradients)
+    // Teams as above; against the next larger one, layer norm (us): 65536 x 128 12.7 and 23.3; 8192 x 512 10.0 and 12.0; x 768 12.7 and 17.1; x 2048
+    // 21.4 and 26.5; x 4096 41 and 55; 4096 x 16384 113 and, in two passes, 144.  Root-mean-square norm (with dresidual, inputs in turn): 65536 x 128 16.7 and 23.5; 8192 x 512 10.9 and 11.9;
+    // x 768 14.2 and 17.3; x 2048 26.8 and 28.7; x 4096 48 and 52; 4096 x 16384 115 and 154.
+    // (1024 threads have room for two chunks each of 16-bit gradients, but for 11 to 23 registers that are spilled in each row: 4096 x 12288 bf16 90 us for 68, 4096 x 16384 115 for 91.
+    // In 32 bits rows of more than 8192 columns are passed over twice: 4096 x 12288 199 us for 126, 4096 x 16384 266 for 169.)
     const bool is_long = a.cols > (type == TENSILE_F32 ? 8192 : 16384);
     const int teams = a.cols <= 128 ? 32 : a.cols <= 512 ? 8 : a.cols <= 1024 ? 4 : a.cols <= 2048 ? 2 : 1, per_cu = a.cols <= 4096 ? 2 : 1;
     const int64_t n_columns = (static_cast<int64_t>(a.cols) + 2047) / 2048;      // (long rows)

@@ -122,7 +122,7 @@ __device__ __forceinline__ void store8(T *p, const float (&f)[8], int left) {
     store_raw(p, r, left);
 }
 
-// The same past the caches (for what is larger than they are): of eight whole elements, else as above.
+// The same past the caches (where what is written displaces what other workgroups are about to read): of eight whole elements, else as above.
 typedef u32x4 u32x4_loose __attribute__((aligned(1)));
 typedef u32x2 u32x2_loose __attribute__((aligned(1)));
 template <typename T>
